@@ -346,6 +346,169 @@ mv_status mv_quant_encode(const float* vals, int64_t ld_vals, int64_t n, int32_t
 mv_status mv_quant_decode(const uint32_t* streams, int64_t ld_words, int64_t n, int32_t rows, int32_t q,
                           const float* means, float* out, int64_t ld_out, void* stream);
 
+/* ---- gradient norm over many tensors, and clipping ------------------------- */
+
+/*
+ * A program has every worker's gradients as a list of tensors; the vote step takes
+ * them as rows of a matrix.  For each group g of tensors (a worker's, as a rule):
+ *
+ *   norm[g] = sqrt(sum of x^2) or max |x| over all elements of the group's tensors
+ *   coef[g] = min(1, max_norm / (norm[g] + 1e-6))          (fp32)
+ *   dst     = src * coef[g]                                (fp32, rounded once to dst's type)
+ *
+ * Sums of squares are formed in fp64 in an order that depends on the sizes alone, so
+ * neither large nor small fp32 values leave the range, and equal inputs give equal
+ * norms.  A NaN makes the group's norm, coef and every dst NaN; an infinity makes norm
+ * infinite and coef 0 (dst: NaN where src is infinite or NaN, else 0): look at norm
+ * before the result is used, as with any clipping.  A group without elements has norm 0.
+ *
+ * Tensors are contiguous, aligned to their own element and at most 2^40 elements long;
+ * numel 0 (then the pointers may be NULL) is allowed; 2^37 elements in all.  dst is a tensor of its own
+ * -- a part of a matrix row at any offset, for instance -- or src itself, if the types agree; apart
+ * from that no dst overlaps another tensor.  dst NULL: the tensor only counts for its group's norm;
+ * then all tensors' must be NULL, and mv_clip_grads reports MV_ERR_STATE.
+ */
+typedef struct mv_clip mv_clip; /* opaque */
+
+typedef enum { MV_NORM_L2 = 0, MV_NORM_MAX = 1 } mv_norm;
+
+typedef struct {
+    const void* src;
+    void*       dst;
+    int64_t     numel;
+    int32_t     group;      /* 0 .. n_groups-1; in any order */
+    int16_t     src_dtype;  /* mv_dtype */
+    int16_t     dst_dtype;  /* mv_dtype */
+} mv_clip_tensor;
+
+typedef struct {
+    uint32_t struct_size;   /* = sizeof(mv_clip_config) */
+    int32_t  device;        /* HIP device ordinal */
+    int32_t  n_groups;      /* 1 .. 65535 */
+    int32_t  norm;          /* mv_norm */
+    void*    workspace;     /* optional device scratch of >= mv_clip_workspace_bytes(); NULL: the handle allocates it */
+    size_t   workspace_bytes;
+} mv_clip_config;
+
+/* Bytes of device scratch for this list; host arithmetic, 0 if anything is invalid.  `tensors` is a HOST array. */
+size_t mv_clip_workspace_bytes(const mv_clip_config* cfg, const mv_clip_tensor* tensors, int64_t n_tensors);
+
+/*
+ * Creates a handle for a list of 1 .. 2^24 tensors (a HOST array, copied).  The handle
+ * holds the tensors' ADDRESSES: they have to stay where they are until mv_clip_bind
+ * gives new ones or the handle ends.  What they hold is read by each call anew.
+ * cfg.workspace, when given, must be 256-byte aligned device memory and outlive the
+ * handle.  Waits for the upload of the list.
+ * Errors: MV_ERR_INVALID_ARG (before any device call), MV_ERR_ALLOC, MV_ERR_DEVICE.
+ */
+mv_status mv_clip_begin(const mv_clip_config* cfg, const mv_clip_tensor* tensors, int64_t n_tensors, mv_clip** out);
+
+/*
+ * Gives the tensors new addresses (HOST arrays of n_tensors pointers, in the order of
+ * mv_clip_begin; sizes, types and groups stay; dst NULL where the list had none),
+ * enqueued on `stream`: calls enqueued before use the old ones.  Allocates nothing.
+ */
+mv_status mv_clip_bind(mv_clip* clip, const void* const* src, void* const* dst, void* stream);
+
+/*
+ * Enqueues the norms of all groups on `stream`: norms = device, n_groups fp32 out.
+ * Calls on one handle must not overlap in time; like mv_vote_step they return without
+ * waiting and allocate nothing.
+ */
+mv_status mv_clip_norms(mv_clip* clip, float* norms, void* stream);
+
+/*
+ * Enqueues norms and clipping.  max_norm: finite, >= 0.  norms: device, n_groups fp32 out.
+ * coefs: the same, out, the factors that were applied; may be NULL.  Tensors clipped in place whose
+ * factor is 1 are not written.
+ */
+mv_status mv_clip_grads(mv_clip* clip, float max_norm, float* norms, float* coefs, void* stream);
+
+/* As mv_end and mv_release: waits for the stream of the last call, frees the handle's scratch; frees the handle. */
+mv_status mv_clip_end(mv_clip* clip);
+void      mv_clip_release(mv_clip* clip);
+
+/* ---- microscaled 4-bit floating point ---------------------------------------- */
+
+/*
+ * Every 32 consecutive values of a row (a block; the row's last one may be shorter)
+ * share a power of two, 2^s with s = floor(log2(largest magnitude)) - 2, at least -127;
+ * a scale byte holds s + 127.  A value is held as a 4-bit code, sign << 3 | place, for
+ * +-{0, 0.5, 1, 1.5, 2, 3, 4, 6}[place] * 2^s: the nearest one, ties to the even place,
+ * magnitudes beyond 6 to 6.  A block of zeros has s = -127.  A block that holds an infinity or a NaN gets
+ * the scale byte 255 and codes 0: all of it reads as NaN.
+ *
+ * Layout: value k of a row is bits [4 (k % 8), 4 (k % 8) + 4) of 32-bit word k / 8.  Rows are whole
+ * blocks: mv_mx_row_words(n) = 4 ceil(n / 32) words, the codes past n are 0, and
+ * mv_mx_row_scales(n) = ceil(n / 32) rounded up to 4 scale bytes, those past the last
+ * block are neither written nor used.  Codes are 16-byte aligned, ld_words a multiple
+ * of 4; scales 4-byte aligned, ld_scales a multiple of 4.
+ * Values (vals, resid, out, x, y, ...) are fp32 or bf16, aligned to their element, with
+ * any row stride >= the row; 1 <= rows, n < 2^31, at most 2^35 values in a matrix.
+ * All of these calls run on the CURRENT device, are enqueued on `stream` and allocate
+ * nothing.  Errors: MV_ERR_INVALID_ARG, MV_ERR_DEVICE.
+ */
+int64_t mv_mx_row_words(int64_t n);   /* 0 for n outside 1 .. 2^31-1 */
+int64_t mv_mx_row_scales(int64_t n);
+
+/*
+ * codes, scales = the rows of vals.  resid (fp32, may be NULL; may be vals itself, with its
+ * stride, if vals is fp32) = vals minus what the codes stand for, exact: what an error
+ * buffer keeps.
+ */
+mv_status mv_mx_encode(const void* vals, int32_t dtype, int64_t ld_vals, int64_t rows, int64_t n, uint32_t* codes,
+                       int64_t ld_words, uint8_t* scales, int64_t ld_scales, float* resid, int64_t ld_resid,
+                       void* stream);
+
+/* codes, scales = the COLUMNS of vals (rows x n): n rows of codes of `rows` values each. */
+mv_status mv_mx_encode_t(const void* vals, int32_t dtype, int64_t ld_vals, int64_t rows, int64_t n, uint32_t* codes,
+                         int64_t ld_words, uint8_t* scales, int64_t ld_scales, void* stream);
+
+/* out (rows x n, fp32 or bf16) = what the codes stand for. */
+mv_status mv_mx_decode(const uint32_t* codes, int64_t ld_words, const uint8_t* scales, int64_t ld_scales, int64_t rows,
+                       int64_t n, void* out, int32_t dtype, int64_t ld_out, void* stream);
+
+/*
+ * What the receiver of the rows (the workers' values) forms, without writing them out:
+ *   agg[k] = sum over rows r of weights[r] * value[r][k]    fp32, r ascending
+ * weights: device, rows fp32; NULL: the mean, the plain sum times fp32 1 / rows.
+ */
+mv_status mv_mx_aggregate(const uint32_t* codes, int64_t ld_words, const uint8_t* scales, int64_t ld_scales,
+                          int64_t rows, int64_t n, const float* weights, float* agg, void* stream);
+
+/*
+ * c[i][j] = sum over k of a[i][k] * b[j][k]: m rows of a, n rows of b, k values each,
+ * all in 4 bits along k; fp32 sums in an order that depends on the sizes alone; c fp32
+ * or bf16.  scratch: device, 16-byte aligned, >= mv_mx_product_scratch_bytes(m, n, k) (0: may be NULL).
+ */
+size_t    mv_mx_product_scratch_bytes(int64_t m, int64_t n, int64_t k);
+mv_status mv_mx_product(const uint32_t* a_codes, int64_t ld_aw, const uint8_t* a_scales, int64_t ld_as,
+                        const uint32_t* b_codes, int64_t ld_bw, const uint8_t* b_scales, int64_t ld_bs, int64_t m,
+                        int64_t n, int64_t k, void* c, int32_t c_dtype, int64_t ld_c, void* scratch,
+                        size_t scratch_bytes, void* stream);
+
+/*
+ * A layer with weights w (n x k) held in 4 bits along k:
+ *   y (m x n) = q(x) w^T,  q(x) = what mv_mx_encode makes of x (m x k).
+ */
+size_t    mv_mx_linear_scratch_bytes(int64_t m, int64_t n, int64_t k);
+mv_status mv_mx_linear(const void* x, int32_t x_dtype, int64_t ld_x, const uint32_t* w_codes, int64_t ld_words,
+                       const uint8_t* w_scales, int64_t ld_scales, int64_t m, int64_t n, int64_t k, void* y,
+                       int32_t y_dtype, int64_t ld_y, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * Its gradients from dy (m x n), each product with both factors in 4 bits along its own
+ * sum (rounding is passed straight through):
+ *   dx (m x k) = q(dy) wt^T            wt: the weights' COLUMNS, k rows of n values (mv_mx_encode_t of w)
+ *   dw (n x k) = qt(dy) qt(x)^T        qt: mv_mx_encode_t
+ * dx or dw may be NULL (then x, or wt_codes and wt_scales, may be too); x and dy have the same type.
+ */
+size_t    mv_mx_linear_grad_scratch_bytes(int64_t m, int64_t n, int64_t k);
+mv_status mv_mx_linear_grad(const void* x, int64_t ld_x, const void* dy, int64_t ld_dy, int32_t dtype,
+                            const uint32_t* wt_codes, int64_t ld_words, const uint8_t* wt_scales, int64_t ld_scales,
+                            int64_t m, int64_t n, int64_t k, void* dx, int32_t dx_dtype, int64_t ld_dx, void* dw,
+                            int32_t dw_dtype, int64_t ld_dw, void* scratch, size_t scratch_bytes, void* stream);
+
 /*
  * Measurement aid, not part of the method: enqueues a plain streaming copy of
  * `bytes` (a multiple of 16; dst and src 16-byte aligned DEVICE pointers, not

@@ -17,6 +17,7 @@ MV_OK, MV_ERR_INVALID_ARG, MV_ERR_UNSUPPORTED, MV_ERR_ALLOC, MV_ERR_DEVICE, MV_E
 MV_F32, MV_BF16 = 0, 1
 MV_REDUCE_MEAN, MV_REDUCE_SUM = 0, 1
 MV_FLAG_ADD_DROP = 1
+MV_NORM_L2, MV_NORM_MAX = 0, 1
 
 # every symbol include/mv.h declares
 ABI_SYMBOLS = (
@@ -25,6 +26,11 @@ ABI_SYMBOLS = (
     "mv_last_step_row_stats", "mv_probe_copy",
     "mv_codec_stream_bits", "mv_codec_scratch_bytes", "mv_codec_encode", "mv_codec_decode", "mv_codec_decode_static",
     "mv_quant_scratch_bytes", "mv_quant_encode", "mv_quant_decode",
+    "mv_clip_workspace_bytes", "mv_clip_begin", "mv_clip_bind", "mv_clip_norms", "mv_clip_grads", "mv_clip_end",
+    "mv_clip_release",
+    "mv_mx_row_words", "mv_mx_row_scales", "mv_mx_encode", "mv_mx_encode_t", "mv_mx_decode", "mv_mx_aggregate",
+    "mv_mx_product_scratch_bytes", "mv_mx_product", "mv_mx_linear_scratch_bytes", "mv_mx_linear",
+    "mv_mx_linear_grad_scratch_bytes", "mv_mx_linear_grad",
 )
 
 
@@ -38,6 +44,28 @@ class mv_config(ctypes.Structure):
         ("k", ctypes.c_int64),
         ("reduce", ctypes.c_int32),
         ("flags", ctypes.c_int32),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class mv_clip_tensor(ctypes.Structure):
+    _fields_ = [
+        ("src", ctypes.c_void_p),
+        ("dst", ctypes.c_void_p),
+        ("numel", ctypes.c_int64),
+        ("group", ctypes.c_int32),
+        ("src_dtype", ctypes.c_int16),
+        ("dst_dtype", ctypes.c_int16),
+    ]
+
+
+class mv_clip_config(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("device", ctypes.c_int32),
+        ("n_groups", ctypes.c_int32),
+        ("norm", ctypes.c_int32),
         ("workspace", ctypes.c_void_p),
         ("workspace_bytes", ctypes.c_size_t),
     ]
@@ -108,6 +136,34 @@ def load() -> ctypes.CDLL:
     L.mv_quant_encode.restype = i32
     L.mv_quant_decode.argtypes = [vp, i64, i64, i32, i32, vp, vp, i64, vp]
     L.mv_quant_decode.restype = i32
+    sz, f32 = ctypes.c_size_t, ctypes.c_float
+    L.mv_clip_workspace_bytes.argtypes = [ctypes.POINTER(mv_clip_config), vp, i64]
+    L.mv_clip_workspace_bytes.restype = sz
+    L.mv_clip_begin.argtypes = [ctypes.POINTER(mv_clip_config), vp, i64, ctypes.POINTER(vp)]
+    L.mv_clip_bind.argtypes = [vp, vp, vp, vp]
+    L.mv_clip_norms.argtypes = [vp, vp, vp]
+    L.mv_clip_grads.argtypes = [vp, f32, vp, vp, vp]
+    L.mv_clip_end.argtypes = [vp]
+    L.mv_clip_release.argtypes = [vp]
+    L.mv_clip_release.restype = None
+    L.mv_mx_row_words.argtypes = [i64]
+    L.mv_mx_row_words.restype = i64
+    L.mv_mx_row_scales.argtypes = [i64]
+    L.mv_mx_row_scales.restype = i64
+    L.mv_mx_encode.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp]
+    L.mv_mx_encode_t.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp]
+    L.mv_mx_decode.argtypes = [vp, i64, vp, i64, i64, i64, vp, i32, i64, vp]
+    L.mv_mx_aggregate.argtypes = [vp, i64, vp, i64, i64, i64, vp, vp, vp]
+    for f in (L.mv_mx_product_scratch_bytes, L.mv_mx_linear_scratch_bytes, L.mv_mx_linear_grad_scratch_bytes):
+        f.argtypes = [i64, i64, i64]
+        f.restype = sz
+    L.mv_mx_product.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, vp, sz, vp]
+    L.mv_mx_linear.argtypes = [vp, i32, i64, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, vp, sz, vp]
+    L.mv_mx_linear_grad.argtypes = [vp, i64, vp, i64, i32, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, vp, i32, i64,
+                                    vp, sz, vp]
+    for f in (L.mv_clip_begin, L.mv_clip_bind, L.mv_clip_norms, L.mv_clip_grads, L.mv_clip_end, L.mv_mx_encode,
+              L.mv_mx_encode_t, L.mv_mx_decode, L.mv_mx_aggregate, L.mv_mx_product, L.mv_mx_linear, L.mv_mx_linear_grad):
+        f.restype = i32
     L.mv_probe_copy.argtypes = [vp, vp, ctypes.c_size_t, vp]
     L.mv_probe_copy.restype = i32
     _lib = L
@@ -318,3 +374,287 @@ def mv_quant_decode(streams, n: int, q: int, means, out, stream=None) -> None:
                                 _dev_ptr(out), out.stride(0), _stream_handle(stream, out))
     if st != MV_OK:
         raise MvError(st, "mv_quant_decode")
+
+
+# ---- gradient norm over many tensors, and clipping ---------------------------------
+
+_dtypes = None      # torch.float32 and torch.bfloat16 to mv_dtype, once torch is there
+
+
+def _value_type(t, what: str) -> int:
+    """mv_dtype of a float32 or bfloat16 tensor."""
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {torch.float32: MV_F32, torch.bfloat16: MV_BF16}
+    d = _dtypes.get(t.dtype)
+    if d is None:
+        raise ValueError("%s is %s: float32 or bfloat16 is wanted" % (what, t.dtype))
+    return d
+
+
+def _float32(t, what: str, numel: int, device: int) -> int:
+    """Address of a contiguous float32 device tensor of at least numel values; 0 for None."""
+    if t is None:
+        return 0
+    if _value_type(t, what) != MV_F32 or not t.is_contiguous() or t.numel() < numel or t.get_device() != device:
+        raise ValueError("%s has to be contiguous float32 of %d values or more on the same GPU" % (what, numel))
+    return t.data_ptr()
+
+
+def _pieces(t, o):
+    """A tensor and where its clipped values go (or None) as pairs of contiguous pieces in the same order of elements."""
+    if o is not None and o.shape != t.shape:
+        raise ValueError("a tensor of shape %s does not go to one of %s" % (tuple(t.shape), tuple(o.shape)))
+    if t.is_contiguous() and (o is None or o.is_contiguous()):
+        yield t, o
+        return
+    # dense in another order of its dimensions, as both have it
+    order = sorted(range(t.dim()), key=lambda i: -t.stride(i))
+    p, q = t.permute(order), o.permute(order) if o is not None else None
+    if p.is_contiguous() and (q is None or q.is_contiguous()):
+        yield p, q
+        return
+    if t.dim() < 2:
+        raise ValueError("a gradient's elements have to lie one behind the other in its last dimension")
+    for i in range(t.shape[0]):
+        yield from _pieces(t[i], o[i] if o is not None else None)
+
+
+class _Clip(ctypes.c_void_p):
+    """Handle of mv_clip_begin, with what the calls on it check against."""
+    n_groups = 0
+    device = -1
+    sizes = ()          # (shape, dtype, out's dtype or None) of each tensor given
+
+
+def _clip_list(tensors, out, groups, device):
+    """The list as the library takes it, and the tensors' shapes and types."""
+    tensors, out = list(tensors), list(out) if out is not None else None
+    if not tensors or (out is not None and len(out) != len(tensors)):
+        raise ValueError("as many tensors to write as to read, and at least one")
+    if len(groups) != len(tensors):
+        raise ValueError("a group for each tensor is wanted")
+    rows, sizes = [], []
+    for i, t in enumerate(tensors):
+        o = out[i] if out is not None else None
+        if t.get_device() != device or (o is not None and o.get_device() != device):
+            raise ValueError("all tensors have to be on one GPU")
+        ts, to = _value_type(t, "a gradient"), _value_type(o, "a gradient's place") if o is not None else MV_F32
+        sizes.append((t.shape, t.dtype, None if o is None else o.dtype))
+        if t.is_contiguous() and (o is None or (o.shape == t.shape and o.is_contiguous())):
+            rows.append((t.data_ptr(), o.data_ptr() if o is not None else 0, t.numel(), groups[i], ts, to))
+        else:
+            rows += [(a.data_ptr(), b.data_ptr() if b is not None else 0, a.numel(), groups[i], ts, to)
+                     for a, b in _pieces(t, o)]
+    return rows, sizes
+
+
+def mv_clip_begin(tensors, out=None, groups=None, norm: int = MV_NORM_L2, n_groups: Optional[int] = None,
+                  workspace: int = 0, workspace_bytes: int = 0) -> _Clip:
+    """A handle for the gradients `tensors` (torch device tensors, float32 or bfloat16, any mixture), groups[i] being the
+    group that tensor i counts for (all one group by default).  out[i] is where its clipped values go: a tensor of the
+    same shape, a view of a matrix row for instance, or tensors[i] itself; None: norms only.  Tensors that are not
+    dense are taken apart into rows; both have to be dense in the same order.  Keep all of them alive and in place as
+    long as the handle uses them (mv_clip_bind gives it others).  End it with mv_clip_end and mv_clip_release."""
+    tensors = list(tensors)
+    device = tensors[0].get_device() if tensors else -1
+    groups = [0] * len(tensors) if groups is None else [int(g) for g in groups]
+    rows, sizes = _clip_list(tensors, out, groups, device)
+    n_groups = max(groups) + 1 if n_groups is None else int(n_groups)
+    cfg = mv_clip_config(ctypes.sizeof(mv_clip_config), device, n_groups, norm, workspace or None, workspace_bytes)
+    h = _Clip()
+    st = load().mv_clip_begin(ctypes.byref(cfg), (mv_clip_tensor * len(rows))(*rows), len(rows), ctypes.byref(h))
+    if st != MV_OK:
+        raise MvError(st, "mv_clip_begin")
+    h.n_groups, h.device, h.sizes, h.groups = n_groups, device, sizes, groups
+    h.rows = [r[2:] for r in rows]
+    return h
+
+
+def mv_clip_bind(clip: _Clip, tensors, out=None, stream=None) -> None:
+    """The handle's tensors from now on (in the stream's order): others of the same shapes, types and strides."""
+    tensors = list(tensors)
+    rows, sizes = _clip_list(tensors, out, clip.groups, clip.device)
+    if sizes != clip.sizes or [r[2:] for r in rows] != clip.rows:
+        raise ValueError("the tensors' shapes, types and strides have to be those the handle was made for")
+    pointers = ctypes.c_void_p * len(rows)
+    st = load().mv_clip_bind(clip, pointers(*[r[0] for r in rows]), pointers(*[r[1] for r in rows]),
+                             _stream_handle(stream, tensors[0]))
+    if st != MV_OK:
+        raise MvError(st, "mv_clip_bind")
+
+
+def mv_clip_norms(clip: _Clip, norms, stream=None) -> None:
+    """norms: n_groups float32 on the device, out."""
+    st = load().mv_clip_norms(clip, _float32(norms, "norms", clip.n_groups, clip.device), _stream_handle(stream, norms))
+    if st != MV_OK:
+        raise MvError(st, "mv_clip_norms")
+
+
+def mv_clip_grads(clip: _Clip, max_norm: float, norms, coefs=None, stream=None) -> None:
+    """The clipped gradients in the handle's `out` tensors; norms and coefs (may be None): n_groups float32, out."""
+    st = load().mv_clip_grads(clip, max_norm, _float32(norms, "norms", clip.n_groups, clip.device),
+                              _float32(coefs, "coefs", clip.n_groups, clip.device), _stream_handle(stream, norms))
+    if st != MV_OK:
+        raise MvError(st, "mv_clip_grads")
+
+
+def mv_clip_end(clip: _Clip) -> None:
+    st = load().mv_clip_end(clip)
+    if st != MV_OK:
+        raise MvError(st, "mv_clip_end")
+
+
+def mv_clip_release(clip: _Clip) -> None:
+    """Frees the handle, which must not be used any more."""
+    load().mv_clip_release(clip)
+    clip.value = None
+
+
+# ---- microscaled 4-bit floating point ----------------------------------------------
+
+
+def mv_mx_row_words(n: int) -> int:
+    return int(load().mv_mx_row_words(n))
+
+
+def mv_mx_row_scales(n: int) -> int:
+    return int(load().mv_mx_row_scales(n))
+
+
+def _matrix(t, what: str, shape, device: int):
+    """(address, mv_dtype, row stride) of a float32 or bfloat16 matrix with unit column stride."""
+    d = _value_type(t, what)
+    if t.shape != shape or t.get_device() != device:
+        raise ValueError("%s is %s on GPU %d: %s on GPU %d is wanted" % (what, tuple(t.shape), t.get_device(), tuple(shape), device))
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
+        raise ValueError("%s has a column stride of %d: 1 is wanted" % (what, step))
+    return t.data_ptr(), d, ld if shape[0] > 1 else max(ld, shape[1])
+
+
+def _codes(codes, scales, rows: int, n: int, device: int, what: str = "codes"):
+    """(address, row stride) of both, for `rows` rows of n values."""
+    blocks = (n + 31) // 32
+    if (codes.element_size() != 4 or scales.element_size() != 1 or codes.get_device() != device or scales.get_device() != device
+            or codes.dim() != 2 or scales.dim() != 2 or codes.shape[0] < rows or scales.shape[0] < rows
+            or codes.shape[1] < 4 * blocks or scales.shape[1] < (blocks + 3) // 4 * 4 or codes.stride(1) != 1
+            or scales.stride(1) != 1):
+        raise ValueError("%s and scales have to be %d rows of mv_mx_row_words(%d) 32-bit words and mv_mx_row_scales(%d) bytes "
+                         "or more, on the same GPU" % (what, rows, n, n))
+    return codes.data_ptr(), codes.stride(0), scales.data_ptr(), scales.stride(0)
+
+
+def _scratch_of(scratch, device: int):
+    if scratch is None:
+        return 0, 0
+    if scratch.get_device() != device or not scratch.is_contiguous():
+        raise ValueError("scratch has to be contiguous memory on the same GPU")
+    return scratch.data_ptr(), scratch.numel() * scratch.element_size()
+
+
+def mv_mx_encode(vals, codes, scales, resid=None, stream=None) -> None:
+    """vals: rows x n float32 or bfloat16; codes: rows x mv_mx_row_words(n) int32 (out); scales: rows x
+    mv_mx_row_scales(n) uint8 (out); resid: rows x n float32 (out), vals less what the codes stand for; vals itself
+    may be given."""
+    rows, n = vals.shape
+    device = vals.get_device()
+    v, d, ld = _matrix(vals, "vals", vals.shape, device)
+    c, ld_c, s, ld_s = _codes(codes, scales, rows, n, device)
+    r, ld_r = 0, 0
+    if resid is not None:
+        r, rd, ld_r = _matrix(resid, "resid", vals.shape, device)
+        if rd != MV_F32:
+            raise ValueError("resid has to be float32")
+    st = load().mv_mx_encode(v, d, ld, rows, n, c, ld_c, s, ld_s, r, ld_r, _stream_handle(stream, vals))
+    if st != MV_OK:
+        raise MvError(st, "mv_mx_encode")
+
+
+def mv_mx_encode_t(vals, codes, scales, stream=None) -> None:
+    """The columns of vals (rows x n): codes: n x mv_mx_row_words(rows), scales: n x mv_mx_row_scales(rows) (out)."""
+    rows, n = vals.shape
+    device = vals.get_device()
+    v, d, ld = _matrix(vals, "vals", vals.shape, device)
+    st = load().mv_mx_encode_t(v, d, ld, rows, n, *_codes(codes, scales, n, rows, device), _stream_handle(stream, vals))
+    if st != MV_OK:
+        raise MvError(st, "mv_mx_encode_t")
+
+
+def mv_mx_decode(codes, scales, out, stream=None) -> None:
+    """out: rows x n float32 or bfloat16 (out), what the codes stand for."""
+    rows, n = out.shape
+    device = out.get_device()
+    o, d, ld = _matrix(out, "out", out.shape, device)
+    st = load().mv_mx_decode(*_codes(codes, scales, rows, n, device), rows, n, o, d, ld, _stream_handle(stream, out))
+    if st != MV_OK:
+        raise MvError(st, "mv_mx_decode")
+
+
+def mv_mx_aggregate(codes, scales, weights, agg, stream=None) -> None:
+    """agg: n float32 (out), the rows' weighted sum; weights: a float32 for each row of codes, or None for the mean."""
+    rows, n, device = codes.shape[0], agg.numel(), agg.get_device()
+    st = load().mv_mx_aggregate(*_codes(codes, scales, rows, n, device), rows, n, _float32(weights, "weights", rows, device),
+                                _float32(agg, "agg", n, device), _stream_handle(stream, agg))
+    if st != MV_OK:
+        raise MvError(st, "mv_mx_aggregate")
+
+
+def mv_mx_product_scratch_bytes(m: int, n: int, k: int) -> int:
+    return int(load().mv_mx_product_scratch_bytes(m, n, k))
+
+
+def mv_mx_product(a_codes, a_scales, b_codes, b_scales, k: int, out, scratch=None, stream=None) -> None:
+    """out (m x n, float32 or bfloat16) = a b^T: a of m rows and b of n rows, k values each, in 4 bits along k.
+    scratch: mv_mx_product_scratch_bytes(m, n, k) bytes."""
+    m, n = out.shape
+    device = out.get_device()
+    o, d, ld = _matrix(out, "out", out.shape, device)
+    st = load().mv_mx_product(*_codes(a_codes, a_scales, m, k, device, "a_codes"), *_codes(b_codes, b_scales, n, k, device, "b_codes"),
+                              m, n, k, o, d, ld, *_scratch_of(scratch, device), _stream_handle(stream, out))
+    if st != MV_OK:
+        raise MvError(st, "mv_mx_product")
+
+
+def mv_mx_linear_scratch_bytes(m: int, n: int, k: int) -> int:
+    return int(load().mv_mx_linear_scratch_bytes(m, n, k))
+
+
+def mv_mx_linear(x, w_codes, w_scales, out, scratch, stream=None) -> None:
+    """out (m x n) = q(x) w^T: x m x k, rounded to 4 bits as mv_mx_encode does; w: n rows of k values in 4 bits."""
+    m, k = x.shape
+    n = out.shape[1]
+    device = out.get_device()
+    a, xd, ld_x = _matrix(x, "x", x.shape, device)
+    o, d, ld = _matrix(out, "out", (m, n), device)
+    st = load().mv_mx_linear(a, xd, ld_x, *_codes(w_codes, w_scales, n, k, device, "w_codes"), m, n, k, o, d, ld,
+                             *_scratch_of(scratch, device), _stream_handle(stream, out))
+    if st != MV_OK:
+        raise MvError(st, "mv_mx_linear")
+
+
+def mv_mx_linear_grad_scratch_bytes(m: int, n: int, k: int) -> int:
+    return int(load().mv_mx_linear_grad_scratch_bytes(m, n, k))
+
+
+def mv_mx_linear_grad(x, dy, wt_codes, wt_scales, dx, dw, scratch, stream=None) -> None:
+    """dx (m x k) = q(dy) wt^T and dw (n x k) = qt(dy) qt(x)^T of mv_mx_linear's product; wt: the weights' columns, k
+    rows of n values in 4 bits.  dx (with wt_codes and wt_scales) or dw (with x) may be None; x and dy have one type."""
+    m, n = dy.shape
+    device = dy.get_device()
+    k = dx.shape[1] if dx is not None else x.shape[1]
+    g, yd, ld_dy = _matrix(dy, "dy", dy.shape, device)
+    a, ld_x, w, o, od, ld_dx, p, pd, ld_dw = 0, 0, (0, 0, 0, 0), 0, 0, 0, 0, 0, 0
+    if dx is not None:
+        w = _codes(wt_codes, wt_scales, k, n, device, "wt_codes")
+        o, od, ld_dx = _matrix(dx, "dx", (m, k), device)
+    if dw is not None:
+        a, xd, ld_x = _matrix(x, "x", (m, k), device)
+        if xd != yd:
+            raise ValueError("x and dy have to be of one type")
+        p, pd, ld_dw = _matrix(dw, "dw", (n, k), device)
+    st = load().mv_mx_linear_grad(a, ld_x, g, ld_dy, yd, *w, m, n, k, o, od, ld_dx, p, pd, ld_dw,
+                                  *_scratch_of(scratch, device), _stream_handle(stream, dy))
+    if st != MV_OK:
+        raise MvError(st, "mv_mx_linear_grad")

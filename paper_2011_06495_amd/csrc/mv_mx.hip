@@ -1,0 +1,248 @@
+// Microscaled 4-bit floating point (mv_mx_* of include/mv.h): quantising rows or columns, reading back, and the
+// receiver's sum over the workers.
+//
+// All of these read and write each value once and compute a few instructions on it: HBM bounds them, launches where they
+// are short.  Four lanes take a block of 32 values, eight each, so the block's largest magnitude is two DPP moves away and
+// a lane writes a whole word of codes.
+#include "mv_mx.hpp"
+
+namespace mvx {
+
+constexpr int kThreads = 256;
+
+// (row, block of the row) of the block that this group of four lanes takes: workgroups take kThreads / 4 consecutive
+// blocks of the rows one after the other.
+struct Place {
+    int64_t row, block;
+};
+__device__ __forceinline__ Place place_of(int64_t first_block, int64_t row_blocks)
+{
+    Place p = {first_block / row_blocks, 0};          // uniform
+    p.block = first_block - p.row * row_blocks + threadIdx.x / 4;
+    if (p.block >= row_blocks) {
+        if (row_blocks <= kThreads / 4) {
+            const uint32_t more = (uint32_t)p.block / (uint32_t)row_blocks;
+            p.row += more;
+            p.block -= (int64_t)more * row_blocks;
+        } else {
+            p.row += 1;
+            p.block -= row_blocks;
+        }
+    }
+    return p;
+}
+
+template <typename T, bool RESID>
+__global__ __launch_bounds__(kThreads) void mv_mx_encode_kernel(const T* vals, int64_t ld_vals, int64_t rows, int64_t n,
+                                                                uint32_t* __restrict__ codes, int64_t ld_words,
+                                                                uint8_t* __restrict__ scales, int64_t ld_scales, float* resid,
+                                                                int64_t ld_resid)
+{
+    const Place p = place_of((int64_t)blockIdx.x * (kThreads / 4), blocks_of(n));
+    if (p.row >= rows) return;                         // whole groups of four lanes
+    const int64_t at = p.block * kBlock + (threadIdx.x & 3) * 8;
+    float x[8];
+    load8(vals + p.row * ld_vals + at, n - at, x);
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    const uint32_t scale = scale_of(top_of_quad(top));
+    const uint32_t w = encode8(x, scale);
+    codes[p.row * ld_words + at / 8] = w;
+    if ((threadIdx.x & 3) == 0) scales[p.row * ld_scales + p.block] = (uint8_t)scale;
+    if constexpr (RESID) {
+        float held[8];
+        decode8(w, scale, held);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] -= held[i];
+        store8(resid + p.row * ld_resid + at, n - at, x);
+    }
+}
+
+// Columns: a wavefront takes 32 rows, a lane a column of them, so a lane has a block; the codes of kTileBlocks wavefronts
+// then go out in runs of 16 kTileBlocks bytes per column.
+constexpr int kTileBlocks = 4;
+template <typename T>
+__global__ __launch_bounds__(64 * kTileBlocks) void mv_mx_encode_t_kernel(const T* __restrict__ vals, int64_t ld_vals,
+                                                                          int64_t rows, int64_t n, int64_t tiles,
+                                                                          uint32_t* __restrict__ codes, int64_t ld_words,
+                                                                          uint8_t* __restrict__ scales, int64_t ld_scales)
+{
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x / 64;
+    const int64_t tile = (int64_t)blockIdx.x % tiles, strip = (int64_t)blockIdx.x / tiles;   // of columns, of rows
+    const int64_t col = tile * 64 + lane, block = strip * kTileBlocks + wave;
+    __shared__ u32x4 out[64][kTileBlocks];
+    __shared__ uint8_t held[64][kTileBlocks];
+    const int64_t row0 = block * kBlock;
+    float x[4][8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        float v = 0.0f;
+        if (col < n && row0 + i < rows) {
+            if constexpr (sizeof(T) == 2) v = widen(vals[(row0 + i) * ld_vals + col]);
+            else v = vals[(row0 + i) * ld_vals + col];
+        }
+        x[i / 8][i % 8] = v;
+        top = max(top, __float_as_uint(v) & 0x7FFFFFFFu);
+    }
+    const uint32_t scale = scale_of(top);
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = encode8(x[i], scale);
+    out[lane][wave] = w;
+    held[lane][wave] = (uint8_t)scale;
+    __syncthreads();
+    const uint32_t c = threadIdx.x / kTileBlocks, b = threadIdx.x % kTileBlocks;
+    const int64_t to = tile * 64 + c, to_block = strip * kTileBlocks + b;
+    if (to < n && to_block < blocks_of(rows)) {
+        *reinterpret_cast<u32x4*>(codes + to * ld_words + to_block * 4) = out[c][b];
+        scales[to * ld_scales + to_block] = held[c][b];
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void mv_mx_decode_kernel(const uint32_t* __restrict__ codes, int64_t ld_words,
+                                                                const uint8_t* __restrict__ scales, int64_t ld_scales,
+                                                                int64_t rows, int64_t n, T* __restrict__ out, int64_t ld_out)
+{
+    const Place p = place_of((int64_t)blockIdx.x * (kThreads / 4), blocks_of(n));
+    if (p.row >= rows) return;
+    const int64_t at = p.block * kBlock + (threadIdx.x & 3) * 8;
+    float x[8];
+    decode8(codes[p.row * ld_words + at / 8], scales[p.row * ld_scales + p.block], x);
+    store8(out + p.row * ld_out + at, n - at, x);
+}
+
+// A lane adds up eight values over the rows.
+__global__ __launch_bounds__(kThreads) void mv_mx_aggregate_kernel(const uint32_t* __restrict__ codes, int64_t ld_words,
+                                                                   const uint8_t* __restrict__ scales, int64_t ld_scales,
+                                                                   int64_t rows, int64_t n, const float* __restrict__ weights,
+                                                                   float mean, float* __restrict__ agg)
+{
+    const int64_t word = (int64_t)blockIdx.x * kThreads + threadIdx.x, at = word * 8;
+    if (at >= n) return;
+    float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int kAhead = 8;
+    for (int64_t r0 = 0; r0 < rows; r0 += kAhead) {
+        uint32_t w[kAhead], s[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t r = r0 + i < rows ? r0 + i : rows - 1;
+            w[i] = codes[r * ld_words + word];
+            s[i] = scales[r * ld_scales + word / 4];
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (r0 + i >= rows) break;
+            float x[8];
+            decode8(w[i], s[i], x);
+            const float f = weights ? weights[r0 + i] : 1.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += f * x[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] *= mean;
+    store8(agg + at, n - at, sum);
+}
+
+mv_status launch_encode(const void* vals, int32_t dtype, int64_t ld_vals, int64_t rows, int64_t n, uint32_t* codes,
+                        int64_t ld_words, uint8_t* scales, int64_t ld_scales, float* resid, int64_t ld_resid, hipStream_t st)
+{
+    const int64_t groups = (rows * blocks_of(n) + kThreads / 4 - 1) / (kThreads / 4);
+    if (groups > kMostGroups) return MV_ERR_INVALID_ARG;
+    const dim3 grid((uint32_t)groups), threads(kThreads);
+#define MV_MX_ENCODE(T, R)                                                                                             \
+    hipLaunchKernelGGL((mv_mx_encode_kernel<T, R>), grid, threads, 0, st, static_cast<const T*>(vals), ld_vals, rows,  \
+                       n, codes, ld_words, scales, ld_scales, resid, ld_resid)
+    if (dtype == MV_BF16) {
+        if (resid) MV_MX_ENCODE(uint16_t, true);
+        else MV_MX_ENCODE(uint16_t, false);
+    } else {
+        if (resid) MV_MX_ENCODE(float, true);
+        else MV_MX_ENCODE(float, false);
+    }
+#undef MV_MX_ENCODE
+    return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
+}
+
+mv_status launch_encode_t(const void* vals, int32_t dtype, int64_t ld_vals, int64_t rows, int64_t n, uint32_t* codes,
+                          int64_t ld_words, uint8_t* scales, int64_t ld_scales, hipStream_t st)
+{
+    const int64_t tiles = (n + 63) / 64, strips = (blocks_of(rows) + kTileBlocks - 1) / kTileBlocks;
+    if (tiles * strips > kMostGroups) return MV_ERR_INVALID_ARG;
+    const dim3 grid((uint32_t)(tiles * strips)), threads(64 * kTileBlocks);
+    if (dtype == MV_BF16)
+        hipLaunchKernelGGL(mv_mx_encode_t_kernel<uint16_t>, grid, threads, 0, st, static_cast<const uint16_t*>(vals), ld_vals,
+                           rows, n, tiles, codes, ld_words, scales, ld_scales);
+    else
+        hipLaunchKernelGGL(mv_mx_encode_t_kernel<float>, grid, threads, 0, st, static_cast<const float*>(vals), ld_vals, rows,
+                           n, tiles, codes, ld_words, scales, ld_scales);
+    return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
+}
+
+}  // namespace mvx
+
+extern "C" {
+
+int64_t mv_mx_row_words(int64_t n) { return mvx::size_valid(n) ? 4 * mvx::blocks_of(n) : 0; }
+int64_t mv_mx_row_scales(int64_t n) { return mvx::size_valid(n) ? (mvx::blocks_of(n) + 3) / 4 * 4 : 0; }
+
+mv_status mv_mx_encode(const void* vals, int32_t dtype, int64_t ld_vals, int64_t rows, int64_t n, uint32_t* codes,
+                       int64_t ld_words, uint8_t* scales, int64_t ld_scales, float* resid, int64_t ld_resid, void* stream)
+{
+    using namespace mvx;
+    if (!size_valid(rows) || !size_valid(n) || !values_valid(vals, dtype, ld_vals, n) ||
+        !codes_valid(codes, ld_words, scales, ld_scales, n))
+        return MV_ERR_INVALID_ARG;
+    if (resid && (!values_valid(resid, MV_F32, ld_resid, n) || (vals == resid && (dtype != MV_F32 || ld_vals != ld_resid))))
+        return MV_ERR_INVALID_ARG;
+    return launch_encode(vals, dtype, ld_vals, rows, n, codes, ld_words, scales, ld_scales, resid, ld_resid,
+                         static_cast<hipStream_t>(stream));
+}
+
+mv_status mv_mx_encode_t(const void* vals, int32_t dtype, int64_t ld_vals, int64_t rows, int64_t n, uint32_t* codes,
+                         int64_t ld_words, uint8_t* scales, int64_t ld_scales, void* stream)
+{
+    using namespace mvx;
+    if (!size_valid(rows) || !size_valid(n) || !values_valid(vals, dtype, ld_vals, n) ||
+        !codes_valid(codes, ld_words, scales, ld_scales, rows))
+        return MV_ERR_INVALID_ARG;
+    return launch_encode_t(vals, dtype, ld_vals, rows, n, codes, ld_words, scales, ld_scales, static_cast<hipStream_t>(stream));
+}
+
+mv_status mv_mx_decode(const uint32_t* codes, int64_t ld_words, const uint8_t* scales, int64_t ld_scales, int64_t rows,
+                       int64_t n, void* out, int32_t dtype, int64_t ld_out, void* stream)
+{
+    using namespace mvx;
+    if (!size_valid(rows) || !size_valid(n) || !values_valid(out, dtype, ld_out, n) ||
+        !codes_valid(codes, ld_words, scales, ld_scales, n))
+        return MV_ERR_INVALID_ARG;
+    const int64_t groups = (rows * blocks_of(n) + kThreads / 4 - 1) / (kThreads / 4);
+    if (groups > kMostGroups) return MV_ERR_INVALID_ARG;
+    const dim3 grid((uint32_t)groups), threads(kThreads);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (dtype == MV_BF16)
+        hipLaunchKernelGGL(mv_mx_decode_kernel<uint16_t>, grid, threads, 0, st, codes, ld_words, scales, ld_scales, rows, n,
+                           static_cast<uint16_t*>(out), ld_out);
+    else
+        hipLaunchKernelGGL(mv_mx_decode_kernel<float>, grid, threads, 0, st, codes, ld_words, scales, ld_scales, rows, n,
+                           static_cast<float*>(out), ld_out);
+    return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
+}
+
+mv_status mv_mx_aggregate(const uint32_t* codes, int64_t ld_words, const uint8_t* scales, int64_t ld_scales, int64_t rows,
+                          int64_t n, const float* weights, float* agg, void* stream)
+{
+    using namespace mvx;
+    if (!size_valid(rows) || !size_valid(n) || !values_valid(agg, MV_F32, n, n) ||
+        !codes_valid(codes, ld_words, scales, ld_scales, n) || (reinterpret_cast<uintptr_t>(weights) & 3))
+        return MV_ERR_INVALID_ARG;
+    const int64_t groups = ((n + 7) / 8 + kThreads - 1) / kThreads;
+    hipLaunchKernelGGL(mv_mx_aggregate_kernel, dim3((uint32_t)groups), dim3(kThreads), 0, static_cast<hipStream_t>(stream), codes,
+                       ld_words, scales, ld_scales, rows, n, weights, weights ? 1.0f : 1.0f / (float)rows, agg);
+    return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
+}
+
+}  // extern "C"

@@ -1,0 +1,345 @@
+"""Norms of many tensors and clipping by them, against numpy in 64 bits: norms to one rounding to fp32, maxima exactly, and
+the clipped values exactly as the products of the norms that came back."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2011_06495_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+GUARD = -12345.5
+
+
+@pytest.fixture(autouse=True)
+def say(request):
+    print("[case] " + request.node.name, flush=True)
+
+
+def f32(t):
+    return t.detach().float().cpu().numpy()
+
+
+def norm64(arrays, kind):
+    x = np.concatenate([a.astype(np.float64).ravel() for a in arrays]) if arrays else np.zeros(0)
+    if x.size == 0:
+        return 0.0
+    return np.abs(x).max() if kind == B.MV_NORM_MAX else np.sqrt((x * x).sum())
+
+
+def check_norm(got, want, kind):
+    if kind == B.MV_NORM_MAX:
+        assert got == np.float32(want)
+    else:
+        # fp64 sums are off by less than 1e-10 here; then one rounding, half a unit in the last place: 2^-24
+        assert abs(float(got) - want) <= want * (2.0 ** -24 + 1e-9), (got, want)
+
+
+def coef32(norm, max_norm):
+    with np.errstate(invalid="ignore", divide="ignore"):
+        c = np.float32(max_norm) / (np.float32(norm) + np.float32(1e-6))
+    return np.float32(1.0) if c >= 1.0 else c
+
+
+def to_type(x, dtype):
+    return torch.from_numpy(x).to(dtype).float().numpy()
+
+
+def make(rng, sizes, dtype, lead):
+    """Tensors of these sizes, the i-th beginning lead * i elements (modulo 8) behind a 512-byte boundary."""
+    out = []
+    for i, n in enumerate(sizes):
+        buf = torch.zeros(n + 8, dtype=dtype, device="cuda")
+        t = buf[(lead * i) % 8:(lead * i) % 8 + n]
+        t.copy_(torch.from_numpy((rng.standard_normal(n) * 10.0 ** rng.uniform(-2, 1)).astype(np.float32)))
+        out.append(t)
+    return out
+
+
+SIZES = [[1], [0, 3, 0, 7], [8, 9, 15, 16, 17], [16383, 16384, 16385, 5], [100_003, 2, 0, 32_768, 777],
+         [5] * 300, [1_000_000]]
+
+
+@pytest.mark.parametrize("kind", [B.MV_NORM_L2, B.MV_NORM_MAX])
+@pytest.mark.parametrize("src,dst", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("which", range(len(SIZES)))
+def test_packed_into_rows(which, src, dst, kind):
+    rng = np.random.default_rng(100 * which + kind)
+    sizes = SIZES[which]
+    workers = 3
+    tensors, groups, out = [], [], []
+    d = sum(sizes)
+    rows = torch.full((workers, d + 5), GUARD, dtype=TYPES[dst], device="cuda")
+    for r in range(workers):
+        tensors += make(rng, sizes, TYPES[src], lead=r)
+        groups += [r] * len(sizes)
+        out += list(rows[r, 2:2 + d].split(sizes))
+    before = [f32(t) for t in tensors]
+    per = [before[r * len(sizes):(r + 1) * len(sizes)] for r in range(workers)]
+    want = [norm64(p, kind) for p in per]
+    max_norm = sorted(want)[1] * 0.999
+    norms = torch.full((workers + 1,), GUARD, device="cuda")
+    coefs = torch.full((workers + 1,), GUARD, device="cuda")
+    clip = B.mv_clip_begin(tensors, out=out, groups=groups, norm=kind)
+    only = torch.zeros(workers, device="cuda")
+    B.mv_clip_norms(clip, only)
+    B.mv_clip_grads(clip, max_norm, norms, coefs)
+    torch.cuda.synchronize()
+    B.mv_clip_end(clip)
+    B.mv_clip_release(clip)
+    n, c, got = norms.cpu().numpy(), coefs.cpu().numpy(), f32(rows)
+    assert np.array_equal(only.cpu().numpy(), n[:workers])
+    assert n[workers] == GUARD and c[workers] == GUARD
+    assert (got[:, :2] == f32(torch.full((1,), GUARD, dtype=TYPES[dst]))).all() and (got[:, 2 + d:] == got[0, 0]).all()
+    for r in range(workers):
+        check_norm(n[r], want[r], kind)
+        assert c[r] == coef32(n[r], max_norm)
+        flat = np.concatenate(per[r])
+        assert np.array_equal(got[r, 2:2 + d], to_type(flat * c[r], TYPES[dst]))
+    for t, b in zip(tensors, before):
+        assert np.array_equal(f32(t), b)
+
+
+@pytest.mark.parametrize("src", ["f32", "bf16"])
+@pytest.mark.parametrize("clipped", [True, False])
+def test_in_place(src, clipped):
+    rng = np.random.default_rng(7)
+    tensors = make(rng, [40_000, 3, 1, 16_384], TYPES[src], lead=1)
+    before = [f32(t) for t in tensors]
+    norm = norm64(before, B.MV_NORM_L2)
+    max_norm = norm * (0.25 if clipped else 1.01)
+    norms, coefs = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    clip = B.mv_clip_begin(tensors, out=tensors)
+    B.mv_clip_grads(clip, max_norm, norms, coefs)
+    torch.cuda.synchronize()
+    c = coefs.cpu().numpy()[0]
+    assert c == coef32(norms.cpu().numpy()[0], max_norm) and (c < 1.0) == clipped
+    for t, b in zip(tensors, before):
+        assert np.array_equal(f32(t), to_type(b * c, TYPES[src]))
+    B.mv_clip_end(clip)
+    B.mv_clip_release(clip)
+
+
+def test_types_mixed_and_groups_in_any_order():
+    rng = np.random.default_rng(3)
+    a, b = make(rng, [20_000, 50, 7], torch.float32, 1), make(rng, [3, 30_000, 11], torch.bfloat16, 3)
+    tensors = [a[0], b[0], a[1], b[1], b[2], a[2]]
+    groups = [2, 0, 0, 2, 3, 2]
+    out = [torch.empty_like(t, dtype=torch.float32) for t in tensors]
+    norms, coefs = torch.zeros(5, device="cuda"), torch.zeros(5, device="cuda")
+    clip = B.mv_clip_begin(tensors, out=out, groups=groups, n_groups=5)
+    B.mv_clip_grads(clip, 1.5, norms, coefs)
+    torch.cuda.synchronize()
+    n, c = norms.cpu().numpy(), coefs.cpu().numpy()
+    for g in range(5):
+        mine = [f32(t) for t, k in zip(tensors, groups) if k == g]
+        check_norm(n[g], norm64(mine, B.MV_NORM_L2), B.MV_NORM_L2)
+        assert c[g] == coef32(n[g], 1.5)             # groups 1 and 4 have no tensor: norm 0, factor 1
+    for t, o, g in zip(tensors, out, groups):
+        assert np.array_equal(f32(o), f32(t) * c[g])
+    B.mv_clip_end(clip)
+    B.mv_clip_release(clip)
+
+
+def test_values_at_the_ends_of_the_range():
+    """Squares of 1e30 and of denormals leave fp32, not fp64."""
+    for scale in (1e30, 1e-40, 3e-45):
+        x = torch.full((1000,), scale, device="cuda")
+        norms = torch.zeros(1, device="cuda")
+        clip = B.mv_clip_begin([x])
+        B.mv_clip_norms(clip, norms)
+        want = float(np.float32(scale)) * np.sqrt(1000.0)
+        got = float(norms.cpu().numpy()[0])
+        assert abs(got - want) <= max(want * 2.0 ** -23, 1.5e-45)
+        B.mv_clip_end(clip)
+        B.mv_clip_release(clip)
+
+
+@pytest.mark.parametrize("kind", [B.MV_NORM_L2, B.MV_NORM_MAX])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+def test_nan_and_infinity_stay_in_their_group(kind, bad):
+    x = torch.ones(50_000, device="cuda")
+    y = torch.ones(50_000, device="cuda")
+    x[40_001] = bad
+    out = [torch.full_like(x, 9.0), torch.full_like(y, 9.0)]
+    norms, coefs = torch.zeros(2, device="cuda"), torch.zeros(2, device="cuda")
+    clip = B.mv_clip_begin([x, y], out=out, groups=[0, 1], norm=kind)
+    B.mv_clip_grads(clip, 0.5, norms, coefs)
+    torch.cuda.synchronize()
+    n, c, o = norms.cpu().numpy(), coefs.cpu().numpy(), f32(out[0])
+    if np.isnan(bad):
+        assert np.isnan(n[0]) and np.isnan(c[0]) and np.isnan(o).all()
+    else:
+        assert np.isposinf(n[0]) and c[0] == 0.0 and np.isnan(o[40_001])
+        assert (np.delete(o, 40_001) == 0.0).all()
+    assert np.isfinite(n[1]) and (f32(out[1]) == c[1]).all()
+    B.mv_clip_end(clip)
+    B.mv_clip_release(clip)
+
+
+def test_max_norm_zero_and_tensors_that_are_zero():
+    x, y = torch.ones(100, device="cuda"), torch.zeros(100, device="cuda")
+    norms, coefs = torch.zeros(2, device="cuda"), torch.zeros(2, device="cuda")
+    out = [torch.full_like(x, 3.0), torch.full_like(x, 3.0)]
+    clip = B.mv_clip_begin([x, y], out=out, groups=[0, 1])
+    B.mv_clip_grads(clip, 0.0, norms, coefs)
+    assert (f32(out[0]) == 0).all() and (f32(out[1]) == 0).all()
+    assert norms.cpu().tolist() == [10.0, 0.0] and coefs.cpu().tolist() == [0.0, 0.0]
+    B.mv_clip_end(clip)
+    B.mv_clip_release(clip)
+
+
+def test_strided_and_permuted_tensors():
+    rng = np.random.default_rng(11)
+    wide = torch.from_numpy(rng.standard_normal((6, 50)).astype(np.float32)).cuda()
+    part = wide[:, 10:31]                                             # rows of 21 at a stride of 50
+    conv = torch.from_numpy(rng.standard_normal((4, 3, 5, 5)).astype(np.float32)).cuda().contiguous(
+        memory_format=torch.channels_last)                            # dense, in another order
+    out = [torch.zeros((6, 21), device="cuda"), torch.zeros_like(conv)]
+    assert out[1].stride() == conv.stride()
+    norms, coefs = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    keep = f32(wide)
+    clip = B.mv_clip_begin([part, conv], out=out)
+    B.mv_clip_grads(clip, 2.0, norms, coefs)
+    c = coefs.cpu().numpy()[0]
+    check_norm(norms.cpu().numpy()[0], norm64([f32(part), f32(conv)], B.MV_NORM_L2), B.MV_NORM_L2)
+    assert np.array_equal(f32(out[0]), keep[:, 10:31] * c) and np.array_equal(f32(out[1]), f32(conv) * c)
+    B.mv_clip_end(clip)
+    B.mv_clip_release(clip)
+    with pytest.raises(ValueError):
+        B.mv_clip_begin([wide[:, ::2]])                               # no rows to take apart into
+    with pytest.raises(ValueError):
+        B.mv_clip_begin([part], out=[torch.zeros((6, 22), device="cuda")])
+    with pytest.raises(ValueError):
+        B.mv_clip_begin([part.half()])
+    with pytest.raises(ValueError):
+        B.mv_clip_begin([part, wide.cpu()])
+
+
+def test_bind_gives_other_tensors():
+    rng = np.random.default_rng(5)
+    sizes = [10, 0, 20_000] + [3] * 300                               # more than one launch's addresses
+    first, second = make(rng, sizes, torch.float32, 1), make(rng, sizes, torch.float32, 3)
+    out1, out2 = [torch.zeros_like(t) for t in first], [torch.zeros_like(t) for t in first]
+    norms = torch.zeros(1, device="cuda")
+    clip = B.mv_clip_begin(first, out=out1)
+    B.mv_clip_grads(clip, 1.0, norms)
+    n1 = norms.clone()
+    B.mv_clip_bind(clip, second, out2)
+    B.mv_clip_grads(clip, 1.0, norms)
+    for ts, os, n in ((first, out1, n1), (second, out2, norms)):
+        n = n.cpu().numpy()[0]
+        check_norm(n, norm64([f32(t) for t in ts], B.MV_NORM_L2), B.MV_NORM_L2)
+        for t, o in zip(ts, os):
+            assert np.array_equal(f32(o), f32(t) * coef32(n, 1.0))
+    with pytest.raises(ValueError):
+        B.mv_clip_bind(clip, second[1:], out2[1:])
+    with pytest.raises(ValueError):
+        B.mv_clip_bind(clip, second, [o.bfloat16() for o in out2])
+    with pytest.raises(ValueError):
+        B.mv_clip_bind(clip, second)
+    B.mv_clip_end(clip)
+    B.mv_clip_release(clip)
+
+
+def test_states_of_a_handle():
+    x, norms = torch.ones(10, device="cuda"), torch.zeros(1, device="cuda")
+    clip = B.mv_clip_begin([x])
+    with pytest.raises(B.MvError) as e:
+        B.mv_clip_grads(clip, 1.0, norms)                             # nowhere to write to
+    assert e.value.status == B.MV_ERR_STATE
+    B.mv_clip_norms(clip, norms)
+    for bad in (float("nan"), float("inf"), -1.0):
+        with pytest.raises(B.MvError) as e:
+            B.mv_clip_grads(clip, bad, norms)
+        assert e.value.status == B.MV_ERR_INVALID_ARG
+    with pytest.raises(ValueError):
+        B.mv_clip_norms(clip, norms.double())
+    B.mv_clip_end(clip)
+    for call in (lambda: B.mv_clip_norms(clip, norms), lambda: B.mv_clip_end(clip), lambda: B.mv_clip_bind(clip, [x])):
+        with pytest.raises(B.MvError) as e:
+            call()
+        assert e.value.status == B.MV_ERR_STATE
+    B.mv_clip_release(clip)
+
+
+def test_own_workspace():
+    x = [torch.ones(30_000, device="cuda"), torch.ones(5, device="cuda")]
+    norms = torch.zeros(1, device="cuda")
+    room = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    base = (room.data_ptr() + 255) // 256 * 256
+    clip = B.mv_clip_begin(x, workspace=base, workspace_bytes=(1 << 16) - 256)
+    B.mv_clip_norms(clip, norms)
+    check_norm(norms.cpu().numpy()[0], np.sqrt(30_005.0), B.MV_NORM_L2)
+    B.mv_clip_end(clip)
+    B.mv_clip_release(clip)
+    for ws, size in ((base, 16), (base + 16, 1 << 15)):
+        with pytest.raises(B.MvError) as e:
+            B.mv_clip_begin(x, workspace=ws, workspace_bytes=size)
+        assert e.value.status == B.MV_ERR_INVALID_ARG
+
+
+def test_other_stream_and_equal_results_each_time():
+    rng = np.random.default_rng(9)
+    tensors = make(rng, [300_000, 17, 70_001], torch.float32, 1)
+    out = [torch.zeros_like(t) for t in tensors]
+    norms = torch.zeros(1, device="cuda")
+    clip = B.mv_clip_begin(tensors, out=out)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    got = []
+    for i in range(4):
+        with torch.cuda.stream(s if i % 2 else torch.cuda.current_stream()):
+            B.mv_clip_grads(clip, 3.0, norms, stream=s if i == 3 else None)
+        torch.cuda.synchronize()
+        got.append((norms.cpu().numpy().view(np.uint32)[0], [f32(o) for o in out]))
+    for n, o in got[1:]:
+        assert n == got[0][0] and all(np.array_equal(a, b) for a, b in zip(o, got[0][1]))
+    B.mv_clip_end(clip)
+    B.mv_clip_release(clip)
+
+
+def test_captured_in_a_graph():
+    rng = np.random.default_rng(13)
+    tensors = make(rng, [200_000, 33], torch.float32, 1)
+    out = [torch.zeros_like(t) for t in tensors]
+    norms = torch.zeros(1, device="cuda")
+    clip = B.mv_clip_begin(tensors, out=out)
+    B.mv_clip_grads(clip, 1.0, norms)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.mv_clip_grads(clip, 1.0, norms)
+    for i in range(3):
+        for t in tensors:
+            t.mul_(1.5)
+        norms.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        n = norms.cpu().numpy()[0]
+        check_norm(n, norm64([f32(t) for t in tensors], B.MV_NORM_L2), B.MV_NORM_L2)
+        for t, o in zip(tensors, out):
+            assert np.array_equal(f32(o), f32(t) * coef32(n, 1.0))
+        B.mv_clip_grads(clip, 2.0, norms)                             # eager work between the replays
+    B.mv_clip_end(clip)
+    B.mv_clip_release(clip)
+
+
+def test_an_element_behind_32_bits():
+    """A tensor of 2^31 + 70 bf16 values: offsets beyond 2^31 elements and 2^32 bytes."""
+    n = (1 << 31) + 70
+    x = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty(n + 3, dtype=torch.bfloat16, device="cuda")[3:]
+    x[5], x[n - 2], x[1 << 31] = 3.0, 4.0, 12.0
+    norms = torch.zeros(1, device="cuda")
+    clip = B.mv_clip_begin([x], out=[out])
+    B.mv_clip_grads(clip, 13.0 / 2, norms)
+    torch.cuda.synchronize()
+    assert norms.cpu().tolist() == [13.0]
+    c = coef32(13.0, 6.5)
+    for at, v in ((5, 3.0), (n - 2, 4.0), (1 << 31, 12.0), (n - 1, 0.0), (0, 0.0)):
+        assert float(out[at]) == float(torch.tensor(np.float32(v) * c).bfloat16())
+    assert int((out != 0).sum()) == 3
+    B.mv_clip_end(clip)
+    B.mv_clip_release(clip)
