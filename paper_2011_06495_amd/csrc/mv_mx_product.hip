@@ -8,6 +8,8 @@
 // consecutive bytes of codes for four instructions, and their four scales in one word.
 #include "mv_mx.hpp"
 
+#include <type_traits>
+
 namespace mvx {
 
 typedef int   i32x8 __attribute__((ext_vector_type(8)));
@@ -44,6 +46,30 @@ __device__ __forceinline__ void load_four(const Factor& f, int64_t row, int64_t 
         w = (w & keep) | (0x7F7F7F7Fu & ~keep);
     }
     v.scales = w;
+}
+
+// Four consecutive results of a row of which `live` are left.
+typedef uint16_t u16x4u __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ void store4(float* p, int64_t live, const f32x4& v)
+{
+    if (live >= 4) {
+        *reinterpret_cast<f32x4u*>(p) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < live) p[e] = v[e];
+    }
+}
+__device__ __forceinline__ void store4(uint16_t* p, int64_t live, const f32x4& v)
+{
+    const u16x4u w = {(uint16_t)narrow(v.x), (uint16_t)narrow(v.y), (uint16_t)narrow(v.z), (uint16_t)narrow(v.w)};
+    if (live >= 4) {
+        *reinterpret_cast<u16x4u*>(p) = w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < live) p[e] = w[e];
+    }
 }
 
 constexpr int kTile = 64;           // rows of each factor that a wavefront takes
@@ -83,28 +109,317 @@ __global__ __launch_bounds__(kProductThreads) void mv_mx_product_kernel(Factor a
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int64_t j = j0 + 16 * u + 4 * group;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (j + e < b.rows) {
-                    if constexpr (sizeof(T) == 2) c[i * ld_c + j + e] = (T)narrow(acc[t][u][e]);
-                    else c[i * ld_c + j + e] = acc[t][u][e];
-                }
+            store4(c + i * ld_c + j, b.rows - j, acc[t][u]);
         }
     }
 }
 
-static mv_status launch_product(const Factor& a, const Factor& b, int64_t k, void* c, int32_t c_dtype, int64_t ld_c, hipStream_t st)
+// ---- tiles through LDS ---------------------------------------------------------------------------------------------
+//
+// A workgroup of WM x WN wavefronts takes 32 MT WM x 32 NT WN results, 32 MT x 32 NT a wavefront, in steps of eight blocks (256 values,
+// 128 bytes a row).  The rows of both factors go from memory straight into LDS, each row's 16-byte blocks in the order
+// block ^ (row % 8): what eight lanes of neighbouring rows read together lies in different banks, and what eight lanes
+// write together is one whole line of memory.  Two buffers: the next step's loads are in flight during this one's
+// products.  Loads beyond the last row or block return zeros by the buffer's bounds.  The scales of two steps, 16 bytes a row,
+// go through registers, where those behind the last block become 1, into LDS of their own.
+//
+// A lane of the 32 x 32 x 64 instruction holds half of a row's eight blocks: blocks 4 (lane / 32) + s of step s, whose
+// scales are one word.
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kStepBlocks = 8;
+constexpr int kScalePitch = 20;     // bytes between the rows' scales in LDS: 16 and a word against bank conflicts
+
+constexpr int kNoLoads = 0x0F70;    // s_waitcnt: none of the vector loads in flight, the other counters as they are
+
+template <int S>
+__device__ __forceinline__ f32x16 mfma32(const u32x4& a, uint32_t a_scale, const u32x4& b, uint32_t b_scale, f32x16 c)
 {
-    const int64_t tiles_m = (a.rows + 2 * kTile - 1) / (2 * kTile), tiles_n = (b.rows + 2 * kTile - 1) / (2 * kTile);
-    if (tiles_m * tiles_n > kMostGroups) return MV_ERR_INVALID_ARG;
-    const dim3 grid((uint32_t)(tiles_m * tiles_n)), threads(kProductThreads);
-    if (c_dtype == MV_BF16)
-        hipLaunchKernelGGL(mv_mx_product_kernel<uint16_t>, grid, threads, 0, st, a, b, blocks_of(k), tiles_n,
-                           static_cast<uint16_t*>(c), ld_c);
-    else
-        hipLaunchKernelGGL(mv_mx_product_kernel<float>, grid, threads, 0, st, a, b, blocks_of(k), tiles_n, static_cast<float*>(c),
-                           ld_c);
+    const i32x8 x = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, y = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, S, (int)a_scale, S, (int)b_scale);
+}
+
+// Which tile a workgroup takes: consecutive workgroups run on eight dies with an L2 of their own, so a die gets a run of
+// consecutive tiles, and those go down eight tiles of a before they go along b.
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn)
+{
+    const uint32_t all = tiles_m * tiles_n, each = all / 8, more = all % 8, die = id % 8;
+    const uint32_t t = die * each + min(die, more) + id / 8;
+    const uint32_t band = t / (8 * tiles_n), first = band * 8, high = min(8u, tiles_m - first), in = t - first * tiles_n;
+    tm = first + in % high;
+    tn = in / high;
+}
+
+// A wavefront's share of one instruction's blocks: rows of a and of b.
+template <int MT, int NT>
+struct Rows {
+    u32x4 x[MT], y[NT];
+};
+
+template <int MT, int NT, int WM, int WN, typename T>
+__global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Factor a, Factor b, uint32_t blocks, uint32_t tiles_m,
+                                                                             uint32_t tiles_n, uint32_t steps_each,
+                                                                             T* __restrict__ c, int64_t ld_c, int64_t split_c)
+{
+    constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+    constexpr int kM = 32 * MT * WM, kN = 32 * NT * WN, kRows = kM + kN;
+    typedef uint8_t Codes[kRows * 128];
+    // two variables, not an array of two: reads of one need not wait for the loads into the other
+    __shared__ __attribute__((aligned(1024))) Codes even, odd;
+    __shared__ uint8_t scales[2][kRows * kScalePitch];
+    const uint32_t t = threadIdx.x, lane = t & 63u, wave = __builtin_amdgcn_readfirstlane(t / 64);
+    uint32_t tm, tn;
+    tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
+    const int64_t i0 = (int64_t)tm * kM, j0 = (int64_t)tn * kN;
+    const uint32_t steps = (blocks + kStepBlocks - 1) / kStepBlocks;
+    const uint32_t step0 = blockIdx.y * steps_each, count = min(steps_each, steps - step0);       // at least one
+    const uint32_t end = min(blocks, (step0 + count) * kStepBlocks);       // an odd count's last step is one of zeros
+
+    // what this wavefront loads: rows [wave kM / kWaves, ...) of a and as many of b, eight rows an instruction
+    const uint32_t a_pitch = (uint32_t)a.ld_words * 4u, b_pitch = (uint32_t)b.ld_words * 4u;
+    const int64_t a_rows = a.rows - i0 < kM ? a.rows - i0 : kM, b_rows = b.rows - j0 < kN ? b.rows - j0 : kN;
+    const __amdgpu_buffer_rsrc_t a_buf = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint32_t*>(a.codes + i0 * a.ld_words), 0, (int)((uint32_t)(a_rows - 1) * a_pitch + blocks * 16u), 0x00020000);
+    const __amdgpu_buffer_rsrc_t b_buf = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint32_t*>(b.codes + j0 * b.ld_words), 0, (int)((uint32_t)(b_rows - 1) * b_pitch + blocks * 16u), 0x00020000);
+    const uint32_t my_block = (lane & 7u) ^ (lane >> 3);
+    const uint32_t a_at = (wave * (kM / kWaves) + (lane >> 3)) * a_pitch + my_block * 16u;
+    const uint32_t b_at = (wave * (kN / kWaves) + (lane >> 3)) * b_pitch + my_block * 16u;
+    auto load_codes = [&](uint32_t k, Codes& to) {
+        const uint32_t step = step0 + k;
+        // The whole offset is the lane's own, for the bounds to hold: below 2^30 + 2^21, and beyond every buffer where the
+        // row has no such block.
+        const bool live = step * kStepBlocks + my_block < end;
+        const uint32_t av = live ? a_at + step * 128u : 0x80000000u, bv = live ? b_at + step * 128u : 0x80000000u;
+#pragma unroll
+        for (int i = 0; i < kM / kWaves / 8; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                a_buf, (__attribute__((address_space(3))) void*)(to + (wave * (kM / kWaves) + i * 8) * 128), 16,
+                av + i * 8 * a_pitch, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kN / kWaves / 8; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                b_buf, (__attribute__((address_space(3))) void*)(to + (kM + wave * (kN / kWaves) + i * 8) * 128), 16,
+                bv + i * 8 * b_pitch, 0, 0, 0);
+    };
+    // the scales' rows
+    constexpr int kScaleRows = (kRows + kThreads - 1) / kThreads;
+    const uint8_t* scale_row[kScaleRows];
+#pragma unroll
+    for (int i = 0; i < kScaleRows; ++i) {
+        const uint32_t r = t + kThreads * i;
+        const int64_t at = r < kM ? i0 + r : j0 + (r - kM);
+        scale_row[i] = r < kM ? a.scales + (at < a.rows ? at : a.rows - 1) * a.ld_scales
+                              : b.scales + (at < b.rows ? at : b.rows - 1) * b.ld_scales;
+    }
+    const uint32_t last_word = (end - 1) / 4 * 4;
+    uint32_t next[kScaleRows][4];
+    auto fetch_scales = [&](uint32_t k) {
+#pragma unroll
+        for (int i = 0; i < kScaleRows; ++i)
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+                next[i][w] = *reinterpret_cast<const uint32_t*>(scale_row[i] + min((step0 + k) * kStepBlocks + 4 * w, last_word));
+    };
+    auto keep_scales = [&](uint32_t pair) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int live = (int)end - (int)((step0 + 2 * pair) * kStepBlocks + 4 * w);
+            const uint32_t real = live >= 4 ? 0xFFFFFFFFu : live > 0 ? (1u << (8 * live)) - 1u : 0u;
+#pragma unroll
+            for (int i = 0; i < kScaleRows; ++i)
+                if (kRows % kThreads == 0 || t + kThreads * i < kRows)
+                    *reinterpret_cast<uint32_t*>(&scales[pair & 1u][(t + kThreads * i) * kScalePitch + 4 * w]) =
+                        (next[i][w] & real) | (0x7F7F7F7Fu & ~real);
+        }
+    };
+
+    const uint32_t in = lane & 31u, half = lane >> 5;
+    const uint32_t a_row = wave / WN * (32 * MT) + in, b_row = kM + wave % WN * (32 * NT) + in;
+    f32x16 acc[MT][NT] = {};
+    Rows<MT, NT> one, two;
+    uint32_t as[MT], bs[NT], as_next[MT], bs_next[NT];
+    auto read_rows = [&](const Codes& from, uint32_t s, Rows<MT, NT>& r) {
+        const uint32_t slot = ((4 * half + s) ^ (lane & 7u)) * 16;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) r.x[i] = *reinterpret_cast<const u32x4*>(from + (a_row + 32 * i) * 128 + slot);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) r.y[i] = *reinterpret_cast<const u32x4*>(from + (b_row + 32 * i) * 128 + slot);
+    };
+    auto read_scales = [&](uint32_t k) {
+        const uint8_t* sc = scales[k >> 1 & 1u] + (k & 1u) * 8 + half * 4;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) as_next[i] = *reinterpret_cast<const uint32_t*>(sc + (a_row + 32 * i) * kScalePitch);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) bs_next[i] = *reinterpret_cast<const uint32_t*>(sc + (b_row + 32 * i) * kScalePitch);
+    };
+    auto products = [&](auto s, const Rows<MT, NT>& r) {
+        constexpr int S = decltype(s)::value;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = mfma32<S>(r.y[j], bs[j], r.x[i], as[i], acc[i][j]);
+    };
+    // The first three quarters of a step whose first rows are in `one` and its scales in the next ones already.
+    auto most_of_step = [&](const Codes& now) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) as[i] = as_next[i];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) bs[i] = bs_next[i];
+        read_rows(now, 1, two);
+        __builtin_amdgcn_sched_barrier(0);
+        products(std::integral_constant<int, 0>{}, one);
+        __builtin_amdgcn_sched_barrier(0);
+        read_rows(now, 2, one);
+        __builtin_amdgcn_sched_barrier(0);
+        products(std::integral_constant<int, 1>{}, two);
+        __builtin_amdgcn_sched_barrier(0);
+        read_rows(now, 3, two);
+        __builtin_amdgcn_sched_barrier(0);
+        products(std::integral_constant<int, 2>{}, one);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto all_here = [&] {
+        __builtin_amdgcn_s_waitcnt(kNoLoads);
+        __syncthreads();
+    };
+    auto last_of_step = [&] {
+        __builtin_amdgcn_sched_barrier(0);
+        products(std::integral_constant<int, 3>{}, two);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    load_codes(0, even);
+    fetch_scales(0);
+    keep_scales(0);
+    all_here();
+    load_codes(1, odd);
+    read_rows(even, 0, one);
+    read_scales(0);
+    // Two steps a turn.  Before a step's last products come the next one's first rows, so those products cover the way
+    // from LDS, and the loads into this step's buffer begin as soon as all wavefronts have read it.  The turn has no
+    // branches, or the compiler moves products past them and runs out of registers: behind the last step zeros are loaded.
+    for (uint32_t k = 0; k < count; k += 2) {
+        most_of_step(even);
+        all_here();
+        read_rows(odd, 0, one);
+        read_scales(k + 1);
+        fetch_scales(k + 2);
+        load_codes(k + 2, even);
+        last_of_step();
+        most_of_step(odd);
+        keep_scales(k / 2 + 1);
+        all_here();
+        read_rows(even, 0, one);
+        read_scales(k + 2);
+        load_codes(k + 3, odd);
+        last_of_step();
+    }
+    __builtin_amdgcn_s_waitcnt(kNoLoads);
+
+    // a lane has, of row i, four times four consecutive columns
+    T* out = c + blockIdx.y * split_c;
+    const int64_t col0 = j0 + wave % WN * (32 * NT) + 4 * half;
+    const bool whole = j0 + kN <= b.rows;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t row = i0 + a_row + 32 * i;
+        if (row >= a.rows) continue;
+        T* to = out + row * ld_c + col0;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                if (whole) store4(to + 32 * j + 8 * q, 4, v);
+                else store4(to + 32 * j + 8 * q, b.rows - (col0 + 32 * j + 8 * q), v);
+            }
+    }
+}
+
+// c = the sum of the splits, in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void mv_mx_product_join_kernel(const float* __restrict__ parts, int splits, int64_t m, int64_t n,
+                                                                 int64_t split_c, int64_t quads, T* __restrict__ c, int64_t ld_c)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t i = at / quads, j = at % quads * 4;
+    if (i >= m) return;
+    const float* p = parts + i * (quads * 4) + j;
+    f32x4 sum = *reinterpret_cast<const f32x4*>(p);
+    for (int s = 1; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(p + s * split_c);
+    store4(c + i * ld_c + j, n - j, sum);
+}
+
+// How a product is cut: tiles of 64 `mt` rows of each factor (0: the kernel without LDS), and the steps of k over `splits`.
+struct Cut {
+    int      mt;
+    int64_t  tiles_m, tiles_n;
+    uint32_t splits, steps_each;
+};
+static Cut cut_of(int64_t m, int64_t n, int64_t k)
+{
+    auto tiles = [](int64_t rows, int mt) { return (rows + 64 * mt - 1) / (64 * mt); };
+    Cut c = {4, tiles(m, 4), tiles(n, 4), 1, 0};
+    const int64_t steps = (blocks_of(k) + kStepBlocks - 1) / kStepBlocks;
+    if (c.tiles_m * c.tiles_n < 192) {
+        c = {2, tiles(m, 2), tiles(n, 2), 1, 0};
+        const int64_t most = 512 / (c.tiles_m * c.tiles_n);
+        int64_t splits = most < steps / 4 ? most : steps / 4;
+        if (splits > 16) splits = 16;
+        if (splits > 1) c.splits = (uint32_t)splits;
+    }
+    c.steps_each = (uint32_t)((steps + c.splits - 1) / c.splits);
+    c.splits = (uint32_t)((steps + c.steps_each - 1) / c.steps_each);
+    return c;
+}
+inline int64_t quads_of(int64_t n) { return (n + 3) / 4; }
+inline size_t parts_bytes(int64_t m, int64_t n, int64_t k)
+{
+    const Cut c = cut_of(m, n, k);
+    return c.splits > 1 ? (size_t)c.splits * (size_t)m * (size_t)quads_of(n) * 16 : 0;
+}
+
+template <typename T>
+static mv_status launch_product_of(const Factor& a, const Factor& b, int64_t k, T* c, int64_t ld_c, float* parts, hipStream_t st)
+{
+    const Cut cut = cut_of(a.rows, b.rows, k);
+    const dim3 threads(256);
+    if (cut.tiles_m * cut.tiles_n * cut.splits > kMostGroups) return MV_ERR_INVALID_ARG;
+    const dim3 grid((uint32_t)(cut.tiles_m * cut.tiles_n), cut.splits);
+    const uint32_t blocks = (uint32_t)blocks_of(k), tm = (uint32_t)cut.tiles_m, tn = (uint32_t)cut.tiles_n;
+    if (cut.mt == 4) {
+        hipLaunchKernelGGL((mv_mx_product_tile_kernel<4, 2, 2, 4, T>), grid, dim3(512), 0, st, a, b, blocks, tm, tn, cut.steps_each, c, ld_c, 0);
+    } else if (cut.splits == 1) {
+        hipLaunchKernelGGL((mv_mx_product_tile_kernel<2, 2, 2, 2, T>), grid, threads, 0, st, a, b, blocks, tm, tn, cut.steps_each, c, ld_c, 0);
+    } else {
+        const int64_t quads = quads_of(b.rows), split_c = a.rows * quads * 4;
+        hipLaunchKernelGGL((mv_mx_product_tile_kernel<2, 2, 2, 2, float>), grid, threads, 0, st, a, b, blocks, tm, tn, cut.steps_each, parts,
+                           quads * 4, split_c);
+        hipLaunchKernelGGL(mv_mx_product_join_kernel<T>, dim3((uint32_t)((a.rows * quads + 255) / 256)), threads, 0, st, parts,
+                           (int)cut.splits, a.rows, b.rows, split_c, quads, c, ld_c);
+    }
     return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
+}
+
+static mv_status launch_product(const Factor& a, const Factor& b, int64_t k, void* c, int32_t c_dtype, int64_t ld_c, void* parts,
+                                hipStream_t st)
+{
+    // byte offsets inside a tile's rows are 32 bits
+    if (a.ld_words * 4 > (1 << 22) || b.ld_words * 4 > (1 << 22)) {
+        const int64_t tiles_m = (a.rows + 2 * kTile - 1) / (2 * kTile), tiles_n = (b.rows + 2 * kTile - 1) / (2 * kTile);
+        if (tiles_m * tiles_n > kMostGroups) return MV_ERR_INVALID_ARG;
+        const dim3 grid((uint32_t)(tiles_m * tiles_n)), threads(kProductThreads);
+        if (c_dtype == MV_BF16)
+            hipLaunchKernelGGL(mv_mx_product_kernel<uint16_t>, grid, threads, 0, st, a, b, blocks_of(k), tiles_n,
+                               static_cast<uint16_t*>(c), ld_c);
+        else
+            hipLaunchKernelGGL(mv_mx_product_kernel<float>, grid, threads, 0, st, a, b, blocks_of(k), tiles_n, static_cast<float*>(c),
+                               ld_c);
+        return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
+    }
+    return c_dtype == MV_BF16 ? launch_product_of(a, b, k, static_cast<uint16_t*>(c), ld_c, static_cast<float*>(parts), st)
+                              : launch_product_of(a, b, k, static_cast<float*>(c), ld_c, static_cast<float*>(parts), st);
 }
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -137,7 +452,8 @@ extern "C" {
 
 size_t mv_mx_product_scratch_bytes(int64_t m, int64_t n, int64_t k)
 {
-    return 0;
+    using namespace mvx;
+    return size_valid(m) && size_valid(n) && size_valid(k) ? parts_bytes(m, n, k) : 0;
 }
 
 mv_status mv_mx_product(const uint32_t* a_codes, int64_t ld_aw, const uint8_t* a_scales, int64_t ld_as,
@@ -150,14 +466,14 @@ mv_status mv_mx_product(const uint32_t* a_codes, int64_t ld_aw, const uint8_t* a
         !scratch_valid(scratch, scratch_bytes, mv_mx_product_scratch_bytes(m, n, k)))
         return MV_ERR_INVALID_ARG;
     return launch_product({a_codes, a_scales, ld_aw, ld_as, m}, {b_codes, b_scales, ld_bw, ld_bs, n}, k, c, c_dtype, ld_c,
-                          static_cast<hipStream_t>(stream));
+                          scratch, static_cast<hipStream_t>(stream));
 }
 
 size_t mv_mx_linear_scratch_bytes(int64_t m, int64_t n, int64_t k)
 {
     using namespace mvx;
     if (!size_valid(m) || !size_valid(n) || !size_valid(k)) return 0;
-    return code_bytes(m, k) + scale_bytes(m, k);
+    return code_bytes(m, k) + scale_bytes(m, k) + parts_bytes(m, n, k);
 }
 
 mv_status mv_mx_linear(const void* x, int32_t x_dtype, int64_t ld_x, const uint32_t* w_codes, int64_t ld_words,
@@ -174,14 +490,16 @@ mv_status mv_mx_linear(const void* x, int32_t x_dtype, int64_t ld_x, const uint3
     const Held q = carve(at, m, k);
     if (const mv_status rc = launch_encode(x, x_dtype, ld_x, m, k, q.codes, q.ld_words, q.scales, q.ld_scales, nullptr, 0, st))
         return rc;
-    return launch_product(q.factor(), {w_codes, w_scales, ld_words, ld_scales, n}, k, y, y_dtype, ld_y, st);
+    return launch_product(q.factor(), {w_codes, w_scales, ld_words, ld_scales, n}, k, y, y_dtype, ld_y, at, st);
 }
 
 size_t mv_mx_linear_grad_scratch_bytes(int64_t m, int64_t n, int64_t k)
 {
     using namespace mvx;
     if (!size_valid(m) || !size_valid(n) || !size_valid(k)) return 0;
-    return code_bytes(m, n) + scale_bytes(m, n) + code_bytes(n, m) + scale_bytes(n, m) + code_bytes(k, m) + scale_bytes(k, m);
+    const size_t dx = code_bytes(m, n) + scale_bytes(m, n), dw = code_bytes(n, m) + scale_bytes(n, m) + code_bytes(k, m) + scale_bytes(k, m);
+    const size_t dx_parts = parts_bytes(m, k, n), dw_parts = parts_bytes(n, k, m);
+    return dx + dw + (dx_parts > dw_parts ? dx_parts : dw_parts);
 }
 
 mv_status mv_mx_linear_grad(const void* x, int64_t ld_x, const void* dy, int64_t ld_dy, int32_t dtype,
@@ -198,18 +516,20 @@ mv_status mv_mx_linear_grad(const void* x, int64_t ld_x, const void* dy, int64_t
     if (dw && (!values_valid(x, dtype, ld_x, k) || !values_valid(dw, dw_dtype, ld_dw, k))) return MV_ERR_INVALID_ARG;
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* at = static_cast<char*>(scratch);
+    // the two products' parts take one place, behind all codes
+    char* parts = at + code_bytes(m, n) + scale_bytes(m, n) + code_bytes(n, m) + scale_bytes(n, m) + code_bytes(k, m) + scale_bytes(k, m);
     if (dx) {
         const Held q = carve(at, m, n);
         if (const mv_status rc = launch_encode(dy, dtype, ld_dy, m, n, q.codes, q.ld_words, q.scales, q.ld_scales, nullptr, 0, st))
             return rc;
-        if (const mv_status rc = launch_product(q.factor(), {wt_codes, wt_scales, ld_words, ld_scales, k}, n, dx, dx_dtype, ld_dx, st))
+        if (const mv_status rc = launch_product(q.factor(), {wt_codes, wt_scales, ld_words, ld_scales, k}, n, dx, dx_dtype, ld_dx, parts, st))
             return rc;
     }
     if (dw) {
         const Held p = carve(at, n, m), q = carve(at, k, m);
         if (const mv_status rc = launch_encode_t(dy, dtype, ld_dy, m, n, p.codes, p.ld_words, p.scales, p.ld_scales, st)) return rc;
         if (const mv_status rc = launch_encode_t(x, dtype, ld_x, m, k, q.codes, q.ld_words, q.scales, q.ld_scales, st)) return rc;
-        return launch_product(p.factor(), q.factor(), m, dw, dw_dtype, ld_dw, st);
+        return launch_product(p.factor(), q.factor(), m, dw, dw_dtype, ld_dw, parts, st);
     }
     return MV_OK;
 }
