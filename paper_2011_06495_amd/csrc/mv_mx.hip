@@ -59,45 +59,65 @@ __global__ __launch_bounds__(kThreads) void mv_mx_encode_kernel(const T* vals, i
     }
 }
 
-// Columns: a wavefront takes 32 rows, a lane a column of them, so a lane has a block; the codes of kTileBlocks wavefronts
-// then go out in runs of 16 kTileBlocks bytes per column.
+// Columns: a wavefront takes 32 rows of 16 bytes of columns in each group of four lanes; lane r of a group has rows
+// 8 r .. 8 r + 8, of each column a word of codes, and the block's largest magnitude is two DPP moves away again.  The
+// codes of kTileBlocks wavefronts, one below the other, go out through LDS in runs of 16 kTileBlocks bytes a column.
 constexpr int kTileBlocks = 4;
+template <typename T>
+constexpr int kLaneCols = 16 / (int)sizeof(T);
+template <typename T>
+__device__ __forceinline__ void load_cols(const T* p, int64_t live, float (&x)[kLaneCols<T>])
+{
+    if constexpr (sizeof(T) == 2) {
+        load8(p, live, x);
+    } else if (live >= 4) {
+        const f32x4u v = *reinterpret_cast<const f32x4u*>(p);
+        x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = i < live ? p[i] : 0.0f;
+    }
+}
 template <typename T>
 __global__ __launch_bounds__(64 * kTileBlocks) void mv_mx_encode_t_kernel(const T* __restrict__ vals, int64_t ld_vals,
                                                                           int64_t rows, int64_t n, int64_t tiles,
                                                                           uint32_t* __restrict__ codes, int64_t ld_words,
                                                                           uint8_t* __restrict__ scales, int64_t ld_scales)
 {
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x / 64;
+    constexpr int kCols = kLaneCols<T>, kTileCols = 16 * kCols;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x / 64, group = lane / 4, r = lane & 3u;
     const int64_t tile = (int64_t)blockIdx.x % tiles, strip = (int64_t)blockIdx.x / tiles;   // of columns, of rows
-    const int64_t col = tile * 64 + lane, block = strip * kTileBlocks + wave;
-    __shared__ u32x4 out[64][kTileBlocks];
-    __shared__ uint8_t held[64][kTileBlocks];
-    const int64_t row0 = block * kBlock;
-    float x[4][8];
-    uint32_t top = 0;
+    const int64_t col = tile * kTileCols + group * kCols, row = (strip * kTileBlocks + wave) * kBlock + 8 * r;
+    __shared__ __attribute__((aligned(16))) uint32_t out[kTileCols][4 * kTileBlocks];
+    __shared__ uint8_t held[kTileCols][kTileBlocks];
+    float x[8][kCols];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        float v = 0.0f;
-        if (col < n && row0 + i < rows) {
-            if constexpr (sizeof(T) == 2) v = widen(vals[(row0 + i) * ld_vals + col]);
-            else v = vals[(row0 + i) * ld_vals + col];
-        }
-        x[i / 8][i % 8] = v;
-        top = max(top, __float_as_uint(v) & 0x7FFFFFFFu);
+    for (int i = 0; i < 8; ++i) {
+        const int64_t live = row + i < rows ? n - col : 0;
+        load_cols(vals + (row + i) * ld_vals + col, live, x[i]);
     }
-    const uint32_t scale = scale_of(top);
-    u32x4 w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = encode8(x[i], scale);
-    out[lane][wave] = w;
-    held[lane][wave] = (uint8_t)scale;
+    for (int j = 0; j < kCols; ++j) {
+        float y[8];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            y[i] = x[i][j];
+            top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
+        }
+        const uint32_t scale = scale_of(top_of_quad(top));
+        out[group * kCols + j][4 * wave + r] = encode8(y, scale);
+        if (r == 0) held[group * kCols + j][wave] = (uint8_t)scale;
+    }
     __syncthreads();
-    const uint32_t c = threadIdx.x / kTileBlocks, b = threadIdx.x % kTileBlocks;
-    const int64_t to = tile * 64 + c, to_block = strip * kTileBlocks + b;
-    if (to < n && to_block < blocks_of(rows)) {
-        *reinterpret_cast<u32x4*>(codes + to * ld_words + to_block * 4) = out[c][b];
-        scales[to * ld_scales + to_block] = held[c][b];
+#pragma unroll
+    for (int i = 0; i < kTileCols / 64; ++i) {
+        const uint32_t c = i * 64 + threadIdx.x / kTileBlocks, b = threadIdx.x % kTileBlocks;
+        const int64_t to = tile * kTileCols + c, to_block = strip * kTileBlocks + b;
+        if (to < n && to_block < blocks_of(rows)) {
+            *reinterpret_cast<u32x4*>(codes + to * ld_words + to_block * 4) = *reinterpret_cast<const u32x4*>(&out[c][4 * b]);
+            scales[to * ld_scales + to_block] = held[c][b];
+        }
     }
 }
 
@@ -170,7 +190,8 @@ mv_status launch_encode(const void* vals, int32_t dtype, int64_t ld_vals, int64_
 mv_status launch_encode_t(const void* vals, int32_t dtype, int64_t ld_vals, int64_t rows, int64_t n, uint32_t* codes,
                           int64_t ld_words, uint8_t* scales, int64_t ld_scales, hipStream_t st)
 {
-    const int64_t tiles = (n + 63) / 64, strips = (blocks_of(rows) + kTileBlocks - 1) / kTileBlocks;
+    const int64_t cols = dtype == MV_BF16 ? 16 * kLaneCols<uint16_t> : 16 * kLaneCols<float>;
+    const int64_t tiles = (n + cols - 1) / cols, strips = (blocks_of(rows) + kTileBlocks - 1) / kTileBlocks;
     if (tiles * strips > kMostGroups) return MV_ERR_INVALID_ARG;
     const dim3 grid((uint32_t)(tiles * strips)), threads(64 * kTileBlocks);
     if (dtype == MV_BF16)

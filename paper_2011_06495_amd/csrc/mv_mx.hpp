@@ -117,6 +117,28 @@ __device__ __forceinline__ void decode8(uint32_t w, uint32_t scale, float (&x)[8
     x[0] = a.x * p, x[1] = a.y * p, x[2] = b.x * p, x[3] = b.y * p, x[4] = c.x * p, x[5] = c.y * p, x[6] = d.x * p, x[7] = d.y * p;
 }
 
+// The same of bf16 pairs as they are.
+typedef __bf16   bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t encode8(const uint32_t (&x)[4], uint32_t scale)
+{
+    if (scale == kNanScale) return 0u;
+    const float p = power_of(scale);
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x[0]), p, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x[1]), p, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x[2]), p, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x[3]), p, 3);
+    return w;
+}
+// The larger patterns without their sign, of each half.
+__device__ __forceinline__ uint32_t top2(uint32_t t, uint32_t x)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, t), __builtin_bit_cast(u16x2, x & 0x7FFF7FFFu)));
+}
+// The larger half as an fp32 pattern.
+__device__ __forceinline__ uint32_t top_of_pair(uint32_t t) { return max(t & 0xFFFF0000u, t << 16); }
+
 // The larger of the lanes' patterns among each four consecutive lanes.
 __device__ __forceinline__ uint32_t top_of_quad(uint32_t t)
 {

@@ -72,6 +72,9 @@ __device__ __forceinline__ void store4(uint16_t* p, int64_t live, const f32x4& v
     }
 }
 
+__device__ __forceinline__ void put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put(uint16_t* p, float x) { *p = (uint16_t)narrow(x); }
+
 constexpr int kTile = 64;           // rows of each factor that a wavefront takes
 constexpr int kProductThreads = 256;
 
@@ -351,6 +354,209 @@ __global__ __launch_bounds__(256) void mv_mx_product_join_kernel(const float* __
     store4(c + i * ld_c + j, n - j, sum);
 }
 
+// ---- few rows of one factor ------------------------------------------------------------------------------------------
+//
+// Up to 16 rows of one factor ("few") against many of the other ("many"), whose codes are the bytes to read.  A workgroup
+// takes 16 NT of the many rows and all of k, its wavefronts turns of 16 blocks; what they have is added up through LDS in
+// the wavefronts' order.  Lane l of an instruction holds row l % 16 and block 4 s + l / 16 of the turn, s = 0 .. 3: the
+// four lanes of a row read 64 bytes in a row; the scales of a lane's four blocks are picked from the row's 16.
+// The few rows' codes and scales are in LDS: copied there, or quantised by every workgroup for itself, a lane a block,
+// while the first turn's codes are on their way.
+
+constexpr int kTurn = 16;           // blocks
+constexpr int kFewWaves = 8;
+template <typename X>
+struct Few {                        // X: uint32_t: codes; uint16_t or float: bf16 or fp32 values
+    const X*       rows;
+    int64_t        ld;
+    const uint8_t* scales;          // of codes
+    int64_t        ld_scales;
+    uint32_t       count;
+};
+
+// Byte g of each of a turn's four words of scales: those of blocks 4 s + g.
+__device__ __forceinline__ uint32_t pick_scales(const u32x4& w, uint32_t g)
+{
+    const uint32_t two = (g | (4u + g) << 8) | 0x0C0C0000u;              // byte g of the second and of the first argument
+    return __builtin_amdgcn_perm(w.y, w.x, two) | __builtin_amdgcn_perm(w.w, w.z, two) << 16;
+}
+
+// A block of the few rows on its way: fetched, and then made codes and scale of.
+template <typename X>
+struct Block;
+template <>
+struct Block<uint32_t> {
+    u32x4    w;
+    uint32_t scale;
+    __device__ __forceinline__ void fetch(const Few<uint32_t>& f, uint32_t row, uint32_t block, int64_t)
+    {
+        w = *reinterpret_cast<const u32x4*>(f.rows + row * f.ld + 4 * (int64_t)block);
+        scale = f.scales[row * f.ld_scales + block];
+    }
+    __device__ __forceinline__ void finish(u32x4& codes, uint32_t& s) const { codes = w, s = scale; }
+};
+template <>
+struct Block<float> {
+    float x[4][8];
+    __device__ __forceinline__ void fetch(const Few<float>& f, uint32_t row, uint32_t block, int64_t k)
+    {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) load8(f.rows + row * f.ld + (int64_t)block * kBlock + 8 * q, k - (int64_t)block * kBlock - 8 * q, x[q]);
+    }
+    __device__ __forceinline__ void finish(u32x4& codes, uint32_t& s) const
+    {
+        uint32_t top = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[q][i]) & 0x7FFFFFFFu);
+        s = scale_of(top);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) codes[q] = encode8(x[q], s);
+    }
+};
+template <>
+struct Block<uint16_t> {
+    uint32_t x[4][4];
+    __device__ __forceinline__ void fetch(const Few<uint16_t>& f, uint32_t row, uint32_t block, int64_t k)
+    {
+        const uint16_t* p = f.rows + row * f.ld + (int64_t)block * kBlock;
+        const int64_t live = k - (int64_t)block * kBlock;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (live >= kBlock) {
+                const u32x4u v = *reinterpret_cast<const u32x4u*>(p + 8 * q);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[q][i] = v[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = 8 * q + 2 * i;
+                    x[q][i] = (at < live ? p[at] : 0u) | (at + 1 < live ? (uint32_t)p[at + 1] << 16 : 0u);
+                }
+            }
+    }
+    __device__ __forceinline__ void finish(u32x4& codes, uint32_t& s) const
+    {
+        uint32_t top = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = top2(top, x[q][i]);
+        s = scale_of(top_of_pair(top));
+#pragma unroll
+        for (int q = 0; q < 4; ++q) codes[q] = encode8(x[q], s);
+    }
+};
+
+// LDS of the few rows: `count` rows of `turns` x 16 blocks, rows 16 bytes longer against bank conflicts, then one byte
+// of scale each, the four of a lane and turn in one word.
+__host__ __device__ constexpr uint32_t few_pitch(uint32_t turns) { return turns * (kTurn * 16) + 16; }
+// Behind them the many rows' scales, rows 16 bytes longer too.
+__host__ __device__ constexpr uint32_t many_pitch(uint32_t turns) { return turns * kTurn + 16; }
+__host__ __device__ constexpr uint32_t few_bytes(uint32_t count, uint32_t turns, uint32_t many)
+{
+    return count * (few_pitch(turns) + turns * kTurn) + many * many_pitch(turns);
+}
+
+// c[many][few] or c[few][many]: element (j, i) lies at j * step_many + i * step_few.
+template <int NT, typename X, typename T>
+__global__ __launch_bounds__(64 * kFewWaves) void mv_mx_product_few_kernel(Factor many, Few<X> few, uint32_t blocks, int64_t k,
+                                                                           T* __restrict__ c, int64_t step_many, int64_t step_few)
+{
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
+    const uint32_t in = lane & 15u, g = lane / 16;
+    const int64_t j0 = (int64_t)blockIdx.x * (16 * NT);
+    extern __shared__ __attribute__((aligned(16))) uint8_t held[];
+    const uint32_t turns = (blocks + kTurn - 1) / kTurn, row_blocks = turns * kTurn, pitch = few_pitch(turns);
+    uint8_t* held_scales = held + few.count * pitch;
+    uint8_t* many_scales = held_scales + few.count * row_blocks;
+
+    // Loads come back in their order, so what LDS gets is asked for first: the thread's first block of the few rows ...
+    Block<X> mine;
+    const uint32_t few_blocks = few.count * row_blocks;
+    auto fetch = [&](uint32_t at) {
+        const uint32_t row = at / row_blocks, block = at - row * row_blocks;
+        if (at < few_blocks && block < blocks) mine.fetch(few, row, block, k);
+    };
+    auto hold = [&](uint32_t at) {
+        const uint32_t row = at / row_blocks, block = at - row * row_blocks;
+        u32x4 codes = {0u, 0u, 0u, 0u};
+        uint32_t scale = 127;
+        if (block < blocks) mine.finish(codes, scale);
+        *reinterpret_cast<u32x4*>(held + row * pitch + block * 16) = codes;
+        // block 4 s + g of a turn is byte s of word g
+        held_scales[row * row_blocks + (block & ~15u) + (block & 3u) * 4 + (block >> 2 & 3u)] = (uint8_t)scale;
+    };
+    fetch(threadIdx.x);
+    // ... and the many rows' scales, a word a thread; those behind the last block are 1
+    const uint32_t row_words = row_blocks / 4, last_word = (blocks - 1) / 4;
+    for (uint32_t at = threadIdx.x; at < 16 * NT * row_words; at += blockDim.x) {
+        const uint32_t r = at / row_words, word = at - r * row_words;
+        const int64_t j = j0 + r < many.rows ? j0 + r : many.rows - 1;
+        uint32_t w = word <= last_word ? *reinterpret_cast<const uint32_t*>(many.scales + j * many.ld_scales + 4 * word) : 0x7F7F7F7Fu;
+        const uint32_t live = blocks - 4 * word;
+        if (word == last_word && live < 4) w = (w & ((1u << (8 * live)) - 1u)) | (0x7F7F7F7Fu & ~((1u << (8 * live)) - 1u));
+        *reinterpret_cast<uint32_t*>(many_scales + r * many_pitch(turns) + 4 * word) = w;
+    }
+    // then the first turn's codes; what lies behind the last block is some block's, and meets zeros of the few rows
+    const uint32_t* rows[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int64_t j = j0 + 16 * t + in, row = j < many.rows ? j : many.rows - 1;
+        rows[t] = many.codes + row * many.ld_words;
+    }
+    u32x4 codes[NT][4];
+    auto load = [&](uint32_t block) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                codes[t][s] = *reinterpret_cast<const u32x4*>(rows[t] + 4 * (int64_t)min(block + 4 * s + g, blocks - 1));
+    };
+    uint32_t block = wave * kTurn;
+    load(block);
+    for (uint32_t at = threadIdx.x; at < few_blocks; at += blockDim.x) {
+        if (at >= blockDim.x) fetch(at);
+        hold(at);
+    }
+    __syncthreads();
+    f32x4 acc[NT] = {};
+    const uint32_t few_row = min(in, few.count - 1);
+    while (block < blocks) {
+        u32x4 x[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) x[s] = *reinterpret_cast<const u32x4*>(held + few_row * pitch + (block + 4 * s + g) * 16);
+        const uint32_t xs = *reinterpret_cast<const uint32_t*>(held_scales + few_row * row_blocks + block + 4 * g);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const uint32_t ws =
+                pick_scales(*reinterpret_cast<const u32x4*>(many_scales + (16 * t + in) * many_pitch(turns) + block), g);
+            acc[t] = mfma<0>(codes[t][0], ws, x[0], xs, acc[t]);
+            acc[t] = mfma<1>(codes[t][1], ws, x[1], xs, acc[t]);
+            acc[t] = mfma<2>(codes[t][2], ws, x[2], xs, acc[t]);
+            acc[t] = mfma<3>(codes[t][3], ws, x[3], xs, acc[t]);
+        }
+        block += waves * kTurn;
+        if (block < blocks) load(block);
+    }
+    __syncthreads();
+    f32x4* sums = reinterpret_cast<f32x4*>(held);                         // wavefront, tile, lane
+#pragma unroll
+    for (int t = 0; t < NT; ++t) sums[(wave * NT + t) * 64 + lane] = acc[t];
+    __syncthreads();
+    for (uint32_t at = threadIdx.x; at < NT * 64; at += blockDim.x) {
+        f32x4 v = sums[at];
+        for (uint32_t w = 1; w < waves; ++w) v += sums[w * NT * 64 + at];
+        const uint32_t i = at & 15u;
+        const int64_t j = j0 + at / 64 * 16 + (at >> 4 & 3u) * 4;
+        if (i >= few.count) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (j + e < many.rows) put(c + (j + e) * step_many + i * step_few, v[e]);
+    }
+}
+
 // How a product is cut: tiles of 64 `mt` rows of each factor (0: the kernel without LDS), and the steps of k over `splits`.
 struct Cut {
     int      mt;
@@ -402,9 +608,50 @@ static mv_status launch_product_of(const Factor& a, const Factor& b, int64_t k, 
     return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
 }
 
+constexpr int64_t kFewRows = 16;
+constexpr uint32_t kFewLds = 144 * 1024;
+// Workgroups of the kernel for few rows read all of k: so many of its rows, or so short rows, and it is the faster one.
+// Workgroups of 16 rows as long as all of them run at once, three to a unit; beyond that 32 rows, which share what a
+// workgroup spends on the few rows.  Four bf16 rows against 8192 x 8192: 13.0 us with 16 and 13.4 with 32; 12,000 x 8192
+// 15.9 and 17.5; 14,000 x 8192 19.5 and 18.0; 16,384 x 6000 18.8 and 14.7; 16,384 x 8192 28 and 19.9.
+inline int few_tiles(int64_t many) { return many > 12288 ? 2 : 1; }
+inline bool few_fits(int64_t few, int64_t many, int64_t k)
+{
+    const int64_t turns = (blocks_of(k) + kTurn - 1) / kTurn;
+    return few <= kFewRows && (many >= 512 || k <= 8192) && turns < 4096 && few_bytes((uint32_t)few, (uint32_t)turns, 16u * (uint32_t)few_tiles(many)) <= kFewLds;
+}
+
+template <int NT, typename X, typename T>
+static void launch_few_of(const Factor& many, const Few<X>& few, int64_t k, T* c, int64_t step_many, int64_t step_few, hipStream_t st)
+{
+    const uint32_t blocks = (uint32_t)blocks_of(k), turns = (blocks + kTurn - 1) / kTurn;
+    const uint32_t waves = turns < kFewWaves ? turns : kFewWaves;
+    const uint32_t room = few_bytes(few.count, turns, 16 * NT), sums = waves * NT * 1024;
+    hipLaunchKernelGGL((mv_mx_product_few_kernel<NT, X, T>), dim3((uint32_t)((many.rows + 16 * NT - 1) / (16 * NT))),
+                       dim3(64 * waves), room > sums ? room : sums, st, many, few, blocks, k, c, step_many, step_few);
+}
+template <typename X, typename T>
+static mv_status launch_few(const Factor& many, const Few<X>& few, int64_t k, T* c, int64_t step_many, int64_t step_few, hipStream_t st)
+{
+    if (many.rows / 16 > kMostGroups / 2) return MV_ERR_INVALID_ARG;
+    if (few_tiles(many.rows) == 2) launch_few_of<2>(many, few, k, c, step_many, step_few, st);
+    else launch_few_of<1>(many, few, k, c, step_many, step_few, st);
+    return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
+}
+template <typename T>
+static mv_status launch_few_codes(const Factor& a, const Factor& b, int64_t k, T* c, int64_t ld_c, hipStream_t st)
+{
+    if (few_fits(a.rows, b.rows, k))
+        return launch_few(b, Few<uint32_t>{a.codes, a.ld_words, a.scales, a.ld_scales, (uint32_t)a.rows}, k, c, 1, ld_c, st);
+    return launch_few(a, Few<uint32_t>{b.codes, b.ld_words, b.scales, b.ld_scales, (uint32_t)b.rows}, k, c, ld_c, 1, st);
+}
+
 static mv_status launch_product(const Factor& a, const Factor& b, int64_t k, void* c, int32_t c_dtype, int64_t ld_c, void* parts,
                                 hipStream_t st)
 {
+    if (few_fits(a.rows, b.rows, k) || few_fits(b.rows, a.rows, k))
+        return c_dtype == MV_BF16 ? launch_few_codes(a, b, k, static_cast<uint16_t*>(c), ld_c, st)
+                                  : launch_few_codes(a, b, k, static_cast<float*>(c), ld_c, st);
     // byte offsets inside a tile's rows are 32 bits
     if (a.ld_words * 4 > (1 << 22) || b.ld_words * 4 > (1 << 22)) {
         const int64_t tiles_m = (a.rows + 2 * kTile - 1) / (2 * kTile), tiles_n = (b.rows + 2 * kTile - 1) / (2 * kTile);
@@ -486,6 +733,17 @@ mv_status mv_mx_linear(const void* x, int32_t x_dtype, int64_t ld_x, const uint3
         !scratch_valid(scratch, scratch_bytes, mv_mx_linear_scratch_bytes(m, n, k)))
         return MV_ERR_INVALID_ARG;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    if (few_fits(m, n, k)) {
+        const Factor w = {w_codes, w_scales, ld_words, ld_scales, n};
+        if (x_dtype == MV_BF16) {
+            const Few<uint16_t> f = {static_cast<const uint16_t*>(x), ld_x, nullptr, 0, (uint32_t)m};
+            return y_dtype == MV_BF16 ? launch_few(w, f, k, static_cast<uint16_t*>(y), 1, ld_y, st)
+                                      : launch_few(w, f, k, static_cast<float*>(y), 1, ld_y, st);
+        }
+        const Few<float> f = {static_cast<const float*>(x), ld_x, nullptr, 0, (uint32_t)m};
+        return y_dtype == MV_BF16 ? launch_few(w, f, k, static_cast<uint16_t*>(y), 1, ld_y, st)
+                                  : launch_few(w, f, k, static_cast<float*>(y), 1, ld_y, st);
+    }
     char* at = static_cast<char*>(scratch);
     const Held q = carve(at, m, k);
     if (const mv_status rc = launch_encode(x, x_dtype, ld_x, m, k, q.codes, q.ld_words, q.scales, q.ld_scales, nullptr, 0, st))
