@@ -381,13 +381,17 @@ def mv_quant_decode(streams, n: int, q: int, means, out, stream=None) -> None:
 _dtypes = None      # torch.float32 and torch.bfloat16 to mv_dtype, once torch is there
 
 
-def _value_type(t, what: str) -> int:
-    """mv_dtype of a float32 or bfloat16 tensor."""
+def _types():
     global _dtypes
     if _dtypes is None:
         import torch
         _dtypes = {torch.float32: MV_F32, torch.bfloat16: MV_BF16}
-    d = _dtypes.get(t.dtype)
+    return _dtypes
+
+
+def _value_type(t, what: str) -> int:
+    """mv_dtype of a float32 or bfloat16 tensor."""
+    d = (_dtypes or _types()).get(t.dtype)
     if d is None:
         raise ValueError("%s is %s: float32 or bfloat16 is wanted" % (what, t.dtype))
     return d
@@ -425,29 +429,42 @@ class _Clip(ctypes.c_void_p):
     """Handle of mv_clip_begin, with what the calls on it check against."""
     n_groups = 0
     device = -1
-    sizes = ()          # (shape, dtype, out's dtype or None) of each tensor given
+    groups = ()         # of each tensor given
+    rows = None         # the list the library has
+    writes = False
 
 
 def _clip_list(tensors, out, groups, device):
-    """The list as the library takes it, and the tensors' shapes and types."""
-    tensors, out = list(tensors), list(out) if out is not None else None
+    """The list as the library takes it: a numpy array of mv_clip_tensor."""
+    import numpy as np
+    out = list(out) if out is not None else None
     if not tensors or (out is not None and len(out) != len(tensors)):
         raise ValueError("as many tensors to write as to read, and at least one")
     if len(groups) != len(tensors):
         raise ValueError("a group for each tensor is wanted")
-    rows, sizes = [], []
-    for i, t in enumerate(tensors):
-        o = out[i] if out is not None else None
-        if t.get_device() != device or (o is not None and o.get_device() != device):
-            raise ValueError("all tensors have to be on one GPU")
-        ts, to = _value_type(t, "a gradient"), _value_type(o, "a gradient's place") if o is not None else MV_F32
-        sizes.append((t.shape, t.dtype, None if o is None else o.dtype))
-        if t.is_contiguous() and (o is None or (o.shape == t.shape and o.is_contiguous())):
-            rows.append((t.data_ptr(), o.data_ptr() if o is not None else 0, t.numel(), groups[i], ts, to))
-        else:
-            rows += [(a.data_ptr(), b.data_ptr() if b is not None else 0, a.numel(), groups[i], ts, to)
-                     for a, b in _pieces(t, o)]
-    return rows, sizes
+    both = tensors if out is None else tensors + out
+    if any([t.get_device() != device for t in both]):
+        raise ValueError("all tensors have to be on one GPU")
+    if not all([t.is_contiguous() for t in both]):
+        pieces = [(a, b, g) for i, g in enumerate(groups) for a, b in _pieces(tensors[i], out[i] if out is not None else None)]
+        tensors, groups = [p[0] for p in pieces], [p[2] for p in pieces]
+        out = [p[1] for p in pieces] if out is not None else None
+    elif out is not None and [t.shape for t in tensors] != [t.shape for t in out]:
+        raise ValueError("a tensor does not go to one of another shape")
+    types = _types()
+    rows = np.zeros(len(tensors), dtype=np.dtype(mv_clip_tensor))
+    try:
+        rows["src_dtype"] = [types[t.dtype] for t in tensors]
+        if out is not None:
+            rows["dst_dtype"] = [types[t.dtype] for t in out]
+    except KeyError as e:
+        raise ValueError("a gradient or its place is %s: float32 or bfloat16 is wanted" % e) from None
+    rows["src"] = [t.data_ptr() for t in tensors]
+    rows["numel"] = [t.numel() for t in tensors]
+    rows["group"] = groups
+    if out is not None:
+        rows["dst"] = [t.data_ptr() for t in out]
+    return rows
 
 
 def mv_clip_begin(tensors, out=None, groups=None, norm: int = MV_NORM_L2, n_groups: Optional[int] = None,
@@ -460,41 +477,41 @@ def mv_clip_begin(tensors, out=None, groups=None, norm: int = MV_NORM_L2, n_grou
     tensors = list(tensors)
     device = tensors[0].get_device() if tensors else -1
     groups = [0] * len(tensors) if groups is None else [int(g) for g in groups]
-    rows, sizes = _clip_list(tensors, out, groups, device)
+    rows = _clip_list(tensors, out, groups, device)
     n_groups = max(groups) + 1 if n_groups is None else int(n_groups)
     cfg = mv_clip_config(ctypes.sizeof(mv_clip_config), device, n_groups, norm, workspace or None, workspace_bytes)
     h = _Clip()
-    st = load().mv_clip_begin(ctypes.byref(cfg), (mv_clip_tensor * len(rows))(*rows), len(rows), ctypes.byref(h))
+    st = load().mv_clip_begin(ctypes.byref(cfg), rows.ctypes.data, len(rows), ctypes.byref(h))
     if st != MV_OK:
         raise MvError(st, "mv_clip_begin")
-    h.n_groups, h.device, h.sizes, h.groups = n_groups, device, sizes, groups
-    h.rows = [r[2:] for r in rows]
+    h.n_groups, h.device, h.groups, h.rows, h.writes = n_groups, device, groups, rows, out is not None
     return h
 
 
 def mv_clip_bind(clip: _Clip, tensors, out=None, stream=None) -> None:
-    """The handle's tensors from now on (in the stream's order): others of the same shapes, types and strides."""
+    """The handle's tensors from now on (in the stream's order): others of the same sizes, types and strides."""
     tensors = list(tensors)
-    rows, sizes = _clip_list(tensors, out, clip.groups, clip.device)
-    if sizes != clip.sizes or [r[2:] for r in rows] != clip.rows:
-        raise ValueError("the tensors' shapes, types and strides have to be those the handle was made for")
-    pointers = ctypes.c_void_p * len(rows)
-    st = load().mv_clip_bind(clip, pointers(*[r[0] for r in rows]), pointers(*[r[1] for r in rows]),
-                             _stream_handle(stream, tensors[0]))
+    if (out is None) != (not clip.writes):
+        raise ValueError("the handle was made %s places to write to" % ("with" if clip.writes else "without"))
+    rows = _clip_list(tensors, out, clip.groups, clip.device)
+    if len(rows) != len(clip.rows) or any((rows[f] != clip.rows[f]).any() for f in ("numel", "group", "src_dtype", "dst_dtype")):
+        raise ValueError("the tensors' sizes, types and strides have to be those the handle was made for")
+    pointers = rows["src"].copy(), rows["dst"].copy()
+    st = load().mv_clip_bind(clip, pointers[0].ctypes.data, pointers[1].ctypes.data, _stream_handle(stream, tensors[0]))
     if st != MV_OK:
         raise MvError(st, "mv_clip_bind")
 
 
 def mv_clip_norms(clip: _Clip, norms, stream=None) -> None:
     """norms: n_groups float32 on the device, out."""
-    st = load().mv_clip_norms(clip, _float32(norms, "norms", clip.n_groups, clip.device), _stream_handle(stream, norms))
+    st = (_lib or load()).mv_clip_norms(clip, _float32(norms, "norms", clip.n_groups, clip.device), _stream_handle(stream, norms))
     if st != MV_OK:
         raise MvError(st, "mv_clip_norms")
 
 
 def mv_clip_grads(clip: _Clip, max_norm: float, norms, coefs=None, stream=None) -> None:
     """The clipped gradients in the handle's `out` tensors; norms and coefs (may be None): n_groups float32, out."""
-    st = load().mv_clip_grads(clip, max_norm, _float32(norms, "norms", clip.n_groups, clip.device),
+    st = (_lib or load()).mv_clip_grads(clip, max_norm, _float32(norms, "norms", clip.n_groups, clip.device),
                               _float32(coefs, "coefs", clip.n_groups, clip.device), _stream_handle(stream, norms))
     if st != MV_OK:
         raise MvError(st, "mv_clip_grads")
@@ -523,27 +540,30 @@ def mv_mx_row_scales(n: int) -> int:
     return int(load().mv_mx_row_scales(n))
 
 
-def _matrix(t, what: str, shape, device: int):
+def _matrix(t, what: str, rows: int, n: int, device: int):
     """(address, mv_dtype, row stride) of a float32 or bfloat16 matrix with unit column stride."""
-    d = _value_type(t, what)
-    if t.shape != shape or t.get_device() != device:
-        raise ValueError("%s is %s on GPU %d: %s on GPU %d is wanted" % (what, tuple(t.shape), t.get_device(), tuple(shape), device))
+    d = (_dtypes or _types()).get(t.dtype)
     ld, step = t.stride()
-    if step != 1 and shape[1] > 1:
-        raise ValueError("%s has a column stride of %d: 1 is wanted" % (what, step))
-    return t.data_ptr(), d, ld if shape[0] > 1 else max(ld, shape[1])
+    if d is None or step != 1 or t.get_device() != device or t.shape != (rows, n):
+        d = _value_type(t, what)
+        if t.shape != (rows, n) or t.get_device() != device:
+            raise ValueError("%s is %s on GPU %d: %s on GPU %d is wanted" % (what, tuple(t.shape), t.get_device(), (rows, n), device))
+        if n > 1:
+            raise ValueError("%s has a column stride of %d: 1 is wanted" % (what, step))
+    return t.data_ptr(), d, ld if rows > 1 else max(ld, n)
 
 
 def _codes(codes, scales, rows: int, n: int, device: int, what: str = "codes"):
     """(address, row stride) of both, for `rows` rows of n values."""
+    (r, words), (q, places) = codes.shape, scales.shape
+    (ld_c, step_c), (ld_s, step_s) = codes.stride(), scales.stride()
     blocks = (n + 31) // 32
-    if (codes.element_size() != 4 or scales.element_size() != 1 or codes.get_device() != device or scales.get_device() != device
-            or codes.dim() != 2 or scales.dim() != 2 or codes.shape[0] < rows or scales.shape[0] < rows
-            or codes.shape[1] < 4 * blocks or scales.shape[1] < (blocks + 3) // 4 * 4 or codes.stride(1) != 1
-            or scales.stride(1) != 1):
+    if (r < rows or q < rows or words < 4 * blocks or places < (blocks + 3) // 4 * 4 or step_c != 1 or step_s != 1
+            or codes.get_device() != device or scales.get_device() != device or codes.element_size() != 4
+            or scales.element_size() != 1):
         raise ValueError("%s and scales have to be %d rows of mv_mx_row_words(%d) 32-bit words and mv_mx_row_scales(%d) bytes "
                          "or more, on the same GPU" % (what, rows, n, n))
-    return codes.data_ptr(), codes.stride(0), scales.data_ptr(), scales.stride(0)
+    return codes.data_ptr(), ld_c, scales.data_ptr(), ld_s
 
 
 def _scratch_of(scratch, device: int):
@@ -551,7 +571,7 @@ def _scratch_of(scratch, device: int):
         return 0, 0
     if scratch.get_device() != device or not scratch.is_contiguous():
         raise ValueError("scratch has to be contiguous memory on the same GPU")
-    return scratch.data_ptr(), scratch.numel() * scratch.element_size()
+    return scratch.data_ptr(), scratch.nbytes
 
 
 def mv_mx_encode(vals, codes, scales, resid=None, stream=None) -> None:
@@ -560,14 +580,14 @@ def mv_mx_encode(vals, codes, scales, resid=None, stream=None) -> None:
     may be given."""
     rows, n = vals.shape
     device = vals.get_device()
-    v, d, ld = _matrix(vals, "vals", vals.shape, device)
+    v, d, ld = _matrix(vals, "vals", rows, n, device)
     c, ld_c, s, ld_s = _codes(codes, scales, rows, n, device)
     r, ld_r = 0, 0
     if resid is not None:
-        r, rd, ld_r = _matrix(resid, "resid", vals.shape, device)
+        r, rd, ld_r = _matrix(resid, "resid", rows, n, device)
         if rd != MV_F32:
             raise ValueError("resid has to be float32")
-    st = load().mv_mx_encode(v, d, ld, rows, n, c, ld_c, s, ld_s, r, ld_r, _stream_handle(stream, vals))
+    st = (_lib or load()).mv_mx_encode(v, d, ld, rows, n, c, ld_c, s, ld_s, r, ld_r, _stream_handle(stream, vals))
     if st != MV_OK:
         raise MvError(st, "mv_mx_encode")
 
@@ -576,8 +596,8 @@ def mv_mx_encode_t(vals, codes, scales, stream=None) -> None:
     """The columns of vals (rows x n): codes: n x mv_mx_row_words(rows), scales: n x mv_mx_row_scales(rows) (out)."""
     rows, n = vals.shape
     device = vals.get_device()
-    v, d, ld = _matrix(vals, "vals", vals.shape, device)
-    st = load().mv_mx_encode_t(v, d, ld, rows, n, *_codes(codes, scales, n, rows, device), _stream_handle(stream, vals))
+    v, d, ld = _matrix(vals, "vals", rows, n, device)
+    st = (_lib or load()).mv_mx_encode_t(v, d, ld, rows, n, *_codes(codes, scales, n, rows, device), _stream_handle(stream, vals))
     if st != MV_OK:
         raise MvError(st, "mv_mx_encode_t")
 
@@ -586,8 +606,8 @@ def mv_mx_decode(codes, scales, out, stream=None) -> None:
     """out: rows x n float32 or bfloat16 (out), what the codes stand for."""
     rows, n = out.shape
     device = out.get_device()
-    o, d, ld = _matrix(out, "out", out.shape, device)
-    st = load().mv_mx_decode(*_codes(codes, scales, rows, n, device), rows, n, o, d, ld, _stream_handle(stream, out))
+    o, d, ld = _matrix(out, "out", rows, n, device)
+    st = (_lib or load()).mv_mx_decode(*_codes(codes, scales, rows, n, device), rows, n, o, d, ld, _stream_handle(stream, out))
     if st != MV_OK:
         raise MvError(st, "mv_mx_decode")
 
@@ -595,14 +615,14 @@ def mv_mx_decode(codes, scales, out, stream=None) -> None:
 def mv_mx_aggregate(codes, scales, weights, agg, stream=None) -> None:
     """agg: n float32 (out), the rows' weighted sum; weights: a float32 for each row of codes, or None for the mean."""
     rows, n, device = codes.shape[0], agg.numel(), agg.get_device()
-    st = load().mv_mx_aggregate(*_codes(codes, scales, rows, n, device), rows, n, _float32(weights, "weights", rows, device),
+    st = (_lib or load()).mv_mx_aggregate(*_codes(codes, scales, rows, n, device), rows, n, _float32(weights, "weights", rows, device),
                                 _float32(agg, "agg", n, device), _stream_handle(stream, agg))
     if st != MV_OK:
         raise MvError(st, "mv_mx_aggregate")
 
 
 def mv_mx_product_scratch_bytes(m: int, n: int, k: int) -> int:
-    return int(load().mv_mx_product_scratch_bytes(m, n, k))
+    return (_lib or load()).mv_mx_product_scratch_bytes(m, n, k)
 
 
 def mv_mx_product(a_codes, a_scales, b_codes, b_scales, k: int, out, scratch=None, stream=None) -> None:
@@ -610,15 +630,15 @@ def mv_mx_product(a_codes, a_scales, b_codes, b_scales, k: int, out, scratch=Non
     scratch: mv_mx_product_scratch_bytes(m, n, k) bytes."""
     m, n = out.shape
     device = out.get_device()
-    o, d, ld = _matrix(out, "out", out.shape, device)
-    st = load().mv_mx_product(*_codes(a_codes, a_scales, m, k, device, "a_codes"), *_codes(b_codes, b_scales, n, k, device, "b_codes"),
+    o, d, ld = _matrix(out, "out", m, n, device)
+    st = (_lib or load()).mv_mx_product(*_codes(a_codes, a_scales, m, k, device, "a_codes"), *_codes(b_codes, b_scales, n, k, device, "b_codes"),
                               m, n, k, o, d, ld, *_scratch_of(scratch, device), _stream_handle(stream, out))
     if st != MV_OK:
         raise MvError(st, "mv_mx_product")
 
 
 def mv_mx_linear_scratch_bytes(m: int, n: int, k: int) -> int:
-    return int(load().mv_mx_linear_scratch_bytes(m, n, k))
+    return (_lib or load()).mv_mx_linear_scratch_bytes(m, n, k)
 
 
 def mv_mx_linear(x, w_codes, w_scales, out, scratch, stream=None) -> None:
@@ -626,16 +646,16 @@ def mv_mx_linear(x, w_codes, w_scales, out, scratch, stream=None) -> None:
     m, k = x.shape
     n = out.shape[1]
     device = out.get_device()
-    a, xd, ld_x = _matrix(x, "x", x.shape, device)
-    o, d, ld = _matrix(out, "out", (m, n), device)
-    st = load().mv_mx_linear(a, xd, ld_x, *_codes(w_codes, w_scales, n, k, device, "w_codes"), m, n, k, o, d, ld,
+    a, xd, ld_x = _matrix(x, "x", m, k, device)
+    o, d, ld = _matrix(out, "out", m, n, device)
+    st = (_lib or load()).mv_mx_linear(a, xd, ld_x, *_codes(w_codes, w_scales, n, k, device, "w_codes"), m, n, k, o, d, ld,
                              *_scratch_of(scratch, device), _stream_handle(stream, out))
     if st != MV_OK:
         raise MvError(st, "mv_mx_linear")
 
 
 def mv_mx_linear_grad_scratch_bytes(m: int, n: int, k: int) -> int:
-    return int(load().mv_mx_linear_grad_scratch_bytes(m, n, k))
+    return (_lib or load()).mv_mx_linear_grad_scratch_bytes(m, n, k)
 
 
 def mv_mx_linear_grad(x, dy, wt_codes, wt_scales, dx, dw, scratch, stream=None) -> None:
@@ -644,17 +664,17 @@ def mv_mx_linear_grad(x, dy, wt_codes, wt_scales, dx, dw, scratch, stream=None) 
     m, n = dy.shape
     device = dy.get_device()
     k = dx.shape[1] if dx is not None else x.shape[1]
-    g, yd, ld_dy = _matrix(dy, "dy", dy.shape, device)
+    g, yd, ld_dy = _matrix(dy, "dy", m, n, device)
     a, ld_x, w, o, od, ld_dx, p, pd, ld_dw = 0, 0, (0, 0, 0, 0), 0, 0, 0, 0, 0, 0
     if dx is not None:
         w = _codes(wt_codes, wt_scales, k, n, device, "wt_codes")
-        o, od, ld_dx = _matrix(dx, "dx", (m, k), device)
+        o, od, ld_dx = _matrix(dx, "dx", m, k, device)
     if dw is not None:
-        a, xd, ld_x = _matrix(x, "x", (m, k), device)
+        a, xd, ld_x = _matrix(x, "x", m, k, device)
         if xd != yd:
             raise ValueError("x and dy have to be of one type")
-        p, pd, ld_dw = _matrix(dw, "dw", (n, k), device)
-    st = load().mv_mx_linear_grad(a, ld_x, g, ld_dy, yd, *w, m, n, k, o, od, ld_dx, p, pd, ld_dw,
+        p, pd, ld_dw = _matrix(dw, "dw", n, k, device)
+    st = (_lib or load()).mv_mx_linear_grad(a, ld_x, g, ld_dy, yd, *w, m, n, k, o, od, ld_dx, p, pd, ld_dw,
                                   *_scratch_of(scratch, device), _stream_handle(stream, dy))
     if st != MV_OK:
         raise MvError(st, "mv_mx_linear_grad")

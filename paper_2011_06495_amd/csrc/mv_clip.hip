@@ -20,7 +20,14 @@
 
 namespace mvc {
 
-constexpr int kChunk = 16384;
+#ifndef CHUNK
+#define CHUNK 16384
+#endif
+#ifndef BATCH_MB
+#define BATCH_MB 64
+#endif
+constexpr int kChunk = CHUNK;
+constexpr int64_t kBatchBytes = (int64_t)BATCH_MB << 20;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBindMost = 128;      // pairs of addresses in the arguments of one launch
@@ -50,64 +57,74 @@ typedef uint16_t u16x8 __attribute__((ext_vector_type(8), aligned(2)));
 __device__ __forceinline__ float widen(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
 
 // To the nearest bf16, ties to even; NaN stays NaN.
-__device__ __forceinline__ uint16_t narrow(float x)
-{
-    const uint32_t u = __float_as_uint(x);
-    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return (uint16_t)((u >> 16) | 0x40u);
-    return (uint16_t)((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
-}
+__device__ __forceinline__ uint16_t narrow(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+// Addresses that come out of memory are not known to be global memory's otherwise.
+#define MV_GLOBAL __attribute__((address_space(1)))
+typedef MV_GLOBAL float          gfloat;
+typedef MV_GLOBAL uint16_t       gshort;
+typedef const MV_GLOBAL float    cfloat;
+typedef const MV_GLOBAL uint16_t cshort;
 
 // V consecutive elements as fp32.
 template <int V>
-__device__ __forceinline__ void load(const float* p, float (&x)[V])
+__device__ __forceinline__ void load(cfloat* p, float (&x)[V])
 {
 #pragma unroll
     for (int i = 0; i < V; i += 4) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(p + i);
+        const f32x4 v = *reinterpret_cast<const MV_GLOBAL f32x4*>(p + i);
         x[i] = v.x, x[i + 1] = v.y, x[i + 2] = v.z, x[i + 3] = v.w;
     }
 }
 template <int V>
-__device__ __forceinline__ void load(const uint16_t* p, float (&x)[V])
+__device__ __forceinline__ void load(cshort* p, float (&x)[V])
 {
     if constexpr (V == 8) {
-        const u16x8 v = *reinterpret_cast<const u16x8*>(p);
+        const u16x8 v = *reinterpret_cast<const MV_GLOBAL u16x8*>(p);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = widen(v[i]);
     } else {
-        const u16x4 v = *reinterpret_cast<const u16x4*>(p);
+        const u16x4 v = *reinterpret_cast<const MV_GLOBAL u16x4*>(p);
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = widen(v[i]);
     }
 }
 template <int V>
-__device__ __forceinline__ void store(float* p, const float (&x)[V])
+__device__ __forceinline__ void store(gfloat* p, const float (&x)[V])
 {
 #pragma unroll
     for (int i = 0; i < V; i += 4) {
         f32x4 v = {x[i], x[i + 1], x[i + 2], x[i + 3]};
-        *reinterpret_cast<f32x4*>(p + i) = v;
+#ifdef NTS
+        __builtin_nontemporal_store(v, reinterpret_cast<MV_GLOBAL f32x4*>(p + i));
+#else
+        *reinterpret_cast<MV_GLOBAL f32x4*>(p + i) = v;
+#endif
     }
 }
 template <int V>
-__device__ __forceinline__ void store(uint16_t* p, const float (&x)[V])
+__device__ __forceinline__ void store(gshort* p, const float (&x)[V])
 {
     if constexpr (V == 8) {
         u16x8 v;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = narrow(x[i]);
-        *reinterpret_cast<u16x8*>(p) = v;
+#ifdef NTS
+        __builtin_nontemporal_store(v, reinterpret_cast<MV_GLOBAL u16x8*>(p));
+#else
+        *reinterpret_cast<MV_GLOBAL u16x8*>(p) = v;
+#endif
     } else {
         u16x4 v;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = narrow(x[i]);
-        *reinterpret_cast<u16x4*>(p) = v;
+        *reinterpret_cast<MV_GLOBAL u16x4*>(p) = v;
     }
 }
-__device__ __forceinline__ float one(const float* p) { return *p; }
-__device__ __forceinline__ float one(const uint16_t* p) { return widen(*p); }
-__device__ __forceinline__ void put(float* p, float x) { *p = x; }
-__device__ __forceinline__ void put(uint16_t* p, float x) { *p = narrow(x); }
+__device__ __forceinline__ float one(cfloat* p) { return *p; }
+__device__ __forceinline__ float one(cshort* p) { return widen(*p); }
+__device__ __forceinline__ void put(gfloat* p, float x) { *p = x; }
+__device__ __forceinline__ void put(gshort* p, float x) { *p = narrow(x); }
 
 // A lane's share of a sum of squares or of a maximum.
 template <bool MAX>
@@ -165,7 +182,7 @@ __device__ __forceinline__ float coef_of(float norm, float max_norm)
 
 // Elements [0, n) of a chunk: a thread takes V of them at a time, U times in flight.
 template <int V, int U, int THREADS, bool MAX, typename S>
-__device__ __forceinline__ void gather(const S* src, int n, Share<MAX>& share)
+__device__ __forceinline__ void gather(S* src, int n, Share<MAX>& share)
 {
     constexpr int kStep = THREADS * V;
     int at = (int)threadIdx.x * V;
@@ -184,11 +201,11 @@ __device__ __forceinline__ void gather(const S* src, int n, Share<MAX>& share)
 #pragma unroll
         for (int i = 0; i < V; ++i) share.add(i, x[i]);
     }
-    for (int i = 0; at + i < n; ++i) share.add(i, one(src + at + i));
+    for (int i = 0; at + i < n; ++i) share.add(0, one(src + at + i));
 }
 
 template <int V, int U, int THREADS, typename S, typename D>
-__device__ __forceinline__ void scale(const S* src, D* dst, int n, float c)
+__device__ __forceinline__ void scale(S* src, D* dst, int n, float c)
 {
     constexpr int kStep = THREADS * V;
     int at = (int)threadIdx.x * V;
@@ -224,8 +241,8 @@ __device__ __forceinline__ void gather_chunk(const Tensor& t, Chunk c, Share<MAX
 {
     const int n = chunk_count(t, c);
     const int64_t first = (int64_t)c.index * kChunk;
-    if (t.src_bf16) gather<8, 4, THREADS, MAX>(static_cast<const uint16_t*>(t.src) + first, n, share);
-    else gather<4, 8, THREADS, MAX>(static_cast<const float*>(t.src) + first, n, share);
+    if (t.src_bf16) gather<8, 4, THREADS, MAX>((cshort*)t.src + first, n, share);
+    else gather<4, 8, THREADS, MAX>((cfloat*)t.src + first, n, share);
 }
 
 template <int THREADS>
@@ -235,13 +252,13 @@ __device__ __forceinline__ void scale_chunk(const Tensor& t, Chunk k, float c)
     const int n = chunk_count(t, k);
     const int64_t first = (int64_t)k.index * kChunk;
     if (t.src_bf16) {
-        const uint16_t* s = static_cast<const uint16_t*>(t.src) + first;
-        if (t.dst_bf16) scale<8, 4, THREADS>(s, static_cast<uint16_t*>(t.dst) + first, n, c);
-        else scale<4, 8, THREADS>(s, static_cast<float*>(t.dst) + first, n, c);
+        cshort* s = (cshort*)t.src + first;
+        if (t.dst_bf16) scale<8, 4, THREADS>(s, (gshort*)t.dst + first, n, c);
+        else scale<4, 8, THREADS>(s, (gfloat*)t.dst + first, n, c);
     } else {
-        const float* s = static_cast<const float*>(t.src) + first;
-        if (t.dst_bf16) scale<4, 8, THREADS>(s, static_cast<uint16_t*>(t.dst) + first, n, c);
-        else scale<4, 8, THREADS>(s, static_cast<float*>(t.dst) + first, n, c);
+        cfloat* s = (cfloat*)t.src + first;
+        if (t.dst_bf16) scale<4, 8, THREADS>(s, (gshort*)t.dst + first, n, c);
+        else scale<4, 8, THREADS>(s, (gfloat*)t.dst + first, n, c);
     }
 }
 
@@ -254,16 +271,54 @@ __device__ __forceinline__ double group_value(const Lists& l, uint32_t first, ui
     return of_workgroup<MAX, THREADS / 64>(v, lds);
 }
 
+struct Range {
+    uint32_t first, count;          // of chunks
+};
+
 template <bool MAX>
-__global__ __launch_bounds__(kThreads) void mv_clip_gather(Lists l)
+__device__ __forceinline__ void gather_one(const Lists& l, uint32_t at, double* lds)
 {
-    __shared__ double lds[kWaves];
-    const Chunk c = l.chunks[blockIdx.x];
+    const Chunk c = l.chunks[at];
     const Tensor t = l.tensors[c.tensor];
     Share<MAX> share;
     gather_chunk<kThreads, MAX>(t, c, share);
     const double v = of_workgroup<MAX, kWaves>(share.value(), lds);
-    if (threadIdx.x == 0) l.partial[blockIdx.x] = v;
+    if (threadIdx.x == 0) l.partial[at] = v;
+}
+
+template <bool MAX>
+__device__ __forceinline__ void scale_one(const Lists& l, uint32_t at, float max_norm, float* __restrict__ norms,
+                                          float* __restrict__ coefs, double* lds)
+{
+    const Chunk c = l.chunks[at];
+    const Tensor t = l.tensors[c.tensor];
+    const uint32_t first = l.group_first[t.group], last = l.group_first[t.group + 1];
+    const float norm = norm_of<MAX>(group_value<MAX, kThreads>(l, first, last, lds));
+    const float coef = coef_of(norm, max_norm);
+    if (at == first && threadIdx.x == 0) {
+        norms[t.group] = norm;
+        if (coefs) coefs[t.group] = coef;
+    }
+    scale_chunk<kThreads>(t, c, coef);
+}
+
+template <bool MAX>
+__global__ __launch_bounds__(kThreads) void mv_clip_gather(Lists l)
+{
+    __shared__ double lds[kWaves];
+    gather_one<MAX>(l, blockIdx.x, lds);
+}
+
+// One launch scales a batch of groups and reads the next one, workgroups of both in turn.
+template <bool MAX>
+__global__ __launch_bounds__(kThreads) void mv_clip_turn(Lists l, Range scaled, Range read, float max_norm, float* __restrict__ norms,
+                                                         float* __restrict__ coefs)
+{
+    __shared__ double lds[kWaves];
+    const uint32_t both = 2 * min(scaled.count, read.count), b = blockIdx.x;
+    const uint32_t at = b < both ? b / 2 : b - both / 2;
+    if (b < both ? (b & 1u) != 0 : scaled.count > read.count) scale_one<MAX>(l, scaled.first + at, max_norm, norms, coefs, lds);
+    else gather_one<MAX>(l, read.first + at, lds);
 }
 
 // One workgroup per group.
@@ -274,23 +329,6 @@ __global__ __launch_bounds__(kThreads) void mv_clip_norm(Lists l, float* __restr
     const uint32_t g = blockIdx.x;
     const double v = group_value<MAX, kThreads>(l, l.group_first[g], l.group_first[g + 1], lds);
     if (threadIdx.x == 0) norms[g] = norm_of<MAX>(v);
-}
-
-template <bool MAX>
-__global__ __launch_bounds__(kThreads) void mv_clip_scale(Lists l, float max_norm, float* __restrict__ norms,
-                                                          float* __restrict__ coefs)
-{
-    __shared__ double lds[kWaves];
-    const Chunk c = l.chunks[blockIdx.x];
-    const Tensor t = l.tensors[c.tensor];
-    const uint32_t first = l.group_first[t.group], last = l.group_first[t.group + 1];
-    const float norm = norm_of<MAX>(group_value<MAX, kThreads>(l, first, last, lds));
-    const float coef = coef_of(norm, max_norm);
-    if (blockIdx.x == first && threadIdx.x == 0) {
-        norms[t.group] = norm;
-        if (coefs) coefs[t.group] = coef;
-    }
-    scale_chunk<kThreads>(t, c, coef);
 }
 
 // Groups without chunks have no workgroup above.
@@ -328,6 +366,8 @@ struct mv_clip {
     mvc::Lists     lists;
     mvc::Tensor*   tensors;
     mv_clip_tensor* list;      // the caller's list as it was given
+    uint32_t*      batch_end;  // batches of whole groups, their chunks' ends
+    uint32_t       n_batches;
     hipStream_t    last_stream;
 };
 
@@ -446,17 +486,20 @@ mv_status mv_clip_begin(const mv_clip_config* cfg, const mv_clip_tensor* tensors
     mv_clip* c = new (std::nothrow) mv_clip;
     char* host = new (std::nothrow) char[s.off_partial];
     mv_clip_tensor* list = new (std::nothrow) mv_clip_tensor[(size_t)n_tensors];
-    if (c) {
-        memset(static_cast<void*>(c), 0, sizeof *c);
-        c->list = list;
-    }
+    uint32_t* batch_end = new (std::nothrow) uint32_t[(size_t)cfg->n_groups];
+    int64_t* group_bytes = new (std::nothrow) int64_t[(size_t)cfg->n_groups];
     if (host) memset(host, 0, s.off_partial);
-    if (!c || !host || !list || !lay_out(cfg, tensors, n_tensors, s, host)) {
+    if (!c || !host || !list || !batch_end || !group_bytes || !lay_out(cfg, tensors, n_tensors, s, host)) {
         delete c;
         delete[] host;
         delete[] list;
+        delete[] batch_end;
+        delete[] group_bytes;
         return MV_ERR_ALLOC;
     }
+    memset(static_cast<void*>(c), 0, sizeof *c);
+    c->list = list;
+    c->batch_end = batch_end;
     memcpy(list, tensors, (size_t)n_tensors * sizeof *list);
     c->cfg = *cfg;
     c->has_dst = s.has_dst;
@@ -465,6 +508,18 @@ mv_status mv_clip_begin(const mv_clip_config* cfg, const mv_clip_tensor* tensors
     const uint32_t* first = reinterpret_cast<const uint32_t*>(host + s.off_first);
     for (int32_t g = 0; g < cfg->n_groups; ++g)
         if (first[g] == first[g + 1]) c->any_empty = true;
+    memset(group_bytes, 0, (size_t)cfg->n_groups * sizeof *group_bytes);
+    for (int64_t i = 0; i < n_tensors; ++i) group_bytes[tensors[i].group] += tensors[i].numel * (int64_t)elem(tensors[i].src_dtype);
+    int64_t bytes = 0;
+    for (int32_t g = 0; g < cfg->n_groups; ++g) {
+        if (bytes && bytes + group_bytes[g] > mvc::kBatchBytes) {
+            if (first[g] > (c->n_batches ? batch_end[c->n_batches - 1] : 0)) batch_end[c->n_batches++] = first[g];
+            bytes = 0;
+        }
+        bytes += group_bytes[g];
+    }
+    if (c->n_chunks > (c->n_batches ? batch_end[c->n_batches - 1] : 0)) batch_end[c->n_batches++] = c->n_chunks;
+    delete[] group_bytes;
 
     DeviceGuard guard(cfg->device);
     mv_status st = guard.ok ? MV_OK : MV_ERR_DEVICE;
@@ -490,6 +545,7 @@ mv_status mv_clip_begin(const mv_clip_config* cfg, const mv_clip_tensor* tensors
     if (st != MV_OK) {
         if (c->owns_ws) (void)hipFree(c->ws);
         delete[] list;
+        delete[] batch_end;
         delete c;
         return st;
     }
@@ -558,15 +614,17 @@ mv_status mv_clip_grads(mv_clip* c, float max_norm, float* norms, float* coefs, 
     hipStream_t st = static_cast<hipStream_t>(stream);
     c->last_stream = st;
     c->used = true;
-    const dim3 grid(c->n_chunks), threads(mvc::kThreads);
-    if (c->n_chunks) {
-        if (c->cfg.norm == MV_NORM_MAX) {
-            hipLaunchKernelGGL(mvc::mv_clip_gather<true>, grid, threads, 0, st, c->lists);
-            hipLaunchKernelGGL(mvc::mv_clip_scale<true>, grid, threads, 0, st, c->lists, max_norm, norms, coefs);
-        } else {
-            hipLaunchKernelGGL(mvc::mv_clip_gather<false>, grid, threads, 0, st, c->lists);
-            hipLaunchKernelGGL(mvc::mv_clip_scale<false>, grid, threads, 0, st, c->lists, max_norm, norms, coefs);
-        }
+    const dim3 threads(mvc::kThreads);
+    mvc::Range scaled = {0, 0};
+    for (uint32_t b = 0; c->n_chunks && b <= c->n_batches; ++b) {
+        const uint32_t end = b < c->n_batches ? c->batch_end[b] : c->n_chunks;
+        const mvc::Range read = {scaled.first + scaled.count, end - (scaled.first + scaled.count)};
+        const dim3 grid(scaled.count + read.count);
+        if (c->cfg.norm == MV_NORM_MAX)
+            hipLaunchKernelGGL(mvc::mv_clip_turn<true>, grid, threads, 0, st, c->lists, scaled, read, max_norm, norms, coefs);
+        else
+            hipLaunchKernelGGL(mvc::mv_clip_turn<false>, grid, threads, 0, st, c->lists, scaled, read, max_norm, norms, coefs);
+        scaled = read;
     }
     if (c->any_empty)
         hipLaunchKernelGGL(mvc::mv_clip_empty, dim3(1), threads, 0, st, c->lists, (uint32_t)c->cfg.n_groups, max_norm,
@@ -594,6 +652,7 @@ void mv_clip_release(mv_clip* c)
     if (!c) return;
     if (!c->ended) (void)mv_clip_end(c);
     delete[] c->list;
+    delete[] c->batch_end;
     delete c;
 }
 

@@ -32,31 +32,45 @@ __device__ __forceinline__ Place place_of(int64_t first_block, int64_t row_block
     return p;
 }
 
+// A matrix of values and where its codes go.
+template <typename T>
+struct Encode {
+    const T*  vals;
+    int64_t   ld_vals, rows, n;
+    uint32_t* codes;
+    int64_t   ld_words;
+    uint8_t*  scales;
+    int64_t   ld_scales;
+};
+
 template <typename T, bool RESID>
-__global__ __launch_bounds__(kThreads) void mv_mx_encode_kernel(const T* vals, int64_t ld_vals, int64_t rows, int64_t n,
-                                                                uint32_t* __restrict__ codes, int64_t ld_words,
-                                                                uint8_t* __restrict__ scales, int64_t ld_scales, float* resid,
-                                                                int64_t ld_resid)
+__device__ __forceinline__ void encode_rows(const Encode<T>& e, uint32_t at_group, float* resid, int64_t ld_resid)
 {
-    const Place p = place_of((int64_t)blockIdx.x * (kThreads / 4), blocks_of(n));
-    if (p.row >= rows) return;                         // whole groups of four lanes
+    const Place p = place_of((int64_t)at_group * (kThreads / 4), blocks_of(e.n));
+    if (p.row >= e.rows) return;                       // whole groups of four lanes
     const int64_t at = p.block * kBlock + (threadIdx.x & 3) * 8;
     float x[8];
-    load8(vals + p.row * ld_vals + at, n - at, x);
+    load8(e.vals + p.row * e.ld_vals + at, e.n - at, x);
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
     const uint32_t scale = scale_of(top_of_quad(top));
     const uint32_t w = encode8(x, scale);
-    codes[p.row * ld_words + at / 8] = w;
-    if ((threadIdx.x & 3) == 0) scales[p.row * ld_scales + p.block] = (uint8_t)scale;
+    e.codes[p.row * e.ld_words + at / 8] = w;
+    if ((threadIdx.x & 3) == 0) e.scales[p.row * e.ld_scales + p.block] = (uint8_t)scale;
     if constexpr (RESID) {
         float held[8];
         decode8(w, scale, held);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] -= held[i];
-        store8(resid + p.row * ld_resid + at, n - at, x);
+        store8(resid + p.row * ld_resid + at, e.n - at, x);
     }
+}
+
+template <typename T, bool RESID>
+__global__ __launch_bounds__(kThreads) void mv_mx_encode_kernel(Encode<T> e, float* resid, int64_t ld_resid)
+{
+    encode_rows<T, RESID>(e, blockIdx.x, resid, ld_resid);
 }
 
 // Columns: a wavefront takes 32 rows of 16 bytes of columns in each group of four lanes; lane r of a group has rows
@@ -79,22 +93,29 @@ __device__ __forceinline__ void load_cols(const T* p, int64_t live, float (&x)[k
     }
 }
 template <typename T>
-__global__ __launch_bounds__(64 * kTileBlocks) void mv_mx_encode_t_kernel(const T* __restrict__ vals, int64_t ld_vals,
-                                                                          int64_t rows, int64_t n, int64_t tiles,
-                                                                          uint32_t* __restrict__ codes, int64_t ld_words,
-                                                                          uint8_t* __restrict__ scales, int64_t ld_scales)
+constexpr int kTileCols = 16 * kLaneCols<T>;
+template <typename T>
+struct Columns {                    // of a workgroup: codes and scales on their way out
+    uint32_t words[kTileCols<T>][4 * kTileBlocks];
+    uint8_t  scales[kTileCols<T>][kTileBlocks];
+};
+template <typename T>
+inline int64_t column_tiles(int64_t n) { return (n + kTileCols<T> - 1) / kTileCols<T>; }
+template <typename T>
+inline int64_t column_groups(int64_t rows, int64_t n) { return column_tiles<T>(n) * ((blocks_of(rows) + kTileBlocks - 1) / kTileBlocks); }
+
+template <typename T>
+__device__ __forceinline__ void encode_columns(const Encode<T>& e, uint32_t at_group, Columns<T>& out)
 {
-    constexpr int kCols = kLaneCols<T>, kTileCols = 16 * kCols;
+    constexpr int kCols = kLaneCols<T>;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x / 64, group = lane / 4, r = lane & 3u;
-    const int64_t tile = (int64_t)blockIdx.x % tiles, strip = (int64_t)blockIdx.x / tiles;   // of columns, of rows
-    const int64_t col = tile * kTileCols + group * kCols, row = (strip * kTileBlocks + wave) * kBlock + 8 * r;
-    __shared__ __attribute__((aligned(16))) uint32_t out[kTileCols][4 * kTileBlocks];
-    __shared__ uint8_t held[kTileCols][kTileBlocks];
+    const uint32_t tiles = (uint32_t)((e.n + kTileCols<T> - 1) / kTileCols<T>), tile = at_group % tiles, strip = at_group / tiles;
+    const int64_t col = (int64_t)tile * kTileCols<T> + group * kCols, row = ((int64_t)strip * kTileBlocks + wave) * kBlock + 8 * r;
     float x[8][kCols];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int64_t live = row + i < rows ? n - col : 0;
-        load_cols(vals + (row + i) * ld_vals + col, live, x[i]);
+        const int64_t live = row + i < e.rows ? e.n - col : 0;
+        load_cols(e.vals + (row + i) * e.ld_vals + col, live, x[i]);
     }
 #pragma unroll
     for (int j = 0; j < kCols; ++j) {
@@ -106,19 +127,39 @@ __global__ __launch_bounds__(64 * kTileBlocks) void mv_mx_encode_t_kernel(const 
             top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
         }
         const uint32_t scale = scale_of(top_of_quad(top));
-        out[group * kCols + j][4 * wave + r] = encode8(y, scale);
-        if (r == 0) held[group * kCols + j][wave] = (uint8_t)scale;
+        out.words[group * kCols + j][4 * wave + r] = encode8(y, scale);
+        if (r == 0) out.scales[group * kCols + j][wave] = (uint8_t)scale;
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kTileCols / 64; ++i) {
+    for (int i = 0; i < kTileCols<T> / 64; ++i) {
         const uint32_t c = i * 64 + threadIdx.x / kTileBlocks, b = threadIdx.x % kTileBlocks;
-        const int64_t to = tile * kTileCols + c, to_block = strip * kTileBlocks + b;
-        if (to < n && to_block < blocks_of(rows)) {
-            *reinterpret_cast<u32x4*>(codes + to * ld_words + to_block * 4) = *reinterpret_cast<const u32x4*>(&out[c][4 * b]);
-            scales[to * ld_scales + to_block] = held[c][b];
+        const int64_t to = (int64_t)tile * kTileCols<T> + c, to_block = (int64_t)strip * kTileBlocks + b;
+        if (to < e.n && to_block < blocks_of(e.rows)) {
+            *reinterpret_cast<u32x4*>(e.codes + to * e.ld_words + to_block * 4) = *reinterpret_cast<const u32x4*>(&out.words[c][4 * b]);
+            e.scales[to * e.ld_scales + to_block] = out.scales[c][b];
         }
     }
+}
+
+template <typename T>
+__global__ __launch_bounds__(64 * kTileBlocks) void mv_mx_encode_t_kernel(Encode<T> e)
+{
+    __shared__ __attribute__((aligned(16))) Columns<T> out;
+    encode_columns<T>(e, blockIdx.x, out);
+}
+
+// What a layer's gradients need, in one launch: columns of x, columns of dy, rows of dy; none of a kind: no workgroups.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void mv_mx_encode_grad_kernel(Encode<T> x_t, uint32_t x_t_groups, Encode<T> dy_t,
+                                                                     uint32_t dy_t_groups, Encode<T> dy)
+{
+    static_assert(kThreads == 64 * kTileBlocks, "one size of workgroup");
+    __shared__ __attribute__((aligned(16))) Columns<T> out;
+    const uint32_t b = blockIdx.x;
+    if (b < x_t_groups) encode_columns<T>(x_t, b, out);
+    else if (b < x_t_groups + dy_t_groups) encode_columns<T>(dy_t, b - x_t_groups, out);
+    else encode_rows<T, false>(dy, b - x_t_groups - dy_t_groups, nullptr, 0);
 }
 
 template <typename T>
@@ -167,15 +208,18 @@ __global__ __launch_bounds__(kThreads) void mv_mx_aggregate_kernel(const uint32_
     store8(agg + at, n - at, sum);
 }
 
-mv_status launch_encode(const void* vals, int32_t dtype, int64_t ld_vals, int64_t rows, int64_t n, uint32_t* codes,
-                        int64_t ld_words, uint8_t* scales, int64_t ld_scales, float* resid, int64_t ld_resid, hipStream_t st)
+template <typename T>
+static Encode<T> encode_of(const Values& v, const Held& to)
 {
-    const int64_t groups = (rows * blocks_of(n) + kThreads / 4 - 1) / (kThreads / 4);
-    if (groups > kMostGroups) return MV_ERR_INVALID_ARG;
-    const dim3 grid((uint32_t)groups), threads(kThreads);
-#define MV_MX_ENCODE(T, R)                                                                                             \
-    hipLaunchKernelGGL((mv_mx_encode_kernel<T, R>), grid, threads, 0, st, static_cast<const T*>(vals), ld_vals, rows,  \
-                       n, codes, ld_words, scales, ld_scales, resid, ld_resid)
+    return {static_cast<const T*>(v.p), v.ld, v.rows, v.n, to.codes, to.ld_words, to.scales, to.ld_scales};
+}
+static int64_t row_groups(const Values& v) { return (v.rows * blocks_of(v.n) + kThreads / 4 - 1) / (kThreads / 4); }
+
+mv_status launch_encode(const Values& v, int32_t dtype, const Held& to, float* resid, int64_t ld_resid, hipStream_t st)
+{
+    if (row_groups(v) > kMostGroups) return MV_ERR_INVALID_ARG;
+    const dim3 grid((uint32_t)row_groups(v)), threads(kThreads);
+#define MV_MX_ENCODE(T, R) hipLaunchKernelGGL((mv_mx_encode_kernel<T, R>), grid, threads, 0, st, encode_of<T>(v, to), resid, ld_resid)
     if (dtype == MV_BF16) {
         if (resid) MV_MX_ENCODE(uint16_t, true);
         else MV_MX_ENCODE(uint16_t, false);
@@ -187,20 +231,36 @@ mv_status launch_encode(const void* vals, int32_t dtype, int64_t ld_vals, int64_
     return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
 }
 
-mv_status launch_encode_t(const void* vals, int32_t dtype, int64_t ld_vals, int64_t rows, int64_t n, uint32_t* codes,
-                          int64_t ld_words, uint8_t* scales, int64_t ld_scales, hipStream_t st)
+template <typename T>
+static mv_status launch_encode_t_of(const Values& v, const Held& to, hipStream_t st)
 {
-    const int64_t cols = dtype == MV_BF16 ? 16 * kLaneCols<uint16_t> : 16 * kLaneCols<float>;
-    const int64_t tiles = (n + cols - 1) / cols, strips = (blocks_of(rows) + kTileBlocks - 1) / kTileBlocks;
-    if (tiles * strips > kMostGroups) return MV_ERR_INVALID_ARG;
-    const dim3 grid((uint32_t)(tiles * strips)), threads(64 * kTileBlocks);
-    if (dtype == MV_BF16)
-        hipLaunchKernelGGL(mv_mx_encode_t_kernel<uint16_t>, grid, threads, 0, st, static_cast<const uint16_t*>(vals), ld_vals,
-                           rows, n, tiles, codes, ld_words, scales, ld_scales);
-    else
-        hipLaunchKernelGGL(mv_mx_encode_t_kernel<float>, grid, threads, 0, st, static_cast<const float*>(vals), ld_vals, rows,
-                           n, tiles, codes, ld_words, scales, ld_scales);
+    const int64_t groups = column_groups<T>(v.rows, v.n);
+    if (groups > kMostGroups) return MV_ERR_INVALID_ARG;
+    hipLaunchKernelGGL(mv_mx_encode_t_kernel<T>, dim3((uint32_t)groups), dim3(64 * kTileBlocks), 0, st, encode_of<T>(v, to));
     return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
+}
+mv_status launch_encode_t(const Values& v, int32_t dtype, const Held& to, hipStream_t st)
+{
+    return dtype == MV_BF16 ? launch_encode_t_of<uint16_t>(v, to, st) : launch_encode_t_of<float>(v, to, st);
+}
+
+template <typename T>
+static mv_status launch_encode_grad_of(const Values& x, const Held* x_t, const Values& dy, const Held* dy_t, const Held* dy_r, hipStream_t st)
+{
+    const int64_t a = x_t ? column_groups<T>(x.rows, x.n) : 0, b = dy_t ? column_groups<T>(dy.rows, dy.n) : 0;
+    const int64_t c = dy_r ? row_groups(dy) : 0;
+    if (a + b + c > kMostGroups) return MV_ERR_INVALID_ARG;
+    const Encode<T> none = {};
+    hipLaunchKernelGGL(mv_mx_encode_grad_kernel<T>, dim3((uint32_t)(a + b + c)), dim3(kThreads), 0, st,
+                       x_t ? encode_of<T>(x, *x_t) : none, (uint32_t)a, dy_t ? encode_of<T>(dy, *dy_t) : none, (uint32_t)b,
+                       dy_r ? encode_of<T>(dy, *dy_r) : none);
+    return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
+}
+mv_status launch_encode_grad(const Values& x, const Held* x_t, const Values& dy, const Held* dy_t, const Held* dy_r, int32_t dtype,
+                             hipStream_t st)
+{
+    return dtype == MV_BF16 ? launch_encode_grad_of<uint16_t>(x, x_t, dy, dy_t, dy_r, st)
+                            : launch_encode_grad_of<float>(x, x_t, dy, dy_t, dy_r, st);
 }
 
 }  // namespace mvx
@@ -219,7 +279,7 @@ mv_status mv_mx_encode(const void* vals, int32_t dtype, int64_t ld_vals, int64_t
         return MV_ERR_INVALID_ARG;
     if (resid && (!values_valid(resid, MV_F32, ld_resid, n) || (vals == resid && (dtype != MV_F32 || ld_vals != ld_resid))))
         return MV_ERR_INVALID_ARG;
-    return launch_encode(vals, dtype, ld_vals, rows, n, codes, ld_words, scales, ld_scales, resid, ld_resid,
+    return launch_encode({vals, ld_vals, rows, n}, dtype, {codes, scales, ld_words, ld_scales, rows}, resid, ld_resid,
                          static_cast<hipStream_t>(stream));
 }
 
@@ -230,7 +290,7 @@ mv_status mv_mx_encode_t(const void* vals, int32_t dtype, int64_t ld_vals, int64
     if (!size_valid(rows) || !size_valid(n) || !values_valid(vals, dtype, ld_vals, n) ||
         !codes_valid(codes, ld_words, scales, ld_scales, rows))
         return MV_ERR_INVALID_ARG;
-    return launch_encode_t(vals, dtype, ld_vals, rows, n, codes, ld_words, scales, ld_scales, static_cast<hipStream_t>(stream));
+    return launch_encode_t({vals, ld_vals, rows, n}, dtype, {codes, scales, ld_words, ld_scales, n}, static_cast<hipStream_t>(stream));
 }
 
 mv_status mv_mx_decode(const uint32_t* codes, int64_t ld_words, const uint8_t* scales, int64_t ld_scales, int64_t rows,

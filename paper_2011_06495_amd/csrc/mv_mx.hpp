@@ -24,12 +24,7 @@ __host__ __device__ constexpr int64_t blocks_of(int64_t n) { return (n + kBlock 
 __device__ __forceinline__ float widen(uint32_t b) { return __uint_as_float(b << 16); }
 
 // To the nearest bf16, ties to even; NaN stays NaN.
-__device__ __forceinline__ uint32_t narrow(float x)
-{
-    const uint32_t u = __float_as_uint(x);
-    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return (u >> 16) | 0x40u;
-    return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
-}
+__device__ __forceinline__ uint32_t narrow(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
 // Values [0, 8) of p, those at `live` and behind as zeros.
 __device__ __forceinline__ void load8(const float* p, int64_t live, float (&x)[8])
@@ -159,10 +154,20 @@ inline bool values_valid(const void* p, int32_t dtype, int64_t ld, int64_t n)
     return p && dtype_valid(dtype) && (reinterpret_cast<uintptr_t>(p) & (dtype == MV_BF16 ? 1 : 3)) == 0 && ld >= n;
 }
 
-// Rows of vals to codes, in mv_mx.hip; arguments checked by the caller.
-mv_status launch_encode(const void* vals, int32_t dtype, int64_t ld_vals, int64_t rows, int64_t n, uint32_t* codes,
-                        int64_t ld_words, uint8_t* scales, int64_t ld_scales, float* resid, int64_t ld_resid, hipStream_t st);
-mv_status launch_encode_t(const void* vals, int32_t dtype, int64_t ld_vals, int64_t rows, int64_t n, uint32_t* codes,
-                          int64_t ld_words, uint8_t* scales, int64_t ld_scales, hipStream_t st);
+// A matrix of values, and codes that are written.
+struct Values {
+    const void* p;
+    int64_t     ld, rows, n;
+};
+struct Held {
+    uint32_t* codes;
+    uint8_t*  scales;
+    int64_t   ld_words, ld_scales, rows;
+};
+// In mv_mx.hip; arguments checked by the caller.  The last one: columns of x and of dy and rows of dy, where asked for.
+mv_status launch_encode(const Values& v, int32_t dtype, const Held& to, float* resid, int64_t ld_resid, hipStream_t st);
+mv_status launch_encode_t(const Values& v, int32_t dtype, const Held& to, hipStream_t st);
+mv_status launch_encode_grad(const Values& x, const Held* x_t, const Values& dy, const Held* dy_t, const Held* dy_r, int32_t dtype,
+                             hipStream_t st);
 
 }  // namespace mvx

@@ -48,39 +48,40 @@ __device__ __forceinline__ void load_four(const Factor& f, int64_t row, int64_t 
     v.scales = w;
 }
 
-// Four consecutive results of a row of which `live` are left.
-typedef uint16_t u16x4u __attribute__((ext_vector_type(4), aligned(2)));
-__device__ __forceinline__ void store4(float* p, int64_t live, const f32x4& v)
-{
-    if (live >= 4) {
-        *reinterpret_cast<f32x4u*>(p) = v;
-    } else {
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (e < live) p[e] = v[e];
+// Where results go: fp32 or bf16, rounded once.
+struct Out {
+    void*    p;
+    uint32_t bf16;
+    __device__ __forceinline__ void put(int64_t at, float x) const
+    {
+        if (bf16) static_cast<uint16_t*>(p)[at] = (uint16_t)narrow(x);
+        else static_cast<float*>(p)[at] = x;
     }
-}
-__device__ __forceinline__ void store4(uint16_t* p, int64_t live, const f32x4& v)
-{
-    const u16x4u w = {(uint16_t)narrow(v.x), (uint16_t)narrow(v.y), (uint16_t)narrow(v.z), (uint16_t)narrow(v.w)};
-    if (live >= 4) {
-        *reinterpret_cast<u16x4u*>(p) = w;
-    } else {
+    // four consecutive ones of which `live` are left
+    __device__ __forceinline__ void put4(int64_t at, int64_t live, const f32x4& v) const
+    {
+        typedef uint16_t u16x4u __attribute__((ext_vector_type(4), aligned(2)));
+        if (live >= 4) {
+            if (bf16)
+                *reinterpret_cast<u16x4u*>(static_cast<uint16_t*>(p) + at) =
+                    u16x4u{(uint16_t)narrow(v.x), (uint16_t)narrow(v.y), (uint16_t)narrow(v.z), (uint16_t)narrow(v.w)};
+            else
+                *reinterpret_cast<f32x4u*>(static_cast<float*>(p) + at) = v;
+        } else {
 #pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (e < live) p[e] = w[e];
+            for (int e = 0; e < 3; ++e)
+                if (e < live) put(at + e, v[e]);
+        }
     }
-}
+};
 
-__device__ __forceinline__ void put(float* p, float x) { *p = x; }
-__device__ __forceinline__ void put(uint16_t* p, float x) { *p = (uint16_t)narrow(x); }
+inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 constexpr int kTile = 64;           // rows of each factor that a wavefront takes
 constexpr int kProductThreads = 256;
 
-template <typename T>
-__global__ __launch_bounds__(kProductThreads) void mv_mx_product_kernel(Factor a, Factor b, int64_t blocks, int64_t tiles_n,
-                                                                        T* __restrict__ c, int64_t ld_c)
+__global__ __launch_bounds__(kProductThreads) void mv_mx_product_kernel(Factor a, Factor b, int64_t blocks, int64_t tiles_n, Out c,
+                                                                        int64_t ld_c)
 {
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x / 64, in = lane & 15u, group = lane / 16;
     const int64_t i0 = (int64_t)blockIdx.x / tiles_n * (2 * kTile) + wave / 2 * kTile;
@@ -112,7 +113,7 @@ __global__ __launch_bounds__(kProductThreads) void mv_mx_product_kernel(Factor a
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int64_t j = j0 + 16 * u + 4 * group;
-            store4(c + i * ld_c + j, b.rows - j, acc[t][u]);
+            c.put4(i * ld_c + j, b.rows - j, acc[t][u]);
         }
     }
 }
@@ -143,6 +144,15 @@ __device__ __forceinline__ f32x16 mfma32(const u32x4& a, uint32_t a_scale, const
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, S, (int)a_scale, S, (int)b_scale);
 }
 
+// One product and how it is cut: tiles_m x tiles_n tiles, `splits` runs of steps_each steps each.  With several splits c is
+// fp32 and holds their sums one after the other, split_c apart.
+struct Product {
+    Factor   a, b;
+    uint32_t blocks, tiles_m, tiles_n, steps_each, splits;
+    Out      c;
+    int64_t  ld_c, split_c;
+};
+
 // Which tile a workgroup takes: consecutive workgroups run on eight dies with an L2 of their own, so a die gets a run of
 // consecutive tiles, and those go down eight tiles of a before they go along b.
 __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn)
@@ -160,10 +170,9 @@ struct Rows {
     u32x4 x[MT], y[NT];
 };
 
-template <int MT, int NT, int WM, int WN, typename T>
-__global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Factor a, Factor b, uint32_t blocks, uint32_t tiles_m,
-                                                                             uint32_t tiles_n, uint32_t steps_each,
-                                                                             T* __restrict__ c, int64_t ld_c, int64_t split_c)
+// Two products in one launch, the first workgroups take the first one's tiles.
+template <int MT, int NT, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Product first, Product second, uint32_t firsts)
 {
     constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
     constexpr int kM = 32 * MT * WM, kN = 32 * NT * WN, kRows = kM + kN;
@@ -172,11 +181,16 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Fac
     __shared__ __attribute__((aligned(1024))) Codes even, odd;
     __shared__ uint8_t scales[2][kRows * kScalePitch];
     const uint32_t t = threadIdx.x, lane = t & 63u, wave = __builtin_amdgcn_readfirstlane(t / 64);
+    const bool is_first = blockIdx.x < firsts;
+    const Product& p = is_first ? first : second;
+    const Factor a = p.a, b = p.b;
+    const uint32_t blocks = p.blocks, steps_each = p.steps_each, id = is_first ? blockIdx.x : blockIdx.x - firsts;
+    const uint32_t split = id / (p.tiles_m * p.tiles_n);
     uint32_t tm, tn;
-    tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
+    tile_of(id - split * (p.tiles_m * p.tiles_n), p.tiles_m, p.tiles_n, tm, tn);
     const int64_t i0 = (int64_t)tm * kM, j0 = (int64_t)tn * kN;
     const uint32_t steps = (blocks + kStepBlocks - 1) / kStepBlocks;
-    const uint32_t step0 = blockIdx.y * steps_each, count = min(steps_each, steps - step0);       // at least one
+    const uint32_t step0 = split * steps_each, count = min(steps_each, steps - step0);       // at least one
     const uint32_t end = min(blocks, (step0 + count) * kStepBlocks);       // an odd count's last step is one of zeros
 
     // what this wavefront loads: rows [wave kM / kWaves, ...) of a and as many of b, eight rows an instruction
@@ -206,35 +220,25 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Fac
                 b_buf, (__attribute__((address_space(3))) void*)(to + (kM + wave * (kN / kWaves) + i * 8) * 128), 16,
                 bv + i * 8 * b_pitch, 0, 0, 0);
     };
-    // the scales' rows
-    constexpr int kScaleRows = (kRows + kThreads - 1) / kThreads;
-    const uint8_t* scale_row[kScaleRows];
-#pragma unroll
-    for (int i = 0; i < kScaleRows; ++i) {
-        const uint32_t r = t + kThreads * i;
-        const int64_t at = r < kM ? i0 + r : j0 + (r - kM);
-        scale_row[i] = r < kM ? a.scales + (at < a.rows ? at : a.rows - 1) * a.ld_scales
-                              : b.scales + (at < b.rows ? at : b.rows - 1) * b.ld_scales;
-    }
-    const uint32_t last_word = (end - 1) / 4 * 4;
-    uint32_t next[kScaleRows][4];
+    // A thread has one row's scales, of a the first wavefronts, of b the others: one load for two steps, which reads zeros
+    // where the rows end, and the next row's behind a row's last block.
+    static_assert(kThreads == kRows, "a row a thread");
+    const bool of_a = wave < kM / 64;
+    const uint32_t sc_pitch = (uint32_t)(of_a ? a.ld_scales : b.ld_scales), sc_rows = (uint32_t)(of_a ? a_rows : b_rows);
+    const __amdgpu_buffer_rsrc_t sc_buf = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(of_a ? a.scales + i0 * a.ld_scales : b.scales + j0 * b.ld_scales), 0,
+        (int)((sc_rows - 1) * sc_pitch + (blocks + 3) / 4 * 4), 0x00020000);
+    const uint32_t sc_at = (t - (of_a ? 0u : (uint32_t)kM)) * sc_pitch;
+    u32x4 next;
     auto fetch_scales = [&](uint32_t k) {
-#pragma unroll
-        for (int i = 0; i < kScaleRows; ++i)
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-                next[i][w] = *reinterpret_cast<const uint32_t*>(scale_row[i] + min((step0 + k) * kStepBlocks + 4 * w, last_word));
+        next = __builtin_amdgcn_raw_buffer_load_b128(sc_buf, sc_at + (step0 + k) * kStepBlocks, 0, 0);
     };
     auto keep_scales = [&](uint32_t pair) {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const int live = (int)end - (int)((step0 + 2 * pair) * kStepBlocks + 4 * w);
             const uint32_t real = live >= 4 ? 0xFFFFFFFFu : live > 0 ? (1u << (8 * live)) - 1u : 0u;
-#pragma unroll
-            for (int i = 0; i < kScaleRows; ++i)
-                if (kRows % kThreads == 0 || t + kThreads * i < kRows)
-                    *reinterpret_cast<uint32_t*>(&scales[pair & 1u][(t + kThreads * i) * kScalePitch + 4 * w]) =
-                        (next[i][w] & real) | (0x7F7F7F7Fu & ~real);
+            *reinterpret_cast<uint32_t*>(&scales[pair & 1u][t * kScalePitch + 4 * w]) = (next[w] & real) | (0x7F7F7F7Fu & ~real);
         }
     };
 
@@ -321,42 +325,50 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Fac
     __builtin_amdgcn_s_waitcnt(kNoLoads);
 
     // a lane has, of row i, four times four consecutive columns
-    T* out = c + blockIdx.y * split_c;
-    const int64_t col0 = j0 + wave % WN * (32 * NT) + 4 * half;
+    const int64_t col0 = j0 + wave % WN * (32 * NT) + 4 * half, out = split * p.split_c + col0;
     const bool whole = j0 + kN <= b.rows;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const int64_t row = i0 + a_row + 32 * i;
         if (row >= a.rows) continue;
-        T* to = out + row * ld_c + col0;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                if (whole) store4(to + 32 * j + 8 * q, 4, v);
-                else store4(to + 32 * j + 8 * q, b.rows - (col0 + 32 * j + 8 * q), v);
+                p.c.put4(out + row * p.ld_c + 32 * j + 8 * q, whole ? 4 : b.rows - (col0 + 32 * j + 8 * q), v);
             }
     }
 }
 
-// c = the sum of the splits, in their order.
-template <typename T>
-__global__ __launch_bounds__(256) void mv_mx_product_join_kernel(const float* __restrict__ parts, int splits, int64_t m, int64_t n,
-                                                                 int64_t split_c, int64_t quads, T* __restrict__ c, int64_t ld_c)
+// c = the sum of the splits: a group of `lanes` threads takes four results, each thread every lanes-th split, and their
+// sums are added in order.
+__global__ __launch_bounds__(256) void mv_mx_product_join_kernel(const float* __restrict__ parts, uint32_t splits, uint32_t lanes,
+                                                                 int64_t m, int64_t n, int64_t split_c, int64_t quads, Out c,
+                                                                 int64_t ld_c)
 {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    __shared__ f32x4 sums[256];
+    const uint32_t per = 256 / lanes, lane = threadIdx.x / per;          // a group's threads lie `per` apart
+    const int64_t at = (int64_t)blockIdx.x * per + threadIdx.x % per;
     const int64_t i = at / quads, j = at % quads * 4;
-    if (i >= m) return;
-    const float* p = parts + i * (quads * 4) + j;
-    f32x4 sum = *reinterpret_cast<const f32x4*>(p);
-    for (int s = 1; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(p + s * split_c);
-    store4(c + i * ld_c + j, n - j, sum);
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (i < m) {
+        const float* p = parts + i * (quads * 4) + j;
+#pragma unroll 4
+        for (uint32_t s = lane; s < splits; s += lanes) sum += *reinterpret_cast<const f32x4*>(p + s * split_c);
+    }
+    if (lanes > 1) {                                                     // uniform
+        sums[threadIdx.x] = sum;
+        __syncthreads();
+        if (lane) return;
+        for (uint32_t l = 1; l < lanes; ++l) sum += sums[l * per + threadIdx.x];
+    }
+    if (i < m) c.put4(i * ld_c + j, n - j, sum);
 }
 
 // ---- few rows of one factor ------------------------------------------------------------------------------------------
 //
-// Up to 16 rows of one factor ("few") against many of the other ("many"), whose codes are the bytes to read.  A workgroup
+// Up to 16 rows of one factor ("few"; up to 64 where they are values) against many of the other ("many"), whose codes are the bytes to read.  A workgroup
 // takes 16 NT of the many rows and all of k, its wavefronts turns of 16 blocks; what they have is added up through LDS in
 // the wavefronts' order.  Lane l of an instruction holds row l % 16 and block 4 s + l / 16 of the turn, s = 0 .. 3: the
 // four lanes of a row read 64 bytes in a row; the scales of a lane's four blocks are picked from the row's 16.
@@ -460,13 +472,29 @@ __host__ __device__ constexpr uint32_t few_bytes(uint32_t count, uint32_t turns,
 }
 
 // c[many][few] or c[few][many]: element (j, i) lies at j * step_many + i * step_few.
-template <int NT, typename X, typename T>
-__global__ __launch_bounds__(64 * kFewWaves) void mv_mx_product_few_kernel(Factor many, Few<X> few, uint32_t blocks, int64_t k,
-                                                                           T* __restrict__ c, int64_t step_many, int64_t step_few)
+template <typename X>
+struct FewProduct {
+    Factor   many;
+    Few<X>   few;
+    uint32_t blocks;
+    int64_t  k;
+    Out      c;
+    int64_t  step_many, step_few;
+};
+
+// Two products in one launch, the first workgroups take the first one's.  A workgroup: 16 MT few rows, 16 NT of the many.
+template <int MT, int NT, typename X>
+__global__ __launch_bounds__(64 * kFewWaves) void mv_mx_product_few_kernel(FewProduct<X> first, FewProduct<X> second, uint32_t firsts)
 {
+    const bool is_first = blockIdx.x < firsts;
+    const FewProduct<X>& p = is_first ? first : second;
+    const uint32_t id = is_first ? blockIdx.x : blockIdx.x - firsts;
+    const Factor many = p.many;
+    const Few<X> few = p.few;
+    const uint32_t blocks = p.blocks;
+    const int64_t k = p.k, j0 = (int64_t)id * (16 * NT);
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
     const uint32_t in = lane & 15u, g = lane / 16;
-    const int64_t j0 = (int64_t)blockIdx.x * (16 * NT);
     extern __shared__ __attribute__((aligned(16))) uint8_t held[];
     const uint32_t turns = (blocks + kTurn - 1) / kTurn, row_blocks = turns * kTurn, pitch = few_pitch(turns);
     uint8_t* held_scales = held + few.count * pitch;
@@ -521,21 +549,26 @@ __global__ __launch_bounds__(64 * kFewWaves) void mv_mx_product_few_kernel(Facto
         hold(at);
     }
     __syncthreads();
-    f32x4 acc[NT] = {};
-    const uint32_t few_row = min(in, few.count - 1);
+    f32x4 acc[MT][NT] = {};
     while (block < blocks) {
-        u32x4 x[4];
+        uint32_t ws[NT];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) x[s] = *reinterpret_cast<const u32x4*>(held + few_row * pitch + (block + 4 * s + g) * 16);
-        const uint32_t xs = *reinterpret_cast<const uint32_t*>(held_scales + few_row * row_blocks + block + 4 * g);
+        for (int t = 0; t < NT; ++t)
+            ws[t] = pick_scales(*reinterpret_cast<const u32x4*>(many_scales + (16 * t + in) * many_pitch(turns) + block), g);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const uint32_t ws =
-                pick_scales(*reinterpret_cast<const u32x4*>(many_scales + (16 * t + in) * many_pitch(turns) + block), g);
-            acc[t] = mfma<0>(codes[t][0], ws, x[0], xs, acc[t]);
-            acc[t] = mfma<1>(codes[t][1], ws, x[1], xs, acc[t]);
-            acc[t] = mfma<2>(codes[t][2], ws, x[2], xs, acc[t]);
-            acc[t] = mfma<3>(codes[t][3], ws, x[3], xs, acc[t]);
+        for (int i = 0; i < MT; ++i) {
+            const uint32_t row = min(16 * i + in, few.count - 1);
+            u32x4 x[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) x[s] = *reinterpret_cast<const u32x4*>(held + row * pitch + (block + 4 * s + g) * 16);
+            const uint32_t xs = *reinterpret_cast<const uint32_t*>(held_scales + row * row_blocks + block + 4 * g);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                acc[i][t] = mfma<0>(codes[t][0], ws[t], x[0], xs, acc[i][t]);
+                acc[i][t] = mfma<1>(codes[t][1], ws[t], x[1], xs, acc[i][t]);
+                acc[i][t] = mfma<2>(codes[t][2], ws[t], x[2], xs, acc[i][t]);
+                acc[i][t] = mfma<3>(codes[t][3], ws[t], x[3], xs, acc[i][t]);
+            }
         }
         block += waves * kTurn;
         if (block < blocks) load(block);
@@ -543,155 +576,233 @@ __global__ __launch_bounds__(64 * kFewWaves) void mv_mx_product_few_kernel(Facto
     __syncthreads();
     f32x4* sums = reinterpret_cast<f32x4*>(held);                         // wavefront, tile, lane
 #pragma unroll
-    for (int t = 0; t < NT; ++t) sums[(wave * NT + t) * 64 + lane] = acc[t];
-    __syncthreads();
-    for (uint32_t at = threadIdx.x; at < NT * 64; at += blockDim.x) {
-        f32x4 v = sums[at];
-        for (uint32_t w = 1; w < waves; ++w) v += sums[w * NT * 64 + at];
-        const uint32_t i = at & 15u;
-        const int64_t j = j0 + at / 64 * 16 + (at >> 4 & 3u) * 4;
-        if (i >= few.count) continue;
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (j + e < many.rows) put(c + (j + e) * step_many + i * step_few, v[e]);
+        for (int t = 0; t < NT; ++t) sums[((wave * MT + i) * NT + t) * 64 + lane] = acc[i][t];
+    __syncthreads();
+    for (uint32_t at = threadIdx.x; at < MT * NT * 64; at += blockDim.x) {
+        f32x4 v = sums[at];
+        for (uint32_t w = 1; w < waves; ++w) v += sums[w * MT * NT * 64 + at];
+        const uint32_t i = at / (64 * NT) * 16 + (at & 15u);
+        const int64_t j = j0 + at / 64 % NT * 16 + (at >> 4 & 3u) * 4, to = j * p.step_many + i * p.step_few;
+        if (i >= few.count) continue;
+        if (p.step_many == 1) {
+            if (j < many.rows) p.c.put4(to, many.rows - j, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (j + e < many.rows) p.c.put(to + e * p.step_many, v[e]);
+        }
     }
 }
 
-// How a product is cut: tiles of 64 `mt` rows of each factor (0: the kernel without LDS), and the steps of k over `splits`.
+constexpr int64_t  kFewRows = 16, kFewValues = 64;
+constexpr uint32_t kFewLds = 144 * 1024;
+
+// Whether and how the kernel for few rows takes a product.  Up to 16 rows it always is the faster one.  Up to 64 rows of
+// values it saves the launch that quantises them, as long as each unit quantises them once: bf16, 64 rows with 4096 x 2048
+// 11.0 us (two launches 12.1), 4096 x 1024 7.7 (8.9), 1000 x 2048 10.2 (11.3), 400 x 470 8.6 (8.5), 20 rows 5.4 (7.5); but
+// 16,000 x 256, a thousand workgroups, 16.8 (7.9), and 200 rows in four tiles with 1000 x 1000 11.6 (9.2).
+struct FewCut {
+    int      mt, nt;                // 0: it does not
+    uint32_t groups, lds, waves;
+};
+static FewCut few_cut(int64_t few, int64_t many, int64_t k, bool values)
+{
+    if (few > (values ? kFewValues : kFewRows)) return FewCut{};
+    const int64_t turns = (blocks_of(k) + kTurn - 1) / kTurn;
+    FewCut c = {};
+    c.mt = few <= 16 ? 1 : few <= 32 ? 2 : 4;
+    // Workgroups of 16 rows as long as all of them run at once, three to a unit; beyond that 32 rows, which share what a
+    // workgroup spends on the few rows.  Four bf16 rows against 8192 x 8192: 13.0 us with 16 and 13.4 with 32; 12,000 x
+    // 8192 15.9 and 17.5; 14,000 x 8192 19.5 and 18.0; 16,384 x 6000 18.8 and 14.7; 16,384 x 8192 28 and 19.9.
+    c.nt = c.mt == 1 && many > 12288 ? 2 : 1;
+    const int64_t groups = (many + 16 * c.nt - 1) / (16 * c.nt);
+    if (turns >= 4096 || groups > kMostGroups / 4) return FewCut{};
+    c.groups = (uint32_t)groups;
+    // a wavefront for each turn, or for each 64 blocks of the few rows
+    const int64_t waves = few > 4 ? few * turns / 4 + 1 : turns;
+    c.waves = (uint32_t)(waves < kFewWaves ? waves : kFewWaves);
+    const uint32_t sums = c.waves * c.mt * c.nt * 1024;
+    c.lds = few_bytes((uint32_t)few, (uint32_t)turns, 16u * c.nt);
+    if (c.lds < sums) c.lds = sums;
+    if (few <= kFewRows ? (many < 512 && k > 8192) || c.lds > kFewLds : c.groups > 256 || c.lds > kFewLds) return FewCut{};
+    return c;
+}
+
+template <typename X>
+static FewProduct<X> few_product(const Factor& many, const Few<X>& few, int64_t k, const Out& c, int64_t step_many,
+                                 int64_t step_few)
+{
+    return {many, few, (uint32_t)blocks_of(k), k, c, step_many, step_few};
+}
+template <int MT, int NT, typename X>
+static void launch_few_of(const FewProduct<X>& p, const FewCut& cut, const FewProduct<X>& q, const FewCut& cut2, hipStream_t st)
+{
+    hipLaunchKernelGGL((mv_mx_product_few_kernel<MT, NT, X>), dim3(cut.groups + cut2.groups),
+                       dim3(64 * (cut.waves > cut2.waves ? cut.waves : cut2.waves)), cut.lds > cut2.lds ? cut.lds : cut2.lds, st, p, q,
+                       cut.groups);
+}
+// Up to two products; the second's cut has the first's mt and nt, or no groups.
+template <typename X>
+static mv_status launch_few(const FewProduct<X>& p, const FewCut& cut, const FewProduct<X>& q, const FewCut& cut2, hipStream_t st)
+{
+    if (cut.nt == 2) launch_few_of<1, 2>(p, cut, q, cut2, st);
+    else if (cut.mt == 1) launch_few_of<1, 1>(p, cut, q, cut2, st);
+    else if constexpr (!std::is_same_v<X, uint32_t>) {                   // codes: up to 16 rows only
+        if (cut.mt == 2) launch_few_of<2, 1>(p, cut, q, cut2, st);
+        else launch_few_of<4, 1>(p, cut, q, cut2, st);
+    }
+    return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
+}
+
+// How a product is cut for the kernel with tiles of 64 mt rows of each factor.
 struct Cut {
     int      mt;
     int64_t  tiles_m, tiles_n;
     uint32_t splits, steps_each;
+    int64_t  groups() const { return tiles_m * tiles_n * splits; }
 };
-static Cut cut_of(int64_t m, int64_t n, int64_t k)
+static Cut cut_of(int64_t m, int64_t n, int64_t k, int mt)
 {
-    auto tiles = [](int64_t rows, int mt) { return (rows + 64 * mt - 1) / (64 * mt); };
-    Cut c = {4, tiles(m, 4), tiles(n, 4), 1, 0};
+    auto tiles = [mt](int64_t rows) { return (rows + 64 * mt - 1) / (64 * mt); };
+    Cut c = {mt, tiles(m), tiles(n), 1, 0};
     const int64_t steps = (blocks_of(k) + kStepBlocks - 1) / kStepBlocks;
-    if (c.tiles_m * c.tiles_n < 192) {
-        c = {2, tiles(m, 2), tiles(n, 2), 1, 0};
-        const int64_t most = 512 / (c.tiles_m * c.tiles_n);
-        int64_t splits = most < steps / 4 ? most : steps / 4;
-        if (splits > 16) splits = 16;
+    if (mt == 2) {
+        int64_t splits = 512 / (c.tiles_m * c.tiles_n);
+        if (splits > steps / 4) splits = steps / 4;
+        // many splits only of small results: all of them are written and read again
+        if (splits > 16 && splits * m * n > (4 << 20)) splits = 16;
         if (splits > 1) c.splits = (uint32_t)splits;
     }
     c.steps_each = (uint32_t)((steps + c.splits - 1) / c.splits);
     c.splits = (uint32_t)((steps + c.steps_each - 1) / c.steps_each);
     return c;
 }
+static bool large(int64_t m, int64_t n) { return ((m + 255) / 256) * ((n + 255) / 256) >= 192; }
 inline int64_t quads_of(int64_t n) { return (n + 3) / 4; }
 inline size_t parts_bytes(int64_t m, int64_t n, int64_t k)
 {
-    const Cut c = cut_of(m, n, k);
-    return c.splits > 1 ? (size_t)c.splits * (size_t)m * (size_t)quads_of(n) * 16 : 0;
+    const uint32_t splits = cut_of(m, n, k, 2).splits;
+    return splits > 1 ? up256((size_t)splits * (size_t)m * (size_t)quads_of(n) * 16) : 0;
 }
 
-template <typename T>
-static mv_status launch_product_of(const Factor& a, const Factor& b, int64_t k, T* c, int64_t ld_c, float* parts, hipStream_t st)
+// A product that is asked for: c = a b^T, m rows and n rows of k values.
+struct Wanted {
+    Factor  a, b;
+    int64_t k;
+    Out     c;
+    int64_t ld_c;
+    void*   parts;                  // room for parts_bytes
+};
+static Product product_of(const Wanted& w, const Cut& cut)
 {
-    const Cut cut = cut_of(a.rows, b.rows, k);
-    const dim3 threads(256);
-    if (cut.tiles_m * cut.tiles_n * cut.splits > kMostGroups) return MV_ERR_INVALID_ARG;
-    const dim3 grid((uint32_t)(cut.tiles_m * cut.tiles_n), cut.splits);
-    const uint32_t blocks = (uint32_t)blocks_of(k), tm = (uint32_t)cut.tiles_m, tn = (uint32_t)cut.tiles_n;
-    if (cut.mt == 4) {
-        hipLaunchKernelGGL((mv_mx_product_tile_kernel<4, 2, 2, 4, T>), grid, dim3(512), 0, st, a, b, blocks, tm, tn, cut.steps_each, c, ld_c, 0);
-    } else if (cut.splits == 1) {
-        hipLaunchKernelGGL((mv_mx_product_tile_kernel<2, 2, 2, 2, T>), grid, threads, 0, st, a, b, blocks, tm, tn, cut.steps_each, c, ld_c, 0);
-    } else {
-        const int64_t quads = quads_of(b.rows), split_c = a.rows * quads * 4;
-        hipLaunchKernelGGL((mv_mx_product_tile_kernel<2, 2, 2, 2, float>), grid, threads, 0, st, a, b, blocks, tm, tn, cut.steps_each, parts,
-                           quads * 4, split_c);
-        hipLaunchKernelGGL(mv_mx_product_join_kernel<T>, dim3((uint32_t)((a.rows * quads + 255) / 256)), threads, 0, st, parts,
-                           (int)cut.splits, a.rows, b.rows, split_c, quads, c, ld_c);
-    }
+    const int64_t quads = quads_of(w.b.rows);
+    const bool split = cut.splits > 1;
+    return {w.a, w.b, (uint32_t)blocks_of(w.k), (uint32_t)cut.tiles_m, (uint32_t)cut.tiles_n, cut.steps_each, cut.splits,
+            split ? Out{w.parts, 0} : w.c, split ? quads * 4 : w.ld_c, w.a.rows * quads * 4};
+}
+static void launch_join(const Wanted& w, const Cut& cut, hipStream_t st)
+{
+    if (cut.splits == 1) return;
+    const int64_t quads = quads_of(w.b.rows), all = w.a.rows * quads;
+    const uint32_t lanes = cut.splits > 16 ? 16 : 1, per = 256 / lanes;
+    hipLaunchKernelGGL(mv_mx_product_join_kernel, dim3((uint32_t)((all + per - 1) / per)), dim3(256), 0, st,
+                       static_cast<const float*>(w.parts), cut.splits, lanes, w.a.rows, w.b.rows, all * 4, quads, w.c, w.ld_c);
+}
+// The kernel without LDS, for rows so long that a tile's byte offsets leave 32 bits.
+static mv_status launch_plain(const Wanted& w, hipStream_t st)
+{
+    const int64_t tiles_m = (w.a.rows + 2 * kTile - 1) / (2 * kTile), tiles_n = (w.b.rows + 2 * kTile - 1) / (2 * kTile);
+    if (tiles_m * tiles_n > kMostGroups) return MV_ERR_INVALID_ARG;
+    hipLaunchKernelGGL(mv_mx_product_kernel, dim3((uint32_t)(tiles_m * tiles_n)), dim3(kProductThreads), 0, st, w.a, w.b,
+                       blocks_of(w.k), tiles_n, w.c, w.ld_c);
     return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
 }
 
-constexpr int64_t kFewRows = 16;
-constexpr uint32_t kFewLds = 144 * 1024;
-// Workgroups of the kernel for few rows read all of k: so many of its rows, or so short rows, and it is the faster one.
-// Workgroups of 16 rows as long as all of them run at once, three to a unit; beyond that 32 rows, which share what a
-// workgroup spends on the few rows.  Four bf16 rows against 8192 x 8192: 13.0 us with 16 and 13.4 with 32; 12,000 x 8192
-// 15.9 and 17.5; 14,000 x 8192 19.5 and 18.0; 16,384 x 6000 18.8 and 14.7; 16,384 x 8192 28 and 19.9.
-inline int few_tiles(int64_t many) { return many > 12288 ? 2 : 1; }
-inline bool few_fits(int64_t few, int64_t many, int64_t k)
+// The kernel for few rows on codes: which factor's rows are the few ones.
+static FewCut few_codes_cut(const Wanted& w, bool& few_a)
 {
-    const int64_t turns = (blocks_of(k) + kTurn - 1) / kTurn;
-    return few <= kFewRows && (many >= 512 || k <= 8192) && turns < 4096 && few_bytes((uint32_t)few, (uint32_t)turns, 16u * (uint32_t)few_tiles(many)) <= kFewLds;
-}
-
-template <int NT, typename X, typename T>
-static void launch_few_of(const Factor& many, const Few<X>& few, int64_t k, T* c, int64_t step_many, int64_t step_few, hipStream_t st)
-{
-    const uint32_t blocks = (uint32_t)blocks_of(k), turns = (blocks + kTurn - 1) / kTurn;
-    const uint32_t waves = turns < kFewWaves ? turns : kFewWaves;
-    const uint32_t room = few_bytes(few.count, turns, 16 * NT), sums = waves * NT * 1024;
-    hipLaunchKernelGGL((mv_mx_product_few_kernel<NT, X, T>), dim3((uint32_t)((many.rows + 16 * NT - 1) / (16 * NT))),
-                       dim3(64 * waves), room > sums ? room : sums, st, many, few, blocks, k, c, step_many, step_few);
-}
-template <typename X, typename T>
-static mv_status launch_few(const Factor& many, const Few<X>& few, int64_t k, T* c, int64_t step_many, int64_t step_few, hipStream_t st)
-{
-    if (many.rows / 16 > kMostGroups / 2) return MV_ERR_INVALID_ARG;
-    if (few_tiles(many.rows) == 2) launch_few_of<2>(many, few, k, c, step_many, step_few, st);
-    else launch_few_of<1>(many, few, k, c, step_many, step_few, st);
-    return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
-}
-template <typename T>
-static mv_status launch_few_codes(const Factor& a, const Factor& b, int64_t k, T* c, int64_t ld_c, hipStream_t st)
-{
-    if (few_fits(a.rows, b.rows, k))
-        return launch_few(b, Few<uint32_t>{a.codes, a.ld_words, a.scales, a.ld_scales, (uint32_t)a.rows}, k, c, 1, ld_c, st);
-    return launch_few(a, Few<uint32_t>{b.codes, b.ld_words, b.scales, b.ld_scales, (uint32_t)b.rows}, k, c, ld_c, 1, st);
-}
-
-static mv_status launch_product(const Factor& a, const Factor& b, int64_t k, void* c, int32_t c_dtype, int64_t ld_c, void* parts,
-                                hipStream_t st)
-{
-    if (few_fits(a.rows, b.rows, k) || few_fits(b.rows, a.rows, k))
-        return c_dtype == MV_BF16 ? launch_few_codes(a, b, k, static_cast<uint16_t*>(c), ld_c, st)
-                                  : launch_few_codes(a, b, k, static_cast<float*>(c), ld_c, st);
-    // byte offsets inside a tile's rows are 32 bits
-    if (a.ld_words * 4 > (1 << 22) || b.ld_words * 4 > (1 << 22)) {
-        const int64_t tiles_m = (a.rows + 2 * kTile - 1) / (2 * kTile), tiles_n = (b.rows + 2 * kTile - 1) / (2 * kTile);
-        if (tiles_m * tiles_n > kMostGroups) return MV_ERR_INVALID_ARG;
-        const dim3 grid((uint32_t)(tiles_m * tiles_n)), threads(kProductThreads);
-        if (c_dtype == MV_BF16)
-            hipLaunchKernelGGL(mv_mx_product_kernel<uint16_t>, grid, threads, 0, st, a, b, blocks_of(k), tiles_n,
-                               static_cast<uint16_t*>(c), ld_c);
-        else
-            hipLaunchKernelGGL(mv_mx_product_kernel<float>, grid, threads, 0, st, a, b, blocks_of(k), tiles_n, static_cast<float*>(c),
-                               ld_c);
-        return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
+    few_a = w.a.rows <= w.b.rows;
+    FewCut c = few_a ? few_cut(w.a.rows, w.b.rows, w.k, false) : few_cut(w.b.rows, w.a.rows, w.k, false);
+    if (!c.mt) {
+        few_a = !few_a;
+        c = few_a ? few_cut(w.a.rows, w.b.rows, w.k, false) : few_cut(w.b.rows, w.a.rows, w.k, false);
     }
-    return c_dtype == MV_BF16 ? launch_product_of(a, b, k, static_cast<uint16_t*>(c), ld_c, static_cast<float*>(parts), st)
-                              : launch_product_of(a, b, k, static_cast<float*>(c), ld_c, static_cast<float*>(parts), st);
+    return c;
 }
+static FewProduct<uint32_t> few_codes(const Wanted& w, bool few_a)
+{
+    const Factor& few = few_a ? w.a : w.b;
+    return few_product(few_a ? w.b : w.a, Few<uint32_t>{few.codes, few.ld_words, few.scales, few.ld_scales, (uint32_t)few.rows}, w.k, w.c,
+                       few_a ? 1 : w.ld_c, few_a ? w.ld_c : 1);
+}
+static bool offsets_fit(const Wanted& w) { return w.a.ld_words * 4 <= (1 << 22) && w.b.ld_words * 4 <= (1 << 22); }
 
-inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
-inline size_t code_bytes(int64_t rows, int64_t n) { return up256((size_t)rows * (size_t)blocks_of(n) * 16); }
-inline size_t scale_bytes(int64_t rows, int64_t n) { return up256((size_t)rows * (size_t)((blocks_of(n) + 3) / 4 * 4)); }
+// Up to two products (n: how many) in as few launches as their sizes allow.
+static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
+{
+    FewCut few[2] = {};
+    bool few_a[2] = {};
+    for (int i = 0; i < n; ++i) few[i] = few_codes_cut(w[i], few_a[i]);
+    if (n == 2 && few[0].mt && few[0].mt == few[1].mt && few[0].nt == few[1].nt)
+        return launch_few(few_codes(w[0], few_a[0]), few[0], few_codes(w[1], few_a[1]), few[1], st);
+    Cut  cut[2] = {};
+    bool tiled[2] = {};
+    for (int i = 0; i < n; ++i) {
+        tiled[i] = !few[i].mt && offsets_fit(w[i]);
+        if (tiled[i]) {
+            cut[i] = cut_of(w[i].a.rows, w[i].b.rows, w[i].k, large(w[i].a.rows, w[i].b.rows) ? 4 : 2);
+            if (cut[i].groups() > kMostGroups / 2) return MV_ERR_INVALID_ARG;
+        }
+    }
+    const bool both = tiled[0] && tiled[1] && n == 2;
+    if (both && cut[0].mt != cut[1].mt)           // in one launch: the smaller tiles for both
+        for (int i = 0; i < 2; ++i) cut[i] = cut_of(w[i].a.rows, w[i].b.rows, w[i].k, 2);
+    for (int i = 0; i < n; ++i) {
+        if (few[i].mt) {
+            if (const mv_status rc = launch_few(few_codes(w[i], few_a[i]), few[i], FewProduct<uint32_t>{}, FewCut{}, st)) return rc;
+        } else if (!tiled[i]) {
+            if (const mv_status rc = launch_plain(w[i], st)) return rc;
+        } else if (!both || i == 0) {
+            const Product p = product_of(w[i], cut[i]), q = both ? product_of(w[1], cut[1]) : Product{};
+            const uint32_t firsts = (uint32_t)cut[i].groups(), all = firsts + (both ? (uint32_t)cut[1].groups() : 0u);
+            if (cut[i].mt == 4) hipLaunchKernelGGL((mv_mx_product_tile_kernel<4, 2, 2, 4>), dim3(all), dim3(512), 0, st, p, q, firsts);
+            else hipLaunchKernelGGL((mv_mx_product_tile_kernel<2, 2, 2, 2>), dim3(all), dim3(256), 0, st, p, q, firsts);
+            launch_join(w[i], cut[i], st);
+            if (both) launch_join(w[1], cut[1], st);
+            if (hipGetLastError() != hipSuccess) return MV_ERR_DEVICE;
+        }
+    }
+    return MV_OK;
+}
 
 // A matrix of codes in the scratch, `at` moves behind it.
-struct Held {
-    uint32_t* codes;
-    uint8_t*  scales;
-    int64_t   ld_words, ld_scales, rows;
-    Factor factor() const { return {codes, scales, ld_words, ld_scales, rows}; }
-};
+inline size_t code_bytes(int64_t rows, int64_t n) { return up256((size_t)rows * (size_t)blocks_of(n) * 16); }
+inline size_t scale_bytes(int64_t rows, int64_t n) { return up256((size_t)rows * (size_t)((blocks_of(n) + 3) / 4 * 4)); }
+inline size_t held_bytes(int64_t rows, int64_t n) { return code_bytes(rows, n) + scale_bytes(rows, n); }
 static Held carve(char*& at, int64_t rows, int64_t n)
 {
     Held h = {reinterpret_cast<uint32_t*>(at), reinterpret_cast<uint8_t*>(at + code_bytes(rows, n)), 4 * blocks_of(n),
               (blocks_of(n) + 3) / 4 * 4, rows};
-    at += code_bytes(rows, n) + scale_bytes(rows, n);
+    at += held_bytes(rows, n);
     return h;
+}
+static Factor factor_of(const Held& h) { return {h.codes, h.scales, h.ld_words, h.ld_scales, h.rows}; }
+
+template <typename X>
+static mv_status launch_few_values(const FewCut& cut, const void* x, int64_t ld_x, int64_t m, const Factor& w, int64_t k, const Out& y,
+                                   int64_t ld_y, hipStream_t st)
+{
+    return launch_few(few_product(w, Few<X>{static_cast<const X*>(x), ld_x, nullptr, 0, (uint32_t)m}, k, y, 1, ld_y), cut,
+                      FewProduct<X>{}, FewCut{}, st);
 }
 
 inline bool scratch_valid(const void* p, size_t have, size_t need)
 {
     return need == 0 || (p && have >= need && (reinterpret_cast<uintptr_t>(p) & 15) == 0);
 }
+inline bool sizes_valid(int64_t m, int64_t n, int64_t k) { return size_valid(m) && size_valid(n) && size_valid(k); }
 
 }  // namespace mvx
 
@@ -700,7 +811,7 @@ extern "C" {
 size_t mv_mx_product_scratch_bytes(int64_t m, int64_t n, int64_t k)
 {
     using namespace mvx;
-    return size_valid(m) && size_valid(n) && size_valid(k) ? parts_bytes(m, n, k) : 0;
+    return sizes_valid(m, n, k) ? parts_bytes(m, n, k) : 0;
 }
 
 mv_status mv_mx_product(const uint32_t* a_codes, int64_t ld_aw, const uint8_t* a_scales, int64_t ld_as,
@@ -708,19 +819,18 @@ mv_status mv_mx_product(const uint32_t* a_codes, int64_t ld_aw, const uint8_t* a
                         int64_t k, void* c, int32_t c_dtype, int64_t ld_c, void* scratch, size_t scratch_bytes, void* stream)
 {
     using namespace mvx;
-    if (!size_valid(m) || !size_valid(n) || !size_valid(k) || !codes_valid(a_codes, ld_aw, a_scales, ld_as, k) ||
+    if (!sizes_valid(m, n, k) || !codes_valid(a_codes, ld_aw, a_scales, ld_as, k) ||
         !codes_valid(b_codes, ld_bw, b_scales, ld_bs, k) || !values_valid(c, c_dtype, ld_c, n) ||
-        !scratch_valid(scratch, scratch_bytes, mv_mx_product_scratch_bytes(m, n, k)))
+        !scratch_valid(scratch, scratch_bytes, parts_bytes(m, n, k)))
         return MV_ERR_INVALID_ARG;
-    return launch_product({a_codes, a_scales, ld_aw, ld_as, m}, {b_codes, b_scales, ld_bw, ld_bs, n}, k, c, c_dtype, ld_c,
-                          scratch, static_cast<hipStream_t>(stream));
+    const Wanted w = {{a_codes, a_scales, ld_aw, ld_as, m}, {b_codes, b_scales, ld_bw, ld_bs, n}, k, {c, c_dtype == MV_BF16}, ld_c, scratch};
+    return launch_products(&w, 1, static_cast<hipStream_t>(stream));
 }
 
 size_t mv_mx_linear_scratch_bytes(int64_t m, int64_t n, int64_t k)
 {
     using namespace mvx;
-    if (!size_valid(m) || !size_valid(n) || !size_valid(k)) return 0;
-    return code_bytes(m, k) + scale_bytes(m, k) + parts_bytes(m, n, k);
+    return sizes_valid(m, n, k) ? held_bytes(m, k) + parts_bytes(m, n, k) : 0;
 }
 
 mv_status mv_mx_linear(const void* x, int32_t x_dtype, int64_t ld_x, const uint32_t* w_codes, int64_t ld_words,
@@ -728,36 +838,28 @@ mv_status mv_mx_linear(const void* x, int32_t x_dtype, int64_t ld_x, const uint3
                        int64_t ld_y, void* scratch, size_t scratch_bytes, void* stream)
 {
     using namespace mvx;
-    if (!size_valid(m) || !size_valid(n) || !size_valid(k) || !values_valid(x, x_dtype, ld_x, k) ||
-        !codes_valid(w_codes, ld_words, w_scales, ld_scales, k) || !values_valid(y, y_dtype, ld_y, n) ||
-        !scratch_valid(scratch, scratch_bytes, mv_mx_linear_scratch_bytes(m, n, k)))
+    if (!sizes_valid(m, n, k) || !values_valid(x, x_dtype, ld_x, k) || !codes_valid(w_codes, ld_words, w_scales, ld_scales, k) ||
+        !values_valid(y, y_dtype, ld_y, n) || !scratch_valid(scratch, scratch_bytes, mv_mx_linear_scratch_bytes(m, n, k)))
         return MV_ERR_INVALID_ARG;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (few_fits(m, n, k)) {
-        const Factor w = {w_codes, w_scales, ld_words, ld_scales, n};
-        if (x_dtype == MV_BF16) {
-            const Few<uint16_t> f = {static_cast<const uint16_t*>(x), ld_x, nullptr, 0, (uint32_t)m};
-            return y_dtype == MV_BF16 ? launch_few(w, f, k, static_cast<uint16_t*>(y), 1, ld_y, st)
-                                      : launch_few(w, f, k, static_cast<float*>(y), 1, ld_y, st);
-        }
-        const Few<float> f = {static_cast<const float*>(x), ld_x, nullptr, 0, (uint32_t)m};
-        return y_dtype == MV_BF16 ? launch_few(w, f, k, static_cast<uint16_t*>(y), 1, ld_y, st)
-                                  : launch_few(w, f, k, static_cast<float*>(y), 1, ld_y, st);
-    }
+    const Factor w = {w_codes, w_scales, ld_words, ld_scales, n};
+    const Out out = {y, y_dtype == MV_BF16};
+    const FewCut cut = few_cut(m, n, k, true);
+    if (cut.mt)
+        return x_dtype == MV_BF16 ? launch_few_values<uint16_t>(cut, x, ld_x, m, w, k, out, ld_y, st)
+                                  : launch_few_values<float>(cut, x, ld_x, m, w, k, out, ld_y, st);
     char* at = static_cast<char*>(scratch);
     const Held q = carve(at, m, k);
-    if (const mv_status rc = launch_encode(x, x_dtype, ld_x, m, k, q.codes, q.ld_words, q.scales, q.ld_scales, nullptr, 0, st))
-        return rc;
-    return launch_product(q.factor(), {w_codes, w_scales, ld_words, ld_scales, n}, k, y, y_dtype, ld_y, at, st);
+    if (const mv_status rc = launch_encode({x, ld_x, m, k}, x_dtype, q, nullptr, 0, st)) return rc;
+    const Wanted p = {factor_of(q), w, k, out, ld_y, at};
+    return launch_products(&p, 1, st);
 }
 
 size_t mv_mx_linear_grad_scratch_bytes(int64_t m, int64_t n, int64_t k)
 {
     using namespace mvx;
-    if (!size_valid(m) || !size_valid(n) || !size_valid(k)) return 0;
-    const size_t dx = code_bytes(m, n) + scale_bytes(m, n), dw = code_bytes(n, m) + scale_bytes(n, m) + code_bytes(k, m) + scale_bytes(k, m);
-    const size_t dx_parts = parts_bytes(m, k, n), dw_parts = parts_bytes(n, k, m);
-    return dx + dw + (dx_parts > dw_parts ? dx_parts : dw_parts);
+    if (!sizes_valid(m, n, k)) return 0;
+    return held_bytes(m, n) + held_bytes(n, m) + held_bytes(k, m) + parts_bytes(m, k, n) + parts_bytes(n, k, m);
 }
 
 mv_status mv_mx_linear_grad(const void* x, int64_t ld_x, const void* dy, int64_t ld_dy, int32_t dtype,
@@ -766,7 +868,7 @@ mv_status mv_mx_linear_grad(const void* x, int64_t ld_x, const void* dy, int64_t
                             int32_t dw_dtype, int64_t ld_dw, void* scratch, size_t scratch_bytes, void* stream)
 {
     using namespace mvx;
-    if (!size_valid(m) || !size_valid(n) || !size_valid(k) || !values_valid(dy, dtype, ld_dy, n) || (!dx && !dw) ||
+    if (!sizes_valid(m, n, k) || !values_valid(dy, dtype, ld_dy, n) || (!dx && !dw) ||
         !scratch_valid(scratch, scratch_bytes, mv_mx_linear_grad_scratch_bytes(m, n, k)))
         return MV_ERR_INVALID_ARG;
     if (dx && (!codes_valid(wt_codes, ld_words, wt_scales, ld_scales, n) || !values_valid(dx, dx_dtype, ld_dx, k)))
@@ -774,22 +876,18 @@ mv_status mv_mx_linear_grad(const void* x, int64_t ld_x, const void* dy, int64_t
     if (dw && (!values_valid(x, dtype, ld_x, k) || !values_valid(dw, dw_dtype, ld_dw, k))) return MV_ERR_INVALID_ARG;
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* at = static_cast<char*>(scratch);
-    // the two products' parts take one place, behind all codes
-    char* parts = at + code_bytes(m, n) + scale_bytes(m, n) + code_bytes(n, m) + scale_bytes(n, m) + code_bytes(k, m) + scale_bytes(k, m);
-    if (dx) {
-        const Held q = carve(at, m, n);
-        if (const mv_status rc = launch_encode(dy, dtype, ld_dy, m, n, q.codes, q.ld_words, q.scales, q.ld_scales, nullptr, 0, st))
-            return rc;
-        if (const mv_status rc = launch_product(q.factor(), {wt_codes, wt_scales, ld_words, ld_scales, k}, n, dx, dx_dtype, ld_dx, parts, st))
-            return rc;
-    }
-    if (dw) {
-        const Held p = carve(at, n, m), q = carve(at, k, m);
-        if (const mv_status rc = launch_encode_t(dy, dtype, ld_dy, m, n, p.codes, p.ld_words, p.scales, p.ld_scales, st)) return rc;
-        if (const mv_status rc = launch_encode_t(x, dtype, ld_x, m, k, q.codes, q.ld_words, q.scales, q.ld_scales, st)) return rc;
-        return launch_product(p.factor(), q.factor(), m, dw, dw_dtype, ld_dw, parts, st);
-    }
-    return MV_OK;
+    const Held dy_r = carve(at, m, n), dy_t = carve(at, n, m), x_t = carve(at, k, m);
+    if (const mv_status rc = launch_encode_grad({x, ld_x, m, k}, dw ? &x_t : nullptr, {dy, ld_dy, m, n}, dw ? &dy_t : nullptr,
+                                                dx ? &dy_r : nullptr, dtype, st))
+        return rc;
+    // dw first: its sums are the long ones, as a rule
+    Wanted w[2];
+    int    many = 0;
+    if (dw) w[many++] = {factor_of(dy_t), factor_of(x_t), m, {dw, dw_dtype == MV_BF16}, ld_dw, at};
+    if (dx)
+        w[many++] = {factor_of(dy_r), {wt_codes, wt_scales, ld_words, ld_scales, k}, n, {dx, dx_dtype == MV_BF16}, ld_dx,
+                     at + parts_bytes(n, k, m)};
+    return launch_products(w, many, st);
 }
 
 }  // extern "C"
