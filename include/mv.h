@@ -424,6 +424,14 @@ mv_status mv_clip_norms(mv_clip* clip, float* norms, void* stream);
  */
 mv_status mv_clip_grads(mv_clip* clip, float max_norm, float* norms, float* coefs, void* stream);
 
+/*
+ * Where a group fits the GPU's registers, its gradients are read once: workgroups of one
+ * launch then wait for each other's sums, for at most `polls` looks at memory (default
+ * 2^16, about 50 ms); what is not done then the launch behind does.  Results never depend
+ * on it.  A test hook: 0 makes everyone who does not find what it needs at once give up.
+ */
+mv_status mv_clip_set_spin_limit(mv_clip* clip, uint32_t polls);
+
 /* As mv_end and mv_release: waits for the stream of the last call, frees the handle's scratch; frees the handle. */
 mv_status mv_clip_end(mv_clip* clip);
 void      mv_clip_release(mv_clip* clip);

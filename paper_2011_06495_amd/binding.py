@@ -26,8 +26,8 @@ ABI_SYMBOLS = (
     "mv_last_step_row_stats", "mv_probe_copy",
     "mv_codec_stream_bits", "mv_codec_scratch_bytes", "mv_codec_encode", "mv_codec_decode", "mv_codec_decode_static",
     "mv_quant_scratch_bytes", "mv_quant_encode", "mv_quant_decode",
-    "mv_clip_workspace_bytes", "mv_clip_begin", "mv_clip_bind", "mv_clip_norms", "mv_clip_grads", "mv_clip_end",
-    "mv_clip_release",
+    "mv_clip_workspace_bytes", "mv_clip_begin", "mv_clip_bind", "mv_clip_norms", "mv_clip_grads",
+    "mv_clip_set_spin_limit", "mv_clip_end", "mv_clip_release",
     "mv_mx_row_words", "mv_mx_row_scales", "mv_mx_encode", "mv_mx_encode_t", "mv_mx_decode", "mv_mx_aggregate",
     "mv_mx_product_scratch_bytes", "mv_mx_product", "mv_mx_linear_scratch_bytes", "mv_mx_linear",
     "mv_mx_linear_grad_scratch_bytes", "mv_mx_linear_grad",
@@ -143,6 +143,7 @@ def load() -> ctypes.CDLL:
     L.mv_clip_bind.argtypes = [vp, vp, vp, vp]
     L.mv_clip_norms.argtypes = [vp, vp, vp]
     L.mv_clip_grads.argtypes = [vp, f32, vp, vp, vp]
+    L.mv_clip_set_spin_limit.argtypes = [vp, ctypes.c_uint32]
     L.mv_clip_end.argtypes = [vp]
     L.mv_clip_release.argtypes = [vp]
     L.mv_clip_release.restype = None
@@ -161,7 +162,7 @@ def load() -> ctypes.CDLL:
     L.mv_mx_linear.argtypes = [vp, i32, i64, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, vp, sz, vp]
     L.mv_mx_linear_grad.argtypes = [vp, i64, vp, i64, i32, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, vp, i32, i64,
                                     vp, sz, vp]
-    for f in (L.mv_clip_begin, L.mv_clip_bind, L.mv_clip_norms, L.mv_clip_grads, L.mv_clip_end, L.mv_mx_encode,
+    for f in (L.mv_clip_begin, L.mv_clip_bind, L.mv_clip_norms, L.mv_clip_grads, L.mv_clip_set_spin_limit, L.mv_clip_end, L.mv_mx_encode,
               L.mv_mx_encode_t, L.mv_mx_decode, L.mv_mx_aggregate, L.mv_mx_product, L.mv_mx_linear, L.mv_mx_linear_grad):
         f.restype = i32
     L.mv_probe_copy.argtypes = [vp, vp, ctypes.c_size_t, vp]
@@ -515,6 +516,12 @@ def mv_clip_grads(clip: _Clip, max_norm: float, norms, coefs=None, stream=None) 
                               _float32(coefs, "coefs", clip.n_groups, clip.device), _stream_handle(stream, norms))
     if st != MV_OK:
         raise MvError(st, "mv_clip_grads")
+
+
+def mv_clip_set_spin_limit(clip: _Clip, polls: int) -> None:
+    st = load().mv_clip_set_spin_limit(clip, polls)
+    if st != MV_OK:
+        raise MvError(st, "mv_clip_set_spin_limit")
 
 
 def mv_clip_end(clip: _Clip) -> None:

@@ -343,3 +343,63 @@ def test_an_element_behind_32_bits():
     assert int((out != 0).sum()) == 3
     B.mv_clip_end(clip)
     B.mv_clip_release(clip)
+
+
+@pytest.mark.parametrize("kind", [B.MV_NORM_L2, B.MV_NORM_MAX])
+@pytest.mark.parametrize("polls", [0, 1, 4])
+def test_workgroups_that_give_up_leave_their_chunks(polls, kind):
+    """With hardly any looks allowed, most chunks are done by the launch behind; results and norms are the same."""
+    rng = np.random.default_rng(polls)
+    sizes = [300_000, 17, 1_200_000, 5]
+    tensors, groups = [], []
+    for g in range(5):
+        tensors += make(rng, sizes, torch.float32 if g % 2 else torch.bfloat16, lead=1)
+        groups += [g] * len(sizes)
+    out = [t if i < len(sizes) else torch.zeros(t.numel(), device="cuda") for i, t in enumerate(tensors)]     # group 0 in place
+    before = [f32(t) for t in tensors]
+    norms, coefs = torch.zeros(6, device="cuda"), torch.zeros(6, device="cuda")
+    clip = B.mv_clip_begin(tensors, out=out, groups=groups, n_groups=6, norm=kind)
+    per = [before[g * len(sizes):(g + 1) * len(sizes)] for g in range(5)]
+    want = [norm64(p, kind) for p in per]
+    max_norm = sorted(want)[2]
+    B.mv_clip_set_spin_limit(clip, polls)
+    for turn in range(3):
+        for t, b in zip(tensors[:len(sizes)], before):
+            t.copy_(torch.from_numpy(b))
+        for o in out[len(sizes):]:
+            o.zero_()
+        norms.fill_(-1.0)
+        B.mv_clip_grads(clip, max_norm, norms, coefs)
+        torch.cuda.synchronize()
+        n, c = norms.cpu().numpy(), coefs.cpu().numpy()
+        assert n[5] == 0.0 and c[5] == 1.0
+        for g in range(5):
+            check_norm(n[g], want[g], kind)
+            assert c[g] == coef32(n[g], max_norm)
+        for t, o, b, g in zip(tensors, out, before, groups):
+            assert np.array_equal(f32(o), to_type(b * c[g], o.dtype))
+        if turn == 1:
+            B.mv_clip_set_spin_limit(clip, 1 << 16)
+    B.mv_clip_end(clip)
+    B.mv_clip_release(clip)
+
+
+def test_many_groups_beside_each_other():
+    """More chunks than run at once, in groups that fit: each waits for its own only; and norms between the calls."""
+    rng = np.random.default_rng(17)
+    groups, d = 40, 700_001
+    x = torch.from_numpy(rng.standard_normal((groups, d)).astype(np.float32)).cuda()
+    out = torch.zeros((groups, d), dtype=torch.bfloat16, device="cuda")
+    norms, only = torch.zeros(groups, device="cuda"), torch.zeros(groups, device="cuda")
+    clip = B.mv_clip_begin(list(x), out=list(out), groups=range(groups))
+    h = f32(x)
+    for i in range(3):
+        B.mv_clip_norms(clip, only)
+        B.mv_clip_grads(clip, 800.0 + 30.0 * i, norms)
+        assert torch.equal(norms, only)
+        n, o = norms.cpu().numpy(), f32(out)
+        for g in range(groups):
+            check_norm(n[g], norm64([h[g]], B.MV_NORM_L2), B.MV_NORM_L2)
+            assert np.array_equal(o[g], to_type(h[g] * coef32(n[g], 800.0 + 30.0 * i), torch.bfloat16))
+    B.mv_clip_end(clip)
+    B.mv_clip_release(clip)

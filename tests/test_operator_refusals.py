@@ -65,6 +65,7 @@ def test_clip_null_handles(lib):
     assert lib.mv_clip_norms(None, P, None) == B.MV_ERR_INVALID_ARG
     assert lib.mv_clip_grads(None, 1.0, P, None, None) == B.MV_ERR_INVALID_ARG
     assert lib.mv_clip_bind(None, P, P, None) == B.MV_ERR_INVALID_ARG
+    assert lib.mv_clip_set_spin_limit(None, 1) == B.MV_ERR_INVALID_ARG
     assert lib.mv_clip_end(None) == B.MV_ERR_INVALID_ARG
     lib.mv_clip_release(None)
 
