@@ -452,7 +452,7 @@ void      mv_clip_release(mv_clip* clip);
  * block are neither written nor used.  Codes are 16-byte aligned, ld_words a multiple
  * of 4; scales 4-byte aligned, ld_scales a multiple of 4.
  * Values (vals, resid, out, x, y, ...) are fp32 or bf16, aligned to their element, with
- * any row stride >= the row; 1 <= rows, n < 2^31, at most 2^35 values in a matrix.
+ * any row stride >= the row; 1 <= rows, n < 2^31, at most 2^34 - 2^15 values in whole blocks.
  * All of these calls run on the CURRENT device, are enqueued on `stream` and allocate
  * nothing.  Errors: MV_ERR_INVALID_ARG, MV_ERR_DEVICE.
  */

@@ -2,35 +2,36 @@
 // receiver's sum over the workers.
 //
 // All of these read and write each value once and compute a few instructions on it: HBM bounds them, launches where they
-// are short.  Four lanes take a block of 32 values, eight each, so the block's largest magnitude is two DPP moves away and
-// a lane writes a whole word of codes.
+// are short.  A lane takes 16 bytes of values, so a wavefront's loads and stores cover one run of memory: four lanes a
+// block of 32 bf16 values, eight lanes one of fp32; the block's largest magnitude is two or three DPP moves away.
 #include "mv_mx.hpp"
 
 namespace mvx {
 
 constexpr int kThreads = 256;
 
-// (row, block of the row) of the block that this group of four lanes takes: workgroups take kThreads / 4 consecutive
-// blocks of the rows one after the other.
+// (row, block of the row) of a block of all rows one after the other.  There are fewer than 2^31 of them in a launch.
 struct Place {
-    int64_t row, block;
+    uint32_t row, block;
 };
-__device__ __forceinline__ Place place_of(int64_t first_block, int64_t row_blocks)
+// Block `first` + `more`, with a division for the whole workgroup and, where a row may end in between, one of small numbers.
+__device__ __forceinline__ Place place_of(uint32_t first, uint32_t more, uint32_t row_blocks)
 {
-    Place p = {first_block / row_blocks, 0};          // uniform
-    p.block = first_block - p.row * row_blocks + threadIdx.x / 4;
+    const uint32_t row = first / row_blocks;
+    Place p = {row, first - row * row_blocks + more};
     if (p.block >= row_blocks) {
-        if (row_blocks <= kThreads / 4) {
-            const uint32_t more = (uint32_t)p.block / (uint32_t)row_blocks;
-            p.row += more;
-            p.block -= (int64_t)more * row_blocks;
-        } else {
-            p.row += 1;
-            p.block -= row_blocks;
-        }
+        const uint32_t rows = row_blocks > more ? 1u : p.block / row_blocks;
+        p.row += rows;
+        p.block -= rows * row_blocks;
     }
     return p;
 }
+
+// Lanes of a block, and blocks of a workgroup.
+template <typename T>
+constexpr int kBlockLanes = sizeof(T) == 2 ? 4 : 8;
+template <typename T>
+constexpr int kGroupBlocks = kThreads / kBlockLanes<T>;
 
 // A matrix of values and where its codes go.
 template <typename T>
@@ -46,24 +47,35 @@ struct Encode {
 template <typename T, bool RESID>
 __device__ __forceinline__ void encode_rows(const Encode<T>& e, uint32_t at_group, float* resid, int64_t ld_resid)
 {
-    const Place p = place_of((int64_t)at_group * (kThreads / 4), blocks_of(e.n));
-    if (p.row >= e.rows) return;                       // whole groups of four lanes
-    const int64_t at = p.block * kBlock + (threadIdx.x & 3) * 8;
-    float x[8];
-    load8(e.vals + p.row * e.ld_vals + at, e.n - at, x);
+    constexpr int kLanes = kBlockLanes<T>, V = kBlock / kLanes;
+    const uint32_t mine = threadIdx.x % kLanes;
+    const Place p = place_of(at_group * kGroupBlocks<T>, threadIdx.x / kLanes, (uint32_t)blocks_of(e.n));
+    if (p.row >= e.rows) return;                       // all lanes of a block
+    const int64_t at = (int64_t)p.block * kBlock + mine * V;
+    float x[V];
+    if constexpr (V == 8) load8(e.vals + p.row * e.ld_vals + at, e.n - at, x);
+    else load4(e.vals + p.row * e.ld_vals + at, e.n - at, x);
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-    const uint32_t scale = scale_of(top_of_quad(top));
-    const uint32_t w = encode8(x, scale);
-    e.codes[p.row * e.ld_words + at / 8] = w;
-    if ((threadIdx.x & 3) == 0) e.scales[p.row * e.ld_scales + p.block] = (uint8_t)scale;
+    for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    const uint32_t scale = scale_of(V == 8 ? top_of_quad(top) : top_of_eight(top));
+    float held[V];
+    if constexpr (V == 8) {
+        const uint32_t w = encode8(x, scale);
+        e.codes[p.row * e.ld_words + at / 8] = w;
+        if constexpr (RESID) decode8(w, scale, held);
+    } else {
+        const uint32_t w = encode4(x, scale);
+        const uint32_t next = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0xB1, 0xf, 0xf, false);   // the neighbour's
+        if ((mine & 1u) == 0) e.codes[p.row * e.ld_words + at / 8] = w | next << 16;
+        if constexpr (RESID) decode4(w, scale, held);
+    }
+    if (mine == 0) e.scales[p.row * e.ld_scales + p.block] = (uint8_t)scale;
     if constexpr (RESID) {
-        float held[8];
-        decode8(w, scale, held);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] -= held[i];
-        store8(resid + p.row * ld_resid + at, e.n - at, x);
+        for (int i = 0; i < V; ++i) held[i] = x[i] - held[i];
+        if constexpr (V == 8) store8(resid + p.row * ld_resid + at, e.n - at, held);
+        else store4(resid + p.row * ld_resid + at, e.n - at, held);
     }
 }
 
@@ -82,15 +94,8 @@ constexpr int kLaneCols = 16 / (int)sizeof(T);
 template <typename T>
 __device__ __forceinline__ void load_cols(const T* p, int64_t live, float (&x)[kLaneCols<T>])
 {
-    if constexpr (sizeof(T) == 2) {
-        load8(p, live, x);
-    } else if (live >= 4) {
-        const f32x4u v = *reinterpret_cast<const f32x4u*>(p);
-        x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = i < live ? p[i] : 0.0f;
-    }
+    if constexpr (sizeof(T) == 2) load8(p, live, x);
+    else load4(p, live, x);
 }
 template <typename T>
 constexpr int kTileCols = 16 * kLaneCols<T>;
@@ -167,12 +172,20 @@ __global__ __launch_bounds__(kThreads) void mv_mx_decode_kernel(const uint32_t* 
                                                                 const uint8_t* __restrict__ scales, int64_t ld_scales,
                                                                 int64_t rows, int64_t n, T* __restrict__ out, int64_t ld_out)
 {
-    const Place p = place_of((int64_t)blockIdx.x * (kThreads / 4), blocks_of(n));
+    constexpr int kLanes = kBlockLanes<T>, V = kBlock / kLanes;
+    const uint32_t mine = threadIdx.x % kLanes;
+    const Place p = place_of(blockIdx.x * kGroupBlocks<T>, threadIdx.x / kLanes, (uint32_t)blocks_of(n));
     if (p.row >= rows) return;
-    const int64_t at = p.block * kBlock + (threadIdx.x & 3) * 8;
-    float x[8];
-    decode8(codes[p.row * ld_words + at / 8], scales[p.row * ld_scales + p.block], x);
-    store8(out + p.row * ld_out + at, n - at, x);
+    const int64_t at = (int64_t)p.block * kBlock + mine * V;
+    const uint32_t w = codes[p.row * ld_words + at / 8], scale = scales[p.row * ld_scales + p.block];
+    float x[V];
+    if constexpr (V == 8) {
+        decode8(w, scale, x);
+        store8(out + p.row * ld_out + at, n - at, x);
+    } else {
+        decode4(w >> (16 * (mine & 1u)), scale, x);
+        store4(out + p.row * ld_out + at, n - at, x);
+    }
 }
 
 // A lane adds up eight values over the rows.
@@ -213,12 +226,16 @@ static Encode<T> encode_of(const Values& v, const Held& to)
 {
     return {static_cast<const T*>(v.p), v.ld, v.rows, v.n, to.codes, to.ld_words, to.scales, to.ld_scales};
 }
-static int64_t row_groups(const Values& v) { return (v.rows * blocks_of(v.n) + kThreads / 4 - 1) / (kThreads / 4); }
+static int64_t row_groups(int64_t rows, int64_t n, int32_t dtype)
+{
+    const int64_t per = dtype == MV_BF16 ? kGroupBlocks<uint16_t> : kGroupBlocks<float>;
+    return (rows * blocks_of(n) + per - 1) / per;
+}
 
 mv_status launch_encode(const Values& v, int32_t dtype, const Held& to, float* resid, int64_t ld_resid, hipStream_t st)
 {
-    if (row_groups(v) > kMostGroups) return MV_ERR_INVALID_ARG;
-    const dim3 grid((uint32_t)row_groups(v)), threads(kThreads);
+    if (!count_valid(v.rows, v.n)) return MV_ERR_INVALID_ARG;
+    const dim3 grid((uint32_t)row_groups(v.rows, v.n, dtype)), threads(kThreads);
 #define MV_MX_ENCODE(T, R) hipLaunchKernelGGL((mv_mx_encode_kernel<T, R>), grid, threads, 0, st, encode_of<T>(v, to), resid, ld_resid)
     if (dtype == MV_BF16) {
         if (resid) MV_MX_ENCODE(uint16_t, true);
@@ -248,8 +265,8 @@ template <typename T>
 static mv_status launch_encode_grad_of(const Values& x, const Held* x_t, const Values& dy, const Held* dy_t, const Held* dy_r, hipStream_t st)
 {
     const int64_t a = x_t ? column_groups<T>(x.rows, x.n) : 0, b = dy_t ? column_groups<T>(dy.rows, dy.n) : 0;
-    const int64_t c = dy_r ? row_groups(dy) : 0;
-    if (a + b + c > kMostGroups) return MV_ERR_INVALID_ARG;
+    const int64_t c = dy_r ? row_groups(dy.rows, dy.n, sizeof(T) == 2 ? MV_BF16 : MV_F32) : 0;
+    if ((dy_r && !count_valid(dy.rows, dy.n)) || a + b + c > kMostGroups) return MV_ERR_INVALID_ARG;
     const Encode<T> none = {};
     hipLaunchKernelGGL(mv_mx_encode_grad_kernel<T>, dim3((uint32_t)(a + b + c)), dim3(kThreads), 0, st,
                        x_t ? encode_of<T>(x, *x_t) : none, (uint32_t)a, dy_t ? encode_of<T>(dy, *dy_t) : none, (uint32_t)b,
@@ -300,9 +317,8 @@ mv_status mv_mx_decode(const uint32_t* codes, int64_t ld_words, const uint8_t* s
     if (!size_valid(rows) || !size_valid(n) || !values_valid(out, dtype, ld_out, n) ||
         !codes_valid(codes, ld_words, scales, ld_scales, n))
         return MV_ERR_INVALID_ARG;
-    const int64_t groups = (rows * blocks_of(n) + kThreads / 4 - 1) / (kThreads / 4);
-    if (groups > kMostGroups) return MV_ERR_INVALID_ARG;
-    const dim3 grid((uint32_t)groups), threads(kThreads);
+    if (!count_valid(rows, n)) return MV_ERR_INVALID_ARG;
+    const dim3 grid((uint32_t)row_groups(rows, n, dtype)), threads(kThreads);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (dtype == MV_BF16)
         hipLaunchKernelGGL(mv_mx_decode_kernel<uint16_t>, grid, threads, 0, st, codes, ld_words, scales, ld_scales, rows, n,
