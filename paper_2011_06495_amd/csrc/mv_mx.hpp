@@ -63,11 +63,12 @@ __device__ __forceinline__ void load4(const float* p, int64_t live, float (&x)[4
 }
 // Stores of which a wavefront's cover one run of memory pass the caches: 8192 x 4096 bf16 quantised and read back 36.5 ->
 // 29.3 us.  Where lanes leave gaps for a second store, that costs more than it saves (fp32 in 32 bytes a lane 57 -> 78 us).
-__device__ __forceinline__ void store4(float* p, int64_t live, const float* x)
+__device__ __forceinline__ void store4(float* p, int64_t live, const float* x, bool past = true)
 {
     if (live >= 4) {
         const f32x4u v = {x[0], x[1], x[2], x[3]};
-        __builtin_nontemporal_store(v, reinterpret_cast<f32x4u*>(p));
+        if (past) __builtin_nontemporal_store(v, reinterpret_cast<f32x4u*>(p));
+        else *reinterpret_cast<f32x4u*>(p) = v;
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -86,13 +87,14 @@ __device__ __forceinline__ void store8(float* p, int64_t live, const float (&x)[
             if (i < live) p[i] = x[i];
     }
 }
-__device__ __forceinline__ void store8(uint16_t* p, int64_t live, const float (&x)[8])
+__device__ __forceinline__ void store8(uint16_t* p, int64_t live, const float (&x)[8], bool past = true)
 {
     if (live >= 8) {
         u32x4u a;
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = narrow(x[2 * i]) | narrow(x[2 * i + 1]) << 16;
-        __builtin_nontemporal_store(a, reinterpret_cast<u32x4u*>(p));
+        if (past) __builtin_nontemporal_store(a, reinterpret_cast<u32x4u*>(p));
+        else *reinterpret_cast<u32x4u*>(p) = a;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)

@@ -151,6 +151,7 @@ struct Product {
     uint32_t blocks, tiles_m, tiles_n, steps_each, splits;
     Out      c;
     int64_t  ld_c, split_c;
+    uint32_t past;                  // store past the caches
 };
 
 // Which tile a workgroup takes: consecutive workgroups run on eight dies with an L2 of their own, so a die gets a run of
@@ -324,20 +325,40 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Pro
     }
     __builtin_amdgcn_s_waitcnt(kNoLoads);
 
-    // a lane has, of row i, four times four consecutive columns
-    const int64_t col0 = j0 + wave % WN * (32 * NT) + 4 * half, out = split * p.split_c + col0;
-    const bool whole = j0 + kN <= b.rows;
+    // A lane has, of 32 rows, four times four consecutive columns.  32 rows of the wavefront's 64 columns at a time go
+    // through its part of LDS, 16-byte units in the order unit ^ (row % 16), and out in whole runs of a row.
+    static_assert(NT == 2 && kWaves * 8192 <= sizeof(Codes), "a wavefront's 32 x 64 results");
+    float* mine = reinterpret_cast<float*>(even + wave * 8192);
+    const int64_t col0 = j0 + wave % WN * 64, out = split * p.split_c;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        const int64_t row = i0 + a_row + 32 * i;
-        if (row >= a.rows) continue;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                p.c.put4(out + row * p.ld_c + 32 * j + 8 * q, whole ? 4 : b.rows - (col0 + 32 * j + 8 * q), v);
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f32x4*>(mine + in * 64 + ((8 * j + 2 * q + half) ^ (in & 15u)) * 4) =
+                    f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        const int64_t row0 = i0 + wave / WN * (32 * MT) + 32 * i;
+        if (p.c.bf16) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t r = 8 * u + lane / 8, unit = lane % 8 * 2;
+                const f32x4 x = *reinterpret_cast<const f32x4*>(mine + r * 64 + (unit ^ (r & 15u)) * 4);
+                const f32x4 y = *reinterpret_cast<const f32x4*>(mine + r * 64 + ((unit + 1) ^ (r & 15u)) * 4);
+                const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                const int64_t col = col0 + 4 * unit;
+                if (row0 + r < a.rows) store8(static_cast<uint16_t*>(p.c.p) + out + (row0 + r) * p.ld_c + col, b.rows - col, v, p.past);
             }
+        } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const uint32_t r = 4 * u + lane / 16, unit = lane % 16;
+                const f32x4 x = *reinterpret_cast<const f32x4*>(mine + r * 64 + (unit ^ (r & 15u)) * 4);
+                const float v[4] = {x.x, x.y, x.z, x.w};
+                const int64_t col = col0 + 4 * unit;
+                if (row0 + r < a.rows) store4(static_cast<float*>(p.c.p) + out + (row0 + r) * p.ld_c + col, b.rows - col, v, p.past);
+            }
+        }
     }
 }
 
@@ -663,13 +684,13 @@ struct Cut {
     uint32_t splits, steps_each;
     int64_t  groups() const { return tiles_m * tiles_n * splits; }
 };
-static Cut cut_of(int64_t m, int64_t n, int64_t k, int mt)
+static Cut cut_of(int64_t m, int64_t n, int64_t k, int mt, int64_t beside = 0)
 {
     auto tiles = [mt](int64_t rows) { return (rows + 64 * mt - 1) / (64 * mt); };
     Cut c = {mt, tiles(m), tiles(n), 1, 0};
     const int64_t steps = (blocks_of(k) + kStepBlocks - 1) / kStepBlocks;
     if (mt == 2) {
-        int64_t splits = 512 / (c.tiles_m * c.tiles_n);
+        int64_t splits = 512 / (c.tiles_m * c.tiles_n + beside);
         if (splits > steps / 4) splits = steps / 4;
         // many splits only of small results: all of them are written and read again
         if (splits > 16 && splits * m * n > (4 << 20)) splits = 16;
@@ -687,6 +708,11 @@ inline size_t parts_bytes(int64_t m, int64_t n, int64_t k)
     return splits > 1 ? up256((size_t)splits * (size_t)m * (size_t)quads_of(n) * 16) : 0;
 }
 
+// Results beyond the L2s' 32 MB are stored past them: 4096 x 8192 bf16 by 8192 201 -> 170 us with whole runs of a row, so
+// stored.  Smaller ones, and sums that are added up right away, are a little faster stored as usual: 1000 x 1000 by 1000
+// 10.1 : 10.6 us, 130 x 130 by 8000 14.1 : 16.3.
+constexpr int64_t kPastBytes = 16 << 20;
+
 // A product that is asked for: c = a b^T, m rows and n rows of k values.
 struct Wanted {
     Factor  a, b;
@@ -700,7 +726,8 @@ static Product product_of(const Wanted& w, const Cut& cut)
     const int64_t quads = quads_of(w.b.rows);
     const bool split = cut.splits > 1;
     return {w.a, w.b, (uint32_t)blocks_of(w.k), (uint32_t)cut.tiles_m, (uint32_t)cut.tiles_n, cut.steps_each, cut.splits,
-            split ? Out{w.parts, 0} : w.c, split ? quads * 4 : w.ld_c, w.a.rows * quads * 4};
+            split ? Out{w.parts, 0} : w.c, split ? quads * 4 : w.ld_c, w.a.rows * quads * 4,
+            w.a.rows * w.b.rows * (split ? 4 * (int64_t)cut.splits : w.c.bf16 ? 2 : 4) >= kPastBytes};
 }
 static void launch_join(const Wanted& w, const Cut& cut, hipStream_t st)
 {
@@ -757,8 +784,11 @@ static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
         }
     }
     const bool both = tiled[0] && tiled[1] && n == 2;
-    if (both && cut[0].mt != cut[1].mt)           // in one launch: the smaller tiles for both
-        for (int i = 0; i < 2; ++i) cut[i] = cut_of(w[i].a.rows, w[i].b.rows, w[i].k, 2);
+    // in one launch: the smaller tiles for both, and each other's tiles to fill the units with
+    if (both && (cut[0].mt == 2 || cut[1].mt == 2)) {
+        const int64_t tiles[2] = {cut_of(w[0].a.rows, w[0].b.rows, w[0].k, 2, 512).groups(), cut_of(w[1].a.rows, w[1].b.rows, w[1].k, 2, 512).groups()};
+        for (int i = 0; i < 2; ++i) cut[i] = cut_of(w[i].a.rows, w[i].b.rows, w[i].k, 2, tiles[1 - i]);
+    }
     for (int i = 0; i < n; ++i) {
         if (few[i].mt) {
             if (const mv_status rc = launch_few(few_codes(w[i], few_a[i]), few[i], FewProduct<uint32_t>{}, FewCut{}, st)) return rc;
