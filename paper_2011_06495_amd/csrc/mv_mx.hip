@@ -102,7 +102,7 @@ constexpr int kTileCols = 16 * kLaneCols<T>;
 template <typename T>
 struct Columns {                    // of a workgroup: codes and scales on their way out
     uint32_t words[kTileCols<T>][4 * kTileBlocks];
-    uint8_t  scales[kTileCols<T>][kTileBlocks];
+    alignas(4) uint8_t scales[kTileCols<T>][kTileBlocks];
 };
 template <typename T>
 inline int64_t column_tiles(int64_t n) { return (n + kTileCols<T> - 1) / kTileCols<T>; }
@@ -142,7 +142,10 @@ __device__ __forceinline__ void encode_columns(const Encode<T>& e, uint32_t at_g
         const int64_t to = (int64_t)tile * kTileCols<T> + c, to_block = (int64_t)strip * kTileBlocks + b;
         if (to < e.n && to_block < blocks_of(e.rows)) {
             *reinterpret_cast<u32x4*>(e.codes + to * e.ld_words + to_block * 4) = *reinterpret_cast<const u32x4*>(&out.words[c][4 * b]);
-            e.scales[to * e.ld_scales + to_block] = out.scales[c][b];
+            // four scales in one store where there are four
+            const bool whole = ((int64_t)strip + 1) * kTileBlocks <= blocks_of(e.rows);
+            if (!whole) e.scales[to * e.ld_scales + to_block] = out.scales[c][b];
+            else if (b == 0) *reinterpret_cast<uint32_t*>(e.scales + to * e.ld_scales + to_block) = *reinterpret_cast<const uint32_t*>(out.scales[c]);
         }
     }
 }

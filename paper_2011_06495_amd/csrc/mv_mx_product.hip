@@ -808,12 +808,14 @@ static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
 }
 
 // A matrix of codes in the scratch, `at` moves behind it.
-inline size_t code_bytes(int64_t rows, int64_t n) { return up256((size_t)rows * (size_t)blocks_of(n) * 16); }
+// Its rows of codes are whole lines of 128 bytes: the columns' codes come in runs of 64.
+inline int64_t line_words(int64_t n) { return (4 * blocks_of(n) + 31) / 32 * 32; }
+inline size_t code_bytes(int64_t rows, int64_t n) { return up256((size_t)rows * (size_t)line_words(n) * 4); }
 inline size_t scale_bytes(int64_t rows, int64_t n) { return up256((size_t)rows * (size_t)((blocks_of(n) + 3) / 4 * 4)); }
 inline size_t held_bytes(int64_t rows, int64_t n) { return code_bytes(rows, n) + scale_bytes(rows, n); }
 static Held carve(char*& at, int64_t rows, int64_t n)
 {
-    Held h = {reinterpret_cast<uint32_t*>(at), reinterpret_cast<uint8_t*>(at + code_bytes(rows, n)), 4 * blocks_of(n),
+    Held h = {reinterpret_cast<uint32_t*>(at), reinterpret_cast<uint8_t*>(at + code_bytes(rows, n)), line_words(n),
               (blocks_of(n) + 3) / 4 * 4, rows};
     at += held_bytes(rows, n);
     return h;
