@@ -144,6 +144,16 @@ __device__ __forceinline__ f32x16 mfma32(const u32x4& a, uint32_t a_scale, const
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, S, (int)a_scale, S, (int)b_scale);
 }
 
+// One or two products of a launch, the first workgroups are the first one's.  A launch from the host takes a microsecond
+// longer with 400 bytes of arguments than with 8, so a single product's have room for one only.
+template <typename P, bool PAIR>
+struct Launch {
+    P        products[PAIR ? 2 : 1];
+    uint32_t firsts;
+    __device__ __forceinline__ const P& product() const { return products[PAIR && blockIdx.x >= firsts ? 1 : 0]; }
+    __device__ __forceinline__ uint32_t id() const { return PAIR && blockIdx.x >= firsts ? blockIdx.x - firsts : blockIdx.x; }
+};
+
 // One product and how it is cut: tiles_m x tiles_n tiles, `splits` runs of steps_each steps each.  With several splits c is
 // fp32 and holds their sums one after the other, split_c apart.
 struct Product {
@@ -171,9 +181,8 @@ struct Rows {
     u32x4 x[MT], y[NT];
 };
 
-// Two products in one launch, the first workgroups take the first one's tiles.
-template <int MT, int NT, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Product first, Product second, uint32_t firsts)
+template <int MT, int NT, int WM, int WN, bool PAIR>
+__global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Launch<Product, PAIR> l)
 {
     constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
     constexpr int kM = 32 * MT * WM, kN = 32 * NT * WN, kRows = kM + kN;
@@ -182,10 +191,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Pro
     __shared__ __attribute__((aligned(1024))) Codes even, odd;
     __shared__ uint8_t scales[2][kRows * kScalePitch];
     const uint32_t t = threadIdx.x, lane = t & 63u, wave = __builtin_amdgcn_readfirstlane(t / 64);
-    const bool is_first = blockIdx.x < firsts;
-    const Product& p = is_first ? first : second;
+    const Product& p = l.product();
     const Factor a = p.a, b = p.b;
-    const uint32_t blocks = p.blocks, steps_each = p.steps_each, id = is_first ? blockIdx.x : blockIdx.x - firsts;
+    const uint32_t blocks = p.blocks, steps_each = p.steps_each, id = l.id();
     const uint32_t split = id / (p.tiles_m * p.tiles_n);
     uint32_t tm, tn;
     tile_of(id - split * (p.tiles_m * p.tiles_n), p.tiles_m, p.tiles_n, tm, tn);
@@ -503,13 +511,12 @@ struct FewProduct {
     int64_t  step_many, step_few;
 };
 
-// Two products in one launch, the first workgroups take the first one's.  A workgroup: 16 MT few rows, 16 NT of the many.
-template <int MT, int NT, typename X>
-__global__ __launch_bounds__(64 * kFewWaves) void mv_mx_product_few_kernel(FewProduct<X> first, FewProduct<X> second, uint32_t firsts)
+// A workgroup: 16 MT few rows, 16 NT of the many.
+template <int MT, int NT, typename X, bool PAIR>
+__global__ __launch_bounds__(64 * kFewWaves) void mv_mx_product_few_kernel(Launch<FewProduct<X>, PAIR> l)
 {
-    const bool is_first = blockIdx.x < firsts;
-    const FewProduct<X>& p = is_first ? first : second;
-    const uint32_t id = is_first ? blockIdx.x : blockIdx.x - firsts;
+    const FewProduct<X>& p = l.product();
+    const uint32_t id = l.id();
     const Factor many = p.many;
     const Few<X> few = p.few;
     const uint32_t blocks = p.blocks;
@@ -657,22 +664,30 @@ static FewProduct<X> few_product(const Factor& many, const Few<X>& few, int64_t 
 {
     return {many, few, (uint32_t)blocks_of(k), k, c, step_many, step_few};
 }
+// One product, or two whose cuts have the same mt and nt.
 template <int MT, int NT, typename X>
-static void launch_few_of(const FewProduct<X>& p, const FewCut& cut, const FewProduct<X>& q, const FewCut& cut2, hipStream_t st)
+static void launch_few_of(const FewProduct<X>* p, const FewCut* cut, int n, hipStream_t st)
 {
-    hipLaunchKernelGGL((mv_mx_product_few_kernel<MT, NT, X>), dim3(cut.groups + cut2.groups),
-                       dim3(64 * (cut.waves > cut2.waves ? cut.waves : cut2.waves)), cut.lds > cut2.lds ? cut.lds : cut2.lds, st, p, q,
-                       cut.groups);
+    const dim3 threads(64 * (n == 2 && cut[1].waves > cut[0].waves ? cut[1].waves : cut[0].waves));
+    const uint32_t lds = n == 2 && cut[1].lds > cut[0].lds ? cut[1].lds : cut[0].lds;
+    if constexpr (std::is_same_v<X, uint32_t>) {
+        if (n == 2) {
+            hipLaunchKernelGGL((mv_mx_product_few_kernel<MT, NT, X, true>), dim3(cut[0].groups + cut[1].groups), threads, lds, st,
+                               Launch<FewProduct<X>, true>{{p[0], p[1]}, cut[0].groups});
+            return;
+        }
+    }
+    hipLaunchKernelGGL((mv_mx_product_few_kernel<MT, NT, X, false>), dim3(cut[0].groups), threads, lds, st,
+                       Launch<FewProduct<X>, false>{{p[0]}, cut[0].groups});
 }
-// Up to two products; the second's cut has the first's mt and nt, or no groups.
 template <typename X>
-static mv_status launch_few(const FewProduct<X>& p, const FewCut& cut, const FewProduct<X>& q, const FewCut& cut2, hipStream_t st)
+static mv_status launch_few(const FewProduct<X>* p, const FewCut* cut, int n, hipStream_t st)
 {
-    if (cut.nt == 2) launch_few_of<1, 2>(p, cut, q, cut2, st);
-    else if (cut.mt == 1) launch_few_of<1, 1>(p, cut, q, cut2, st);
+    if (cut[0].nt == 2) launch_few_of<1, 2>(p, cut, n, st);
+    else if (cut[0].mt == 1) launch_few_of<1, 1>(p, cut, n, st);
     else if constexpr (!std::is_same_v<X, uint32_t>) {                   // codes: up to 16 rows only
-        if (cut.mt == 2) launch_few_of<2, 1>(p, cut, q, cut2, st);
-        else launch_few_of<4, 1>(p, cut, q, cut2, st);
+        if (cut[0].mt == 2) launch_few_of<2, 1>(p, cut, n, st);
+        else launch_few_of<4, 1>(p, cut, n, st);
     }
     return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
 }
@@ -771,9 +786,12 @@ static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
 {
     FewCut few[2] = {};
     bool few_a[2] = {};
-    for (int i = 0; i < n; ++i) few[i] = few_codes_cut(w[i], few_a[i]);
-    if (n == 2 && few[0].mt && few[0].mt == few[1].mt && few[0].nt == few[1].nt)
-        return launch_few(few_codes(w[0], few_a[0]), few[0], few_codes(w[1], few_a[1]), few[1], st);
+    FewProduct<uint32_t> fp[2];
+    for (int i = 0; i < n; ++i) {
+        few[i] = few_codes_cut(w[i], few_a[i]);
+        if (few[i].mt) fp[i] = few_codes(w[i], few_a[i]);
+    }
+    if (n == 2 && few[0].mt && few[0].mt == few[1].mt && few[0].nt == few[1].nt) return launch_few(fp, few, 2, st);
     Cut  cut[2] = {};
     bool tiled[2] = {};
     for (int i = 0; i < n; ++i) {
@@ -783,22 +801,34 @@ static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
             if (cut[i].groups() > kMostGroups / 2) return MV_ERR_INVALID_ARG;
         }
     }
-    const bool both = tiled[0] && tiled[1] && n == 2;
+    const bool both = tiled[0] && tiled[1];
     // in one launch: the smaller tiles for both, and each other's tiles to fill the units with
     if (both && (cut[0].mt == 2 || cut[1].mt == 2)) {
-        const int64_t tiles[2] = {cut_of(w[0].a.rows, w[0].b.rows, w[0].k, 2, 512).groups(), cut_of(w[1].a.rows, w[1].b.rows, w[1].k, 2, 512).groups()};
+        const int64_t tiles[2] = {cut_of(w[0].a.rows, w[0].b.rows, w[0].k, 2, 512).groups(),
+                                  cut_of(w[1].a.rows, w[1].b.rows, w[1].k, 2, 512).groups()};
         for (int i = 0; i < 2; ++i) cut[i] = cut_of(w[i].a.rows, w[i].b.rows, w[i].k, 2, tiles[1 - i]);
+        if (cut[0].groups() + cut[1].groups() > kMostGroups) return MV_ERR_INVALID_ARG;
     }
     for (int i = 0; i < n; ++i) {
         if (few[i].mt) {
-            if (const mv_status rc = launch_few(few_codes(w[i], few_a[i]), few[i], FewProduct<uint32_t>{}, FewCut{}, st)) return rc;
+            if (const mv_status rc = launch_few(fp + i, few + i, 1, st)) return rc;
         } else if (!tiled[i]) {
             if (const mv_status rc = launch_plain(w[i], st)) return rc;
         } else if (!both || i == 0) {
-            const Product p = product_of(w[i], cut[i]), q = both ? product_of(w[1], cut[1]) : Product{};
-            const uint32_t firsts = (uint32_t)cut[i].groups(), all = firsts + (both ? (uint32_t)cut[1].groups() : 0u);
-            if (cut[i].mt == 4) hipLaunchKernelGGL((mv_mx_product_tile_kernel<4, 2, 2, 4>), dim3(all), dim3(512), 0, st, p, q, firsts);
-            else hipLaunchKernelGGL((mv_mx_product_tile_kernel<2, 2, 2, 2>), dim3(all), dim3(256), 0, st, p, q, firsts);
+            const Product  p = product_of(w[i], cut[i]);
+            const uint32_t firsts = (uint32_t)cut[i].groups();
+            const bool     mt4 = cut[i].mt == 4;
+            const dim3     threads(mt4 ? 512 : 256);
+            if (both) {
+                const Launch<Product, true> l = {{p, product_of(w[1], cut[1])}, firsts};
+                const dim3 grid(firsts + (uint32_t)cut[1].groups());
+                if (mt4) hipLaunchKernelGGL((mv_mx_product_tile_kernel<4, 2, 2, 4, true>), grid, threads, 0, st, l);
+                else hipLaunchKernelGGL((mv_mx_product_tile_kernel<2, 2, 2, 2, true>), grid, threads, 0, st, l);
+            } else {
+                const Launch<Product, false> l = {{p}, firsts};
+                if (mt4) hipLaunchKernelGGL((mv_mx_product_tile_kernel<4, 2, 2, 4, false>), dim3(firsts), threads, 0, st, l);
+                else hipLaunchKernelGGL((mv_mx_product_tile_kernel<2, 2, 2, 2, false>), dim3(firsts), threads, 0, st, l);
+            }
             launch_join(w[i], cut[i], st);
             if (both) launch_join(w[1], cut[1], st);
             if (hipGetLastError() != hipSuccess) return MV_ERR_DEVICE;
@@ -826,8 +856,8 @@ template <typename X>
 static mv_status launch_few_values(const FewCut& cut, const void* x, int64_t ld_x, int64_t m, const Factor& w, int64_t k, const Out& y,
                                    int64_t ld_y, hipStream_t st)
 {
-    return launch_few(few_product(w, Few<X>{static_cast<const X*>(x), ld_x, nullptr, 0, (uint32_t)m}, k, y, 1, ld_y), cut,
-                      FewProduct<X>{}, FewCut{}, st);
+    const FewProduct<X> p = few_product(w, Few<X>{static_cast<const X*>(x), ld_x, nullptr, 0, (uint32_t)m}, k, y, 1, ld_y);
+    return launch_few(&p, &cut, 1, st);
 }
 
 inline bool scratch_valid(const void* p, size_t have, size_t need)
