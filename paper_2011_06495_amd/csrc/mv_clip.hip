@@ -584,14 +584,14 @@ inline uint64_t chunks_of(const mv_clip_tensor& t, int bytes)
     return (uint64_t)((t.numel + per - 1) / per);
 }
 
-// False: invalid.  Allocates a word per group for the time of the call.
-bool measure(const mv_clip_config* c, const mv_clip_tensor* t, int64_t n, Sizes* s)
+// Allocates a word per group for the time of the call.
+mv_status measure(const mv_clip_config* c, const mv_clip_tensor* t, int64_t n, Sizes* s)
 {
-    if (!c || !t || c->struct_size != sizeof(mv_clip_config) || c->device < 0) return false;
-    if (c->n_groups < 1 || c->n_groups > 65535 || n < 1 || n > (1 << 24)) return false;
-    if (c->norm != MV_NORM_L2 && c->norm != MV_NORM_MAX) return false;
+    if (!c || !t || c->struct_size != sizeof(mv_clip_config) || c->device < 0) return MV_ERR_INVALID_ARG;
+    if (c->n_groups < 1 || c->n_groups > 65535 || n < 1 || n > (1 << 24)) return MV_ERR_INVALID_ARG;
+    if (c->norm != MV_NORM_L2 && c->norm != MV_NORM_MAX) return MV_ERR_INVALID_ARG;
     uint64_t* pieces = new (std::nothrow) uint64_t[(size_t)c->n_groups]();      // of each group
-    if (!pieces) return false;
+    if (!pieces) return MV_ERR_ALLOC;
     int64_t  with = 0, without = 0;
     uint64_t large = 0, small = 0, most = 0;
     bool     fine = true;
@@ -609,7 +609,7 @@ bool measure(const mv_clip_config* c, const mv_clip_tensor* t, int64_t n, Sizes*
         if (pieces[t[i].group] > most) most = pieces[t[i].group];
     }
     delete[] pieces;
-    if (!fine || (with && without) || large > kMostChunks) return false;
+    if (!fine || (with && without) || large > kMostChunks) return MV_ERR_INVALID_ARG;
     s->small = most <= (uint64_t)mvc::kSmallMost;
     s->chunk_bytes = s->small ? mvc::kSmallBytes : mvc::kChunkBytes;
     s->chunks = s->small ? small : large;
@@ -623,7 +623,7 @@ bool measure(const mv_clip_config* c, const mv_clip_tensor* t, int64_t n, Sizes*
     s->off_late = s->off_coefs + align_up(groups * sizeof(uint64_t));
     s->off_sums = s->off_late + align_up(chunks * sizeof(uint32_t));
     s->total = s->off_sums + align_up(chunks * sizeof(mvc::Sum));
-    return true;
+    return MV_OK;
 }
 
 // The lists as the device holds them; false: no memory.  `most`: a group's largest number of chunks.
@@ -680,7 +680,7 @@ extern "C" {
 size_t mv_clip_workspace_bytes(const mv_clip_config* cfg, const mv_clip_tensor* tensors, int64_t n_tensors)
 {
     Sizes s;
-    return measure(cfg, tensors, n_tensors, &s) ? s.total : 0;
+    return measure(cfg, tensors, n_tensors, &s) == MV_OK ? s.total : 0;
 }
 
 mv_status mv_clip_begin(const mv_clip_config* cfg, const mv_clip_tensor* tensors, int64_t n_tensors, mv_clip** out)
@@ -688,7 +688,7 @@ mv_status mv_clip_begin(const mv_clip_config* cfg, const mv_clip_tensor* tensors
     if (!out) return MV_ERR_INVALID_ARG;
     *out = nullptr;
     Sizes s;
-    if (!measure(cfg, tensors, n_tensors, &s)) return MV_ERR_INVALID_ARG;
+    if (const mv_status st = measure(cfg, tensors, n_tensors, &s); st != MV_OK) return st;
     if (cfg->workspace &&
         (cfg->workspace_bytes < s.total || (reinterpret_cast<uintptr_t>(cfg->workspace) & (kAlign - 1)) != 0))
         return MV_ERR_INVALID_ARG;

@@ -30,8 +30,9 @@ __device__ __forceinline__ Place place_of(uint32_t first, uint32_t more, uint32_
 // Lanes of a block, and blocks of a workgroup.
 template <typename T>
 constexpr int kBlockLanes = sizeof(T) == 2 ? 4 : 8;
+constexpr int kBf16Blocks = 2;      // of four lanes, in quantising rows
 template <typename T>
-constexpr int kGroupBlocks = kThreads / kBlockLanes<T>;
+constexpr int kGroupBlocks = kThreads / kBlockLanes<T> * (sizeof(T) == 2 ? kBf16Blocks : 1);
 
 // A matrix of values and where its codes go.
 template <typename T>
@@ -44,45 +45,69 @@ struct Encode {
     int64_t   ld_scales;
 };
 
-template <typename T, bool RESID>
-__device__ __forceinline__ void encode_rows(const Encode<T>& e, uint32_t at_group, float* resid, int64_t ld_resid)
+template <bool RESID>
+__device__ __forceinline__ void encode_rows(const Encode<float>& e, uint32_t at_group, float* resid, int64_t ld_resid)
 {
-    constexpr int kLanes = kBlockLanes<T>, V = kBlock / kLanes;
-    const uint32_t mine = threadIdx.x % kLanes;
-    const Place p = place_of(at_group * kGroupBlocks<T>, threadIdx.x / kLanes, (uint32_t)blocks_of(e.n));
+    const uint32_t mine = threadIdx.x % 8;
+    const Place p = place_of(at_group * kGroupBlocks<float>, threadIdx.x / 8, (uint32_t)blocks_of(e.n));
     if (p.row >= e.rows) return;                       // all lanes of a block
-    const int64_t at = (int64_t)p.block * kBlock + mine * V;
-    float x[V];
-    if constexpr (V == 8) load8(e.vals + p.row * e.ld_vals + at, e.n - at, x);
-    else load4(e.vals + p.row * e.ld_vals + at, e.n - at, x);
+    const int64_t at = (int64_t)p.block * kBlock + mine * 4;
+    float x[4];
+    load4(e.vals + p.row * e.ld_vals + at, e.n - at, x);
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-    const uint32_t scale = scale_of(V == 8 ? top_of_quad(top) : top_of_eight(top));
-    float held[V];
-    if constexpr (V == 8) {
-        const uint32_t w = encode8(x, scale);
-        e.codes[p.row * e.ld_words + at / 8] = w;
-        if constexpr (RESID) decode8(w, scale, held);
-    } else {
-        const uint32_t w = encode4(x, scale);
-        const uint32_t next = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0xB1, 0xf, 0xf, false);   // the neighbour's
-        if ((mine & 1u) == 0) e.codes[p.row * e.ld_words + at / 8] = w | next << 16;
-        if constexpr (RESID) decode4(w, scale, held);
-    }
+    for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    const uint32_t scale = scale_of(top_of_eight(top)), w = encode4(x, scale);
+    const uint32_t next = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0xB1, 0xf, 0xf, false);   // the neighbour's
+    if ((mine & 1u) == 0) e.codes[p.row * e.ld_words + at / 8] = w | next << 16;
     if (mine == 0) e.scales[p.row * e.ld_scales + p.block] = (uint8_t)scale;
     if constexpr (RESID) {
+        float held[4];
+        decode4(w, scale, held);
 #pragma unroll
-        for (int i = 0; i < V; ++i) held[i] = x[i] - held[i];
-        if constexpr (V == 8) store8(resid + p.row * ld_resid + at, e.n - at, held);
-        else store4(resid + p.row * ld_resid + at, e.n - at, held);
+        for (int i = 0; i < 4; ++i) held[i] = x[i] - held[i];
+        store4(resid + p.row * ld_resid + at, e.n - at, held);
+    }
+}
+
+// bf16 values stay pairs as they are; two blocks of a group of lanes are in flight together (8192 x 4096 and back 29.3 -> 27.7
+// us; with four 28.3; fp32 values, of which a block alone is as many bytes, gain nothing).
+template <bool RESID>
+__device__ __forceinline__ void encode_rows(const Encode<uint16_t>& e, uint32_t at_group, float* resid, int64_t ld_resid)
+{
+    const uint32_t mine = threadIdx.x % 4;
+    Place p[kBf16Blocks];
+    uint32_t x[kBf16Blocks][4];
+#pragma unroll
+    for (int u = 0; u < kBf16Blocks; ++u) {
+        p[u] = place_of(at_group * kGroupBlocks<uint16_t>, u * (kThreads / 4) + threadIdx.x / 4, (uint32_t)blocks_of(e.n));
+        const int64_t at = (int64_t)p[u].block * kBlock + mine * 8;
+        load8(e.vals + p[u].row * e.ld_vals + at, p[u].row < e.rows ? e.n - at : 0, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kBf16Blocks; ++u) {
+        if (p[u].row >= e.rows) break;
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = top2(top, x[u][i]);
+        const uint32_t scale = scale_of(top_of_quad(top_of_pair(top))), w = encode8(x[u], scale);
+        e.codes[p[u].row * e.ld_words + p[u].block * 4 + mine] = w;
+        if (mine == 0) e.scales[p[u].row * e.ld_scales + p[u].block] = (uint8_t)scale;
+        if constexpr (RESID) {
+            const int64_t at = (int64_t)p[u].block * kBlock + mine * 8;
+            float held[8];
+            decode8(w, scale, held);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) held[i] = widen(x[u][i / 2] >> (16 * (i & 1))) - held[i];
+            store8(resid + p[u].row * ld_resid + at, e.n - at, held);
+        }
     }
 }
 
 template <typename T, bool RESID>
 __global__ __launch_bounds__(kThreads) void mv_mx_encode_kernel(Encode<T> e, float* resid, int64_t ld_resid)
 {
-    encode_rows<T, RESID>(e, blockIdx.x, resid, ld_resid);
+    encode_rows<RESID>(e, blockIdx.x, resid, ld_resid);
 }
 
 // Columns: a wavefront takes 32 rows of 16 bytes of columns in each group of four lanes; lane r of a group has rows
@@ -167,7 +192,7 @@ __global__ __launch_bounds__(kThreads) void mv_mx_encode_grad_kernel(Encode<T> x
     const uint32_t b = blockIdx.x;
     if (b < x_t_groups) encode_columns<T>(x_t, b, out);
     else if (b < x_t_groups + dy_t_groups) encode_columns<T>(dy_t, b - x_t_groups, out);
-    else encode_rows<T, false>(dy, b - x_t_groups - dy_t_groups, nullptr, 0);
+    else encode_rows<false>(dy, b - x_t_groups - dy_t_groups, nullptr, 0);
 }
 
 template <typename T>
@@ -177,7 +202,7 @@ __global__ __launch_bounds__(kThreads) void mv_mx_decode_kernel(const uint32_t* 
 {
     constexpr int kLanes = kBlockLanes<T>, V = kBlock / kLanes;
     const uint32_t mine = threadIdx.x % kLanes;
-    const Place p = place_of(blockIdx.x * kGroupBlocks<T>, threadIdx.x / kLanes, (uint32_t)blocks_of(n));
+    const Place p = place_of(blockIdx.x * (kThreads / kLanes), threadIdx.x / kLanes, (uint32_t)blocks_of(n));
     if (p.row >= rows) return;
     const int64_t at = (int64_t)p.block * kBlock + mine * V;
     const uint32_t w = codes[p.row * ld_words + at / 8], scale = scales[p.row * ld_scales + p.block];
@@ -229,16 +254,16 @@ static Encode<T> encode_of(const Values& v, const Held& to)
 {
     return {static_cast<const T*>(v.p), v.ld, v.rows, v.n, to.codes, to.ld_words, to.scales, to.ld_scales};
 }
-static int64_t row_groups(int64_t rows, int64_t n, int32_t dtype)
+static int64_t groups_of(int64_t rows, int64_t n, int64_t per) { return (rows * blocks_of(n) + per - 1) / per; }
+static int64_t row_groups(const Values& v, int32_t dtype)
 {
-    const int64_t per = dtype == MV_BF16 ? kGroupBlocks<uint16_t> : kGroupBlocks<float>;
-    return (rows * blocks_of(n) + per - 1) / per;
+    return groups_of(v.rows, v.n, dtype == MV_BF16 ? kGroupBlocks<uint16_t> : kGroupBlocks<float>);
 }
 
 mv_status launch_encode(const Values& v, int32_t dtype, const Held& to, float* resid, int64_t ld_resid, hipStream_t st)
 {
     if (!count_valid(v.rows, v.n)) return MV_ERR_INVALID_ARG;
-    const dim3 grid((uint32_t)row_groups(v.rows, v.n, dtype)), threads(kThreads);
+    const dim3 grid((uint32_t)row_groups(v, dtype)), threads(kThreads);
 #define MV_MX_ENCODE(T, R) hipLaunchKernelGGL((mv_mx_encode_kernel<T, R>), grid, threads, 0, st, encode_of<T>(v, to), resid, ld_resid)
     if (dtype == MV_BF16) {
         if (resid) MV_MX_ENCODE(uint16_t, true);
@@ -268,7 +293,7 @@ template <typename T>
 static mv_status launch_encode_grad_of(const Values& x, const Held* x_t, const Values& dy, const Held* dy_t, const Held* dy_r, hipStream_t st)
 {
     const int64_t a = x_t ? column_groups<T>(x.rows, x.n) : 0, b = dy_t ? column_groups<T>(dy.rows, dy.n) : 0;
-    const int64_t c = dy_r ? row_groups(dy.rows, dy.n, sizeof(T) == 2 ? MV_BF16 : MV_F32) : 0;
+    const int64_t c = dy_r ? row_groups(dy, sizeof(T) == 2 ? MV_BF16 : MV_F32) : 0;
     if ((dy_r && !count_valid(dy.rows, dy.n)) || a + b + c > kMostGroups) return MV_ERR_INVALID_ARG;
     const Encode<T> none = {};
     hipLaunchKernelGGL(mv_mx_encode_grad_kernel<T>, dim3((uint32_t)(a + b + c)), dim3(kThreads), 0, st,
@@ -321,7 +346,7 @@ mv_status mv_mx_decode(const uint32_t* codes, int64_t ld_words, const uint8_t* s
         !codes_valid(codes, ld_words, scales, ld_scales, n))
         return MV_ERR_INVALID_ARG;
     if (!count_valid(rows, n)) return MV_ERR_INVALID_ARG;
-    const dim3 grid((uint32_t)row_groups(rows, n, dtype)), threads(kThreads);
+    const dim3 grid((uint32_t)groups_of(rows, n, kThreads / (dtype == MV_BF16 ? kBlockLanes<uint16_t> : kBlockLanes<float>))), threads(kThreads);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (dtype == MV_BF16)
         hipLaunchKernelGGL(mv_mx_decode_kernel<uint16_t>, grid, threads, 0, st, codes, ld_words, scales, ld_scales, rows, n,

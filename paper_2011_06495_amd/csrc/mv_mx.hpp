@@ -51,6 +51,18 @@ __device__ __forceinline__ void load8(const uint16_t* p, int64_t live, float (&x
         for (int i = 0; i < 8; ++i) x[i] = i < live ? widen(p[i]) : 0.0f;
     }
 }
+// As they are.
+__device__ __forceinline__ void load8(const uint16_t* p, int64_t live, uint32_t (&x)[4])
+{
+    if (live >= 8) {
+        const u32x4u a = *reinterpret_cast<const u32x4u*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = a[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (2 * i < live ? p[2 * i] : 0u) | (2 * i + 1 < live ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+    }
+}
 __device__ __forceinline__ void load4(const float* p, int64_t live, float (&x)[4])
 {
     if (live >= 4) {

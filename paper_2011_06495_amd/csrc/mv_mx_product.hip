@@ -214,8 +214,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Lau
     const uint32_t b_at = (wave * (kN / kWaves) + (lane >> 3)) * b_pitch + my_block * 16u;
     auto load_codes = [&](uint32_t k, Codes& to) {
         const uint32_t step = step0 + k;
-        // The whole offset is the lane's own, for the bounds to hold: below 2^30 + 2^21, and beyond every buffer where the
-        // row has no such block.
+        // The whole offset is the lane's own, for the bounds to hold: beyond every buffer where the row has no such block.
         const bool live = step * kStepBlocks + my_block < end;
         const uint32_t av = live ? a_at + step * 128u : 0x80000000u, bv = live ? b_at + step * 128u : 0x80000000u;
 #pragma unroll
@@ -779,7 +778,15 @@ static FewProduct<uint32_t> few_codes(const Wanted& w, bool few_a)
     return few_product(few_a ? w.b : w.a, Few<uint32_t>{few.codes, few.ld_words, few.scales, few.ld_scales, (uint32_t)few.rows}, w.k, w.c,
                        few_a ? 1 : w.ld_c, few_a ? w.ld_c : 1);
 }
-static bool offsets_fit(const Wanted& w) { return w.a.ld_words * 4 <= (1 << 22) && w.b.ld_words * 4 <= (1 << 22); }
+// Whether a tile's byte offsets fit 32 bits: those of rows that there are stay below 2^31, where the loads of blocks that there
+// are not begin, and those of all rows of a tile below 2^32.
+static bool offsets_fit(const Factor& f, int64_t blocks, int mt)
+{
+    const int64_t pitch = f.ld_words * 4, rows = f.rows < 64 * mt ? f.rows : 64 * mt;
+    return pitch <= ((int64_t)1 << (mt == 4 ? 23 : 24)) && (rows - 1) * pitch + blocks * 16 <= ((int64_t)1 << 31) - 256 &&
+           f.ld_scales <= (1 << 22);
+}
+static bool offsets_fit(const Wanted& w, int mt) { return offsets_fit(w.a, blocks_of(w.k), mt) && offsets_fit(w.b, blocks_of(w.k), mt); }
 
 // Up to two products (n: how many) in as few launches as their sizes allow.
 static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
@@ -795,9 +802,9 @@ static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
     Cut  cut[2] = {};
     bool tiled[2] = {};
     for (int i = 0; i < n; ++i) {
-        tiled[i] = !few[i].mt && offsets_fit(w[i]);
+        tiled[i] = !few[i].mt && offsets_fit(w[i], 2);
         if (tiled[i]) {
-            cut[i] = cut_of(w[i].a.rows, w[i].b.rows, w[i].k, large(w[i].a.rows, w[i].b.rows) ? 4 : 2);
+            cut[i] = cut_of(w[i].a.rows, w[i].b.rows, w[i].k, large(w[i].a.rows, w[i].b.rows) && offsets_fit(w[i], 4) ? 4 : 2);
             if (cut[i].groups() > kMostGroups / 2) return MV_ERR_INVALID_ARG;
         }
     }

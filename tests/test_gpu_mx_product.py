@@ -250,3 +250,34 @@ def test_python_refusals():
     with pytest.raises(B.MvError) as e:
         B.mv_mx_linear(x, c, s, y, scratch[:1])
     assert e.value.status == B.MV_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 5, 9_000_001), (20, 18, 2_000_033)])
+def test_long_sums_of_few_rows(m, n, k):
+    """The products of workers' whole gradients with each other: k is the long side, split over the units."""
+    rng = np.random.default_rng(k)
+    base = rng.standard_normal(4099).astype(np.float32)
+    x, y = (np.stack([np.roll(np.resize(base, k), 7 * r + s) for r in range(rows)]) for rows, s in ((m, 0), (n, 3)))
+    a_codes, a_scales, a = hold(x)
+    b_codes, b_scales, b = hold(y)
+    out = torch.zeros((m, n), device="cuda")
+    B.mv_mx_product(a_codes, a_scales, b_codes, b_scales, k, out, scratch_of(B.mv_mx_product_scratch_bytes(m, n, k)))
+    check(out, a, b, torch.float32)
+
+
+@pytest.mark.parametrize("words,places", [((1 << 20) + 4, 64), ((1 << 22) + 4, 64), (64, (1 << 22) + 4)])
+def test_rows_far_apart(words, places):
+    """Rows of codes 4 and 16 MB apart, and rows of scales 4 MB: offsets inside a tile near and beyond 32 bits."""
+    m, n, k = 40, 20, 300
+    rng = np.random.default_rng(words)
+    a_codes, a_scales, a = hold(normal(rng, m, k))
+    b_codes, b_scales, b = hold(normal(rng, n, k))
+    far = torch.zeros((m, words), dtype=torch.int32, device="cuda")
+    far_scales = torch.zeros((m, places), dtype=torch.uint8, device="cuda")
+    far[:, :40] = a_codes[:, :40]
+    far_scales[:, :12] = a_scales[:, :12]
+    for first in (True, False):
+        out = torch.zeros((m, n) if first else (n, m), device="cuda")
+        sides = (far, far_scales, b_codes, b_scales) if first else (b_codes, b_scales, far, far_scales)
+        B.mv_mx_product(*sides, k, out, scratch_of(B.mv_mx_product_scratch_bytes(*out.shape, k)))
+        check(out, a, b, torch.float32) if first else check(out, b, a, torch.float32)
