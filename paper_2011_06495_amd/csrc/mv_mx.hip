@@ -4,6 +4,9 @@
 // All of these read and write each value once and compute a few instructions on it: HBM bounds them, launches where they
 // are short.  A lane takes 16 bytes of values, so a wavefront's loads and stores cover one run of memory: four lanes a
 // block of 32 bf16 values, eight lanes one of fp32; the block's largest magnitude is two or three DPP moves away.
+// 16 x 11.2 M fp32 to codes and residual 247 us, 6.2 TB/s; 4096 x 8192 bf16 to codes 20 us, 4.2 TB/s (in a loop with a
+// product whose 67 MB of results are still on their way to memory); the mean of 16 x 11.2 M 33 us, 4.3 TB/s; 8192 x 4096
+// codes back to bf16 13 us, 6.5 TB/s, the codes out of the last-level cache.
 #include "mv_mx.hpp"
 
 namespace mvx {
@@ -113,6 +116,8 @@ __global__ __launch_bounds__(kThreads) void mv_mx_encode_kernel(Encode<T> e, flo
 // Columns: a wavefront takes 32 rows of 16 bytes of columns in each group of four lanes; lane r of a group has rows
 // 8 r .. 8 r + 8, of each column a word of codes, and the block's largest magnitude is two DPP moves away again.  The
 // codes of kTileBlocks wavefronts, one below the other, go out through LDS in runs of 16 kTileBlocks bytes a column.
+// Memory is the bound: 8192 x 4096 bf16 18 us, 4.7 TB/s.  Whole lines, by eight wavefronts, change nothing (bf16 17.9 : 17.9,
+// fp32 35.3 : 33.9, but 300 x 1000 5.9 : 6.3 and 3.8 : 4.5).
 constexpr int kTileBlocks = 4;
 template <typename T>
 constexpr int kLaneCols = 16 / (int)sizeof(T);
@@ -132,7 +137,10 @@ struct Columns {                    // of a workgroup: codes and scales on their
 template <typename T>
 inline int64_t column_tiles(int64_t n) { return (n + kTileCols<T> - 1) / kTileCols<T>; }
 template <typename T>
-inline int64_t column_groups(int64_t rows, int64_t n) { return column_tiles<T>(n) * ((blocks_of(rows) + kTileBlocks - 1) / kTileBlocks); }
+inline int64_t column_groups(int64_t rows, int64_t n)
+{
+    return column_tiles<T>(n) * ((blocks_of(rows) + kTileBlocks - 1) / kTileBlocks);
+}
 
 template <typename T>
 __device__ __forceinline__ void encode_columns(const Encode<T>& e, uint32_t at_group, Columns<T>& out)
@@ -170,7 +178,8 @@ __device__ __forceinline__ void encode_columns(const Encode<T>& e, uint32_t at_g
             // four scales in one store where there are four
             const bool whole = ((int64_t)strip + 1) * kTileBlocks <= blocks_of(e.rows);
             if (!whole) e.scales[to * e.ld_scales + to_block] = out.scales[c][b];
-            else if (b == 0) *reinterpret_cast<uint32_t*>(e.scales + to * e.ld_scales + to_block) = *reinterpret_cast<const uint32_t*>(out.scales[c]);
+            else if (b == 0)
+                *reinterpret_cast<uint32_t*>(e.scales + to * e.ld_scales + to_block) = *reinterpret_cast<const uint32_t*>(out.scales[c]);
         }
     }
 }
@@ -183,6 +192,7 @@ __global__ __launch_bounds__(64 * kTileBlocks) void mv_mx_encode_t_kernel(Encode
 }
 
 // What a layer's gradients need, in one launch: columns of x, columns of dy, rows of dy; none of a kind: no workgroups.
+// x 4900 x 4608 and dy 4900 x 512, bf16: 66 MB in 17 us, or 27 right behind a product whose 100 MB are still being stored.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void mv_mx_encode_grad_kernel(Encode<T> x_t, uint32_t x_t_groups, Encode<T> dy_t,
                                                                      uint32_t dy_t_groups, Encode<T> dy)
