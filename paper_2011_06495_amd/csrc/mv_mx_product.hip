@@ -121,17 +121,19 @@ __global__ __launch_bounds__(kProductThreads) void mv_mx_product_kernel(Factor a
 // ---- tiles through LDS ---------------------------------------------------------------------------------------------
 //
 // A workgroup of WM x WN wavefronts takes 32 MT WM x 32 NT WN results, 32 MT x 32 NT a wavefront, in steps of eight
-// blocks (256 values, 128 bytes a row).  The rows of both factors go from memory straight into LDS, each row's 16-byte blocks in the order
-// block ^ (row % 8): what eight lanes of neighbouring rows read together lies in different banks, and what eight lanes
-// write together is one whole line of memory.  Two buffers: the next step's loads are in flight during this one's
-// products.  Loads beyond the last row or block return zeros by the buffer's bounds.  The scales of two steps, 16 bytes a row,
-// go through registers, where those behind the last block become 1, into LDS of their own.
+// blocks (256 values, 128 bytes a row).  The rows of both factors go from memory straight into LDS, each row's
+// 16-byte blocks in the order block ^ (row % 8): what eight lanes of neighbouring rows read together lies in
+// different banks, and what eight lanes write together is one whole line of memory.  Two buffers: the next step's
+// loads are in flight during this one's products.  With few steps, one buffer, and the unit's other workgroups fill
+// the waiting.  Loads beyond the last row or block return zeros by the buffer's bounds.  The scales of two steps, 16
+// bytes a row, go through registers, where those behind the last block become 1, into LDS of their own.
 //
 // A lane of the 32 x 32 x 64 instruction holds half of a row's eight blocks: blocks 4 (lane / 32) + s of step s, whose
 // scales are one word.
 // 4096 x 8192 by 8192, bf16 results: 139 us, 4.0 PFLOP/s.  The instructions alone, out of registers, reach 8.4 on small
 // numbers and 6.2 to 6.7 on random codes, where power bounds them; the rest is the reads from LDS beside them and the end,
-// where 67 MB leave.  With 512 values of k the results are all: 4900 x 512 by 4608 to fp32 26 us, a fill of those 90 MB 15.5.
+// where 67 MB leave.  With 512 values of k the results are all: 4900 x 512 by 4608 to fp32 26 us with the launch
+// that quantises (4), a fill of those 90 MB 15.5.
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -184,15 +186,14 @@ struct Rows {
     u32x4 x[MT], y[NT];
 };
 
-template <int MT, int NT, int WM, int WN, bool PAIR>
-__global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Launch<Product, PAIR> l)
+template <int MT, int NT, int WM, int WN, int BUFFERS, bool PAIR>
+__global__ __launch_bounds__(64 * WM * WN, BUFFERS == 1 ? 3 : 2) void mv_mx_product_tile_kernel(Launch<Product, PAIR> l)
 {
     constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
     constexpr int kM = 32 * MT * WM, kN = 32 * NT * WN, kRows = kM + kN;
     typedef uint8_t Codes[kRows * 128];
-    // two variables, not an array of two: reads of one need not wait for the loads into the other
-    __shared__ __attribute__((aligned(1024))) Codes even, odd;
-    __shared__ uint8_t scales[2][kRows * kScalePitch];
+    __shared__ __attribute__((aligned(1024))) Codes even;
+    __shared__ uint8_t scales[BUFFERS][kRows * kScalePitch];
     const uint32_t t = threadIdx.x, lane = t & 63u, wave = __builtin_amdgcn_readfirstlane(t / 64);
     const Product& p = l.product();
     const Factor a = p.a, b = p.b;
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Lau
         for (int w = 0; w < 4; ++w) {
             const int live = (int)end - (int)((step0 + 2 * pair) * kStepBlocks + 4 * w);
             const uint32_t real = live >= 4 ? 0xFFFFFFFFu : live > 0 ? (1u << (8 * live)) - 1u : 0u;
-            *reinterpret_cast<uint32_t*>(&scales[pair & 1u][t * kScalePitch + 4 * w]) = (next[w] & real) | (0x7F7F7F7Fu & ~real);
+            *reinterpret_cast<uint32_t*>(&scales[pair % BUFFERS][t * kScalePitch + 4 * w]) = (next[w] & real) | (0x7F7F7F7Fu & ~real);
         }
     };
 
@@ -266,7 +267,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Lau
         for (int i = 0; i < NT; ++i) r.y[i] = *reinterpret_cast<const u32x4*>(from + (b_row + 32 * i) * 128 + slot);
     };
     auto read_scales = [&](uint32_t k) {
-        const uint8_t* sc = scales[k >> 1 & 1u] + (k & 1u) * 8 + half * 4;
+        const uint8_t* sc = scales[k / 2 % BUFFERS] + (k & 1u) * 8 + half * 4;
 #pragma unroll
         for (int i = 0; i < MT; ++i) as_next[i] = *reinterpret_cast<const uint32_t*>(sc + (a_row + 32 * i) * kScalePitch);
 #pragma unroll
@@ -307,33 +308,51 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mv_mx_product_tile_kernel(Lau
         products(std::integral_constant<int, 3>{}, two);
         __builtin_amdgcn_sched_barrier(0);
     };
-    load_codes(0, even);
-    fetch_scales(0);
-    keep_scales(0);
-    all_here();
-    load_codes(1, odd);
-    read_rows(even, 0, one);
-    read_scales(0);
-    // Two steps a turn.  Before a step's last products come the next one's first rows, so those products cover the way
-    // from LDS, and the loads into this step's buffer begin as soon as all wavefronts have read it.  The turn has no
-    // branches, or the compiler moves products past them and runs out of registers: behind the last step zeros are loaded.
-    for (uint32_t k = 0; k < count; k += 2) {
-        most_of_step(even);
+    if constexpr (BUFFERS == 1) {
+        for (uint32_t k = 0; k < count; ++k) {
+            load_codes(k, even);
+            if (k % 2 == 0) {
+                fetch_scales(k);
+                keep_scales(k / 2);
+            }
+            all_here();
+            read_rows(even, 0, one);
+            read_scales(k);
+            most_of_step(even);
+            last_of_step();
+            __syncthreads();
+        }
+    } else {
+        // two variables, not an array of two: reads of one need not wait for the loads into the other
+        __shared__ __attribute__((aligned(1024))) Codes odd;
+        load_codes(0, even);
+        fetch_scales(0);
+        keep_scales(0);
         all_here();
-        read_rows(odd, 0, one);
-        read_scales(k + 1);
-        fetch_scales(k + 2);
-        load_codes(k + 2, even);
-        last_of_step();
-        most_of_step(odd);
-        keep_scales(k / 2 + 1);
-        all_here();
+        load_codes(1, odd);
         read_rows(even, 0, one);
-        read_scales(k + 2);
-        load_codes(k + 3, odd);
-        last_of_step();
+        read_scales(0);
+        // Two steps a turn.  Before a step's last products come the next one's first rows, so those products cover the way
+        // from LDS, and the loads into this step's buffer begin as soon as all wavefronts have read it.  The turn has no
+        // branches, or the compiler moves products past them and runs out of registers: behind the last step zeros are loaded.
+        for (uint32_t k = 0; k < count; k += 2) {
+            most_of_step(even);
+            all_here();
+            read_rows(odd, 0, one);
+            read_scales(k + 1);
+            fetch_scales(k + 2);
+            load_codes(k + 2, even);
+            last_of_step();
+            most_of_step(odd);
+            keep_scales(k / 2 + 1);
+            all_here();
+            read_rows(even, 0, one);
+            read_scales(k + 2);
+            load_codes(k + 3, odd);
+            last_of_step();
+        }
+        __builtin_amdgcn_s_waitcnt(kNoLoads);
     }
-    __builtin_amdgcn_s_waitcnt(kNoLoads);
 
     // A lane has, of 32 rows, four times four consecutive columns.  32 rows of the wavefront's 64 columns at a time go
     // through its part of LDS, 16-byte units in the order unit ^ (row % 16), and out in whole runs of a row.
@@ -719,6 +738,12 @@ static Cut cut_of(int64_t m, int64_t n, int64_t k, int mt, int64_t beside = 0)
     c.splits = (uint32_t)((steps + c.steps_each - 1) / c.steps_each);
     return c;
 }
+// Up to four steps and more tiles of 128 x 128 than units: one buffer and three workgroups a unit, of which one loads or
+// stores while another multiplies.  bf16, with the launch that quantises, before -> with: 4900 x 256 by 4608 24.8 -> 17.0 us,
+// x 512 25.4 -> 20.8, x 1024 32.3 -> 27.6, x 2048 44.5 here; 4096 x 1024 by 8192 35.5 : 35.6, x 2048 56.0 : 60.2; 2500 x 512 by
+// 2500, 400 tiles, 12.5 -> 11.8; 2000 x 512 by 2000, 256 tiles, 10.1 : 10.4.
+constexpr int64_t kFewSteps = 4, kUnits = 256;
+inline bool few_steps(int64_t k) { return blocks_of(k) <= kFewSteps * kStepBlocks; }
 static bool large(int64_t m, int64_t n) { return ((m + 255) / 256) * ((n + 255) / 256) >= 192; }
 inline int64_t quads_of(int64_t n) { return (n + 3) / 4; }
 inline size_t parts_bytes(int64_t m, int64_t n, int64_t k)
@@ -793,6 +818,15 @@ static bool offsets_fit(const Factor& f, int64_t blocks, int mt)
 }
 static bool offsets_fit(const Wanted& w, int mt) { return offsets_fit(w.a, blocks_of(w.k), mt) && offsets_fit(w.b, blocks_of(w.k), mt); }
 
+template <bool PAIR>
+static void launch_tiles(const Launch<Product, PAIR>& l, int mt, bool one_buffer, uint32_t groups, hipStream_t st)
+{
+    const dim3 grid(groups), threads(mt == 4 ? 512 : 256);
+    if (mt == 4) hipLaunchKernelGGL((mv_mx_product_tile_kernel<4, 2, 2, 4, 2, PAIR>), grid, threads, 0, st, l);
+    else if (one_buffer) hipLaunchKernelGGL((mv_mx_product_tile_kernel<2, 2, 2, 2, 1, PAIR>), grid, threads, 0, st, l);
+    else hipLaunchKernelGGL((mv_mx_product_tile_kernel<2, 2, 2, 2, 2, PAIR>), grid, threads, 0, st, l);
+}
+
 // Up to two products (n: how many) in as few launches as their sizes allow.
 static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
 {
@@ -814,11 +848,22 @@ static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
         }
     }
     const bool both = tiled[0] && tiled[1];
-    // in one launch: the smaller tiles for both, and each other's tiles to fill the units with
-    if (both && (cut[0].mt == 2 || cut[1].mt == 2)) {
-        const int64_t tiles[2] = {cut_of(w[0].a.rows, w[0].b.rows, w[0].k, 2, 512).groups(),
-                                  cut_of(w[1].a.rows, w[1].b.rows, w[1].k, 2, 512).groups()};
-        for (int i = 0; i < 2; ++i) cut[i] = cut_of(w[i].a.rows, w[i].b.rows, w[i].k, 2, tiles[1 - i]);
+    bool       one_buffer = true;
+    int64_t    all = 0;
+    for (int i = 0; i < n; ++i)
+        if (tiled[i]) {
+            const Cut c = cut_of(w[i].a.rows, w[i].b.rows, w[i].k, 2);
+            one_buffer &= few_steps(w[i].k);
+            all += c.tiles_m * c.tiles_n;
+        }
+    one_buffer &= all > kUnits && all <= kMostGroups;
+    // with one buffer: the smaller tiles; in one launch: those for both, and each other's tiles to fill the units with
+    if (one_buffer || (both && (cut[0].mt == 2 || cut[1].mt == 2))) {
+        int64_t tiles[2] = {};
+        for (int i = 0; i < n; ++i)
+            if (tiled[i]) tiles[i] = cut_of(w[i].a.rows, w[i].b.rows, w[i].k, 2, 512).groups();
+        for (int i = 0; i < n; ++i)
+            if (tiled[i]) cut[i] = cut_of(w[i].a.rows, w[i].b.rows, w[i].k, 2, tiles[1 - i]);
         if (cut[0].groups() + cut[1].groups() > kMostGroups) return MV_ERR_INVALID_ARG;
     }
     for (int i = 0; i < n; ++i) {
@@ -829,17 +874,11 @@ static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
         } else if (!both || i == 0) {
             const Product  p = product_of(w[i], cut[i]);
             const uint32_t firsts = (uint32_t)cut[i].groups();
-            const bool     mt4 = cut[i].mt == 4;
-            const dim3     threads(mt4 ? 512 : 256);
             if (both) {
                 const Launch<Product, true> l = {{p, product_of(w[1], cut[1])}, firsts};
-                const dim3 grid(firsts + (uint32_t)cut[1].groups());
-                if (mt4) hipLaunchKernelGGL((mv_mx_product_tile_kernel<4, 2, 2, 4, true>), grid, threads, 0, st, l);
-                else hipLaunchKernelGGL((mv_mx_product_tile_kernel<2, 2, 2, 2, true>), grid, threads, 0, st, l);
+                launch_tiles(l, cut[i].mt, one_buffer, firsts + (uint32_t)cut[1].groups(), st);
             } else {
-                const Launch<Product, false> l = {{p}, firsts};
-                if (mt4) hipLaunchKernelGGL((mv_mx_product_tile_kernel<4, 2, 2, 4, false>), dim3(firsts), threads, 0, st, l);
-                else hipLaunchKernelGGL((mv_mx_product_tile_kernel<2, 2, 2, 2, false>), dim3(firsts), threads, 0, st, l);
+                launch_tiles(Launch<Product, false>{{p}, firsts}, cut[i].mt, one_buffer, firsts, st);
             }
             launch_join(w[i], cut[i], st);
             if (both) launch_join(w[1], cut[1], st);

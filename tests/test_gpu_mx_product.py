@@ -281,3 +281,31 @@ def test_rows_far_apart(words, places):
         sides = (far, far_scales, b_codes, b_scales) if first else (b_codes, b_scales, far, far_scales)
         B.mv_mx_product(*sides, k, out, scratch_of(B.mv_mx_product_scratch_bytes(*out.shape, k)))
         check(out, a, b, torch.float32) if first else check(out, b, a, torch.float32)
+
+
+@pytest.mark.parametrize("dst", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(2100, 2070, 20), (2049, 2100, 257), (1030, 4500, 768), (2500, 2100, 1000), (2100, 2200, 1056),
+                                   (3600, 3500, 1100)])
+def test_many_tiles(m, n, k, dst):
+    """More tiles than units, with few steps along k and with more of them, and the large tiles."""
+    rng = np.random.default_rng(m + n + k)
+    a_codes, a_scales, a = hold(normal(rng, m, k))
+    b_codes, b_scales, b = hold(normal(rng, n, k))
+    out = torch.full((m + 1, n + 3), 7.5, dtype=TYPES[dst], device="cuda")
+    B.mv_mx_product(a_codes, a_scales, b_codes, b_scales, k, out[:m, 1:n + 1], scratch_of(B.mv_mx_product_scratch_bytes(m, n, k)))
+    check(out[:m, 1:n + 1], a, b, TYPES[dst])
+    o = out.float().cpu().numpy()
+    o[:m, 1:n + 1] = 7.5
+    assert (o == 7.5).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(1000, 130, 4500), (300, 900, 5000), (2000, 1100, 1300)])
+def test_gradients_of_many_tiles(m, n, k):
+    rng = np.random.default_rng(m + n + k)
+    x, dy = torch.from_numpy(normal(rng, m, k)).cuda().bfloat16(), torch.from_numpy(normal(rng, m, n)).cuda().bfloat16()
+    wt_codes, wt_scales, wt = hold(normal(rng, k, n))
+    dx, dw = torch.zeros((m, k), device="cuda"), torch.zeros((n, k), device="cuda")
+    B.mv_mx_linear_grad(x, dy, wt_codes, wt_scales, dx, dw, scratch_of(B.mv_mx_linear_grad_scratch_bytes(m, n, k)))
+    x32, dy32 = x.float().cpu().numpy(), dy.float().cpu().numpy()
+    check(dx, R.held(dy32), wt, torch.float32)
+    check(dw, R.held(np.ascontiguousarray(dy32.T)), R.held(np.ascontiguousarray(x32.T)), torch.float32)
