@@ -424,8 +424,9 @@ __global__ __launch_bounds__(256) void mv_mx_product_join_kernel(const float* __
 // 16 and block 4 s + l / 16 of the turn, s = 0 .. 3: the four lanes of a row read 64 bytes in a row; the scales of a
 // lane's four blocks are picked from the row's 16. The few rows' codes and scales are in LDS: copied there, or
 // quantised by every workgroup for itself, a lane a block, while the first turn's codes are on their way.
-// 5 x 8192 bf16 by 16,384: 18.8 us for 71.5 MB, 3.8 TB/s: the few rows' way into LDS is a good part of it.  1 x 2048 by 1000
-// 4.0, which is a launch.
+// Loads in flight are what it lives on: codes of two turns are asked for before the first are needed, behind what LDS gets.
+// 5 x 8192 bf16 by 16,384: 18.0 us for 71.5 MB, 4.0 TB/s (one turn, and the scales one word after the other, 19.8); 4 x 8192 by
+// 8192 10.4 (12.6).  1 x 2048 by 1000 3.9, which is a launch.
 
 constexpr int kTurn = 16;           // blocks
 constexpr int kFewWaves = 8;
@@ -464,8 +465,15 @@ struct Block<float> {
     float x[4][8];
     __device__ __forceinline__ void fetch(const Few<float>& f, uint32_t row, uint32_t block, int64_t k)
     {
+        const float* p = f.rows + row * f.ld + (int64_t)block * kBlock;
+        const int64_t live = k - (int64_t)block * kBlock;
+        if (live >= kBlock) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) load8(f.rows + row * f.ld + (int64_t)block * kBlock + 8 * q, k - (int64_t)block * kBlock - 8 * q, x[q]);
+            for (int q = 0; q < 4; ++q) load8(p + 8 * q, 8, x[q]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) load8(p + 8 * q, live - 8 * q, x[q]);
+        }
     }
     __device__ __forceinline__ void finish(u32x4& codes, uint32_t& s) const
     {
@@ -486,19 +494,22 @@ struct Block<uint16_t> {
     {
         const uint16_t* p = f.rows + row * f.ld + (int64_t)block * kBlock;
         const int64_t live = k - (int64_t)block * kBlock;
+        if (live >= kBlock) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (live >= kBlock) {
+            for (int q = 0; q < 4; ++q) {
                 const u32x4u v = *reinterpret_cast<const u32x4u*>(p + 8 * q);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[q][i] = v[i];
-            } else {
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int at = 8 * q + 2 * i;
                     x[q][i] = (at < live ? p[at] : 0u) | (at + 1 < live ? (uint32_t)p[at + 1] << 16 : 0u);
                 }
-            }
+        }
     }
     __device__ __forceinline__ void finish(u32x4& codes, uint32_t& s) const
     {
@@ -551,57 +562,90 @@ __global__ __launch_bounds__(64 * kFewWaves) void mv_mx_product_few_kernel(Launc
     uint8_t* held_scales = held + few.count * pitch;
     uint8_t* many_scales = held_scales + few.count * row_blocks;
 
-    // Loads come back in their order, so what LDS gets is asked for first: the thread's first block of the few rows ...
-    Block<X> mine;
+    // Loads come back in their order, so all that goes into LDS is asked for first, several pieces of a thread at once: the
+    // few rows' blocks ...
+    constexpr uint32_t kFirst = 2;
+    Block<X> mine[kFirst];
     const uint32_t few_blocks = few.count * row_blocks;
-    auto fetch = [&](uint32_t at) {
+    auto fetch = [&](uint32_t at, Block<X>& b) {
         const uint32_t row = at / row_blocks, block = at - row * row_blocks;
-        if (at < few_blocks && block < blocks) mine.fetch(few, row, block, k);
+        if (at < few_blocks && block < blocks) b.fetch(few, row, block, k);
     };
-    auto hold = [&](uint32_t at) {
+    auto hold = [&](uint32_t at, const Block<X>& b) {
+        if (at >= few_blocks) return;
         const uint32_t row = at / row_blocks, block = at - row * row_blocks;
         u32x4 codes = {0u, 0u, 0u, 0u};
         uint32_t scale = 127;
-        if (block < blocks) mine.finish(codes, scale);
+        if (block < blocks) b.finish(codes, scale);
         *reinterpret_cast<u32x4*>(held + row * pitch + block * 16) = codes;
         // block 4 s + g of a turn is byte s of word g
         held_scales[row * row_blocks + (block & ~15u) + (block & 3u) * 4 + (block >> 2 & 3u)] = (uint8_t)scale;
     };
-    fetch(threadIdx.x);
-    // ... and the many rows' scales, a word a thread; those behind the last block are 1
-    const uint32_t row_words = row_blocks / 4, last_word = (blocks - 1) / 4;
-    for (uint32_t at = threadIdx.x; at < 16 * NT * row_words; at += blockDim.x) {
-        const uint32_t r = at / row_words, word = at - r * row_words;
+    // ... and the many rows' scales, a turn's 16; those behind the last block are 1
+    const uint32_t many_turns = 16 * NT * turns, last_word = (blocks - 1) / 4;
+    auto fetch_scales = [&](uint32_t at, u32x4& w) {
+        const uint32_t r = at / turns, word = (at - r * turns) * 4;
         const int64_t j = j0 + r < many.rows ? j0 + r : many.rows - 1;
-        uint32_t w = word <= last_word ? *reinterpret_cast<const uint32_t*>(many.scales + j * many.ld_scales + 4 * word) : 0x7F7F7F7Fu;
-        const uint32_t live = blocks - 4 * word;
-        if (word == last_word && live < 4) w = (w & ((1u << (8 * live)) - 1u)) | (0x7F7F7F7Fu & ~((1u << (8 * live)) - 1u));
-        *reinterpret_cast<uint32_t*>(many_scales + r * many_pitch(turns) + 4 * word) = w;
-    }
-    // then the first turn's codes; what lies behind the last block is some block's, and meets zeros of the few rows
+        const uint32_t* from = reinterpret_cast<const uint32_t*>(many.scales + j * many.ld_scales) + word;
+        if (at >= many_turns) return;
+        if (word + 3 <= last_word) {
+            w = *reinterpret_cast<const u32x4u*>(from);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) w[i] = word + i <= last_word ? from[i] : 0u;
+        }
+    };
+    auto hold_scales = [&](uint32_t at, u32x4 w) {
+        if (at >= many_turns) return;
+        const uint32_t r = at / turns, word = (at - r * turns) * 4;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const int live = (int)blocks - 4 * (int)(word + i);
+            const uint32_t real = live >= 4 ? 0xFFFFFFFFu : live > 0 ? (1u << (8 * live)) - 1u : 0u;
+            w[i] = (w[i] & real) | (0x7F7F7F7Fu & ~real);
+        }
+        *reinterpret_cast<u32x4*>(many_scales + r * many_pitch(turns) + 4 * word) = w;
+    };
+    u32x4 my_scales;
+#pragma unroll
+    for (uint32_t i = 0; i < kFirst; ++i) fetch(threadIdx.x + i * blockDim.x, mine[i]);
+    fetch_scales(threadIdx.x, my_scales);
+    // then codes, of two turns; what lies behind the last block is some block's, and meets zeros of the few rows
     const uint32_t* rows[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int64_t j = j0 + 16 * t + in, row = j < many.rows ? j : many.rows - 1;
         rows[t] = many.codes + row * many.ld_words;
     }
-    u32x4 codes[NT][4];
-    auto load = [&](uint32_t block) {
+    typedef u32x4 Codes[NT][4];
+    Codes one, two;
+    auto load = [&](uint32_t block, Codes& codes) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int s = 0; s < 4; ++s)
                 codes[t][s] = *reinterpret_cast<const u32x4*>(rows[t] + 4 * (int64_t)min(block + 4 * s + g, blocks - 1));
     };
+    const uint32_t step = waves * kTurn;
     uint32_t block = wave * kTurn;
-    load(block);
-    for (uint32_t at = threadIdx.x; at < few_blocks; at += blockDim.x) {
-        if (at >= blockDim.x) fetch(at);
-        hold(at);
+    load(block, one);
+#pragma unroll
+    for (uint32_t i = 0; i < kFirst; ++i) hold(threadIdx.x + i * blockDim.x, mine[i]);
+    hold_scales(threadIdx.x, my_scales);
+    if (block + step < blocks) load(block + step, two);
+    for (uint32_t at = threadIdx.x + kFirst * blockDim.x; at < few_blocks; at += kFirst * blockDim.x) {
+#pragma unroll
+        for (uint32_t i = 0; i < kFirst; ++i) fetch(at + i * blockDim.x, mine[i]);
+#pragma unroll
+        for (uint32_t i = 0; i < kFirst; ++i) hold(at + i * blockDim.x, mine[i]);
+    }
+    for (uint32_t at = threadIdx.x + blockDim.x; at < many_turns; at += blockDim.x) {
+        fetch_scales(at, my_scales);
+        hold_scales(at, my_scales);
     }
     __syncthreads();
     f32x4 acc[MT][NT] = {};
-    while (block < blocks) {
+    auto turn = [&](const Codes& codes) {
         uint32_t ws[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -621,8 +665,15 @@ __global__ __launch_bounds__(64 * kFewWaves) void mv_mx_product_few_kernel(Launc
                 acc[i][t] = mfma<3>(codes[t][3], ws[t], x[3], xs, acc[i][t]);
             }
         }
-        block += waves * kTurn;
-        if (block < blocks) load(block);
+    };
+    while (block < blocks) {
+        turn(one);
+        if (block + 2 * step < blocks) load(block + 2 * step, one);
+        block += step;
+        if (block >= blocks) break;
+        turn(two);
+        if (block + 2 * step < blocks) load(block + 2 * step, two);
+        block += step;
     }
     __syncthreads();
     f32x4* sums = reinterpret_cast<f32x4*>(held);                         // wavefront, tile, lane
@@ -650,26 +701,32 @@ __global__ __launch_bounds__(64 * kFewWaves) void mv_mx_product_few_kernel(Launc
 constexpr int64_t  kFewRows = 16, kFewValues = 64;
 constexpr uint32_t kFewLds = 144 * 1024;
 
-// Whether and how the kernel for few rows takes a product.  Up to 16 rows it always is the faster one.  Up to 64 rows of
-// values it saves the launch that quantises them, as long as each unit quantises them once: bf16, 64 rows with 4096 x 2048
-// 11.0 us (two launches 12.1), 4096 x 1024 7.7 (8.9), 1000 x 2048 10.2 (11.3), 400 x 470 8.6 (8.5), 20 rows 5.4 (7.5); but
-// 16,000 x 256, a thousand workgroups, 16.8 (7.9), and 200 rows in four tiles with 1000 x 1000 11.6 (9.2).
+// Whether and how the kernel for few rows takes a product.  Up to 16 rows of codes it always is the faster one.  Of values it
+// takes up to 64, as long as each unit quantises them once, and saves the launch that quantises them: bf16, 64 rows with
+// 4096 x 1024 7.4 us (two launches 9.0), 20 rows with 4000 x 2048 6.0 (11.1), 5 with 16,384 x 8192 18.1 (18.6), 1 with 8192 x
+// 8192 9.4 (11.3); but 16,000 x 256, a thousand workgroups, 16.8 (7.9), and 200 rows in four tiles with 1000 x 1000 11.6 (9.2).
+// What all workgroups quantise together is bounded, too, fp32 at a third of bf16: 16 rows bf16 with 16,384 x 4096, 33 M values,
+// 14.9 us (13.8), 12 with 12,000 x 8192, 74 M, 21.9 (17.0); fp32 8 with 4096 x 4096, 8 M, 8.5 (6.5, but a launch costs the host
+// 3 more), 4 with 8192 x 8192, 17 M, 15.4 (11.5), 16 with 14,000 x 8192, 57 M, 44 (20).
+constexpr int64_t kQuantisedBf16 = 36000000, kQuantisedF32 = 12000000;
 struct FewCut {
     int      mt, nt;                // 0: it does not
     uint32_t groups, lds, waves;
 };
-static FewCut few_cut(int64_t few, int64_t many, int64_t k, bool values)
+static FewCut few_cut(int64_t few, int64_t many, int64_t k, int64_t quantised)     // most values to quantise; 0: codes
 {
+    const bool values = quantised > 0;
     if (few > (values ? kFewValues : kFewRows)) return FewCut{};
     const int64_t turns = (blocks_of(k) + kTurn - 1) / kTurn;
     FewCut c = {};
     c.mt = few <= 16 ? 1 : few <= 32 ? 2 : 4;
     // Workgroups of 16 rows as long as all of them run at once, three to a unit; beyond that 32 rows, which share what a
-    // workgroup spends on the few rows.  Four bf16 rows against 8192 x 8192: 13.0 us with 16 and 13.4 with 32; 12,000 x
-    // 8192 15.9 and 17.5; 14,000 x 8192 19.5 and 18.0; 16,384 x 6000 18.8 and 14.7; 16,384 x 8192 28 and 19.9.
+    // workgroup spends on the few rows.  bf16 us with 16 and with 32: four rows against 8192 x 8192 10.5, 10.4; 10,000 x 8192
+    // 13.0, 15.5; 12,000 x 8192 13.9, 15.8; 14,000 x 8192 16.6, 16.5; 16,384 x 8192 17.4, 17.6; 16,384 x 6000 16.8, 15.9; five
+    // fp32 rows 16,384 x 8192 30, 24; sixteen bf16 rows 16,384 x 4096 18.3, 14.7.
     c.nt = c.mt == 1 && many > 12288 ? 2 : 1;
     const int64_t groups = (many + 16 * c.nt - 1) / (16 * c.nt);
-    if (turns >= 4096 || groups > kMostGroups / 4) return FewCut{};
+    if (turns >= 4096 || groups > kMostGroups / 4 || (values && groups * few * k > quantised)) return FewCut{};
     c.groups = (uint32_t)groups;
     // a wavefront for each turn, or for each 64 blocks of the few rows
     const int64_t waves = few > 4 ? few * turns / 4 + 1 : turns;
@@ -795,10 +852,10 @@ static mv_status launch_plain(const Wanted& w, hipStream_t st)
 static FewCut few_codes_cut(const Wanted& w, bool& few_a)
 {
     few_a = w.a.rows <= w.b.rows;
-    FewCut c = few_a ? few_cut(w.a.rows, w.b.rows, w.k, false) : few_cut(w.b.rows, w.a.rows, w.k, false);
+    FewCut c = few_a ? few_cut(w.a.rows, w.b.rows, w.k, 0) : few_cut(w.b.rows, w.a.rows, w.k, 0);
     if (!c.mt) {
         few_a = !few_a;
-        c = few_a ? few_cut(w.a.rows, w.b.rows, w.k, false) : few_cut(w.b.rows, w.a.rows, w.k, false);
+        c = few_a ? few_cut(w.a.rows, w.b.rows, w.k, 0) : few_cut(w.b.rows, w.a.rows, w.k, 0);
     }
     return c;
 }
@@ -957,7 +1014,7 @@ mv_status mv_mx_linear(const void* x, int32_t x_dtype, int64_t ld_x, const uint3
     hipStream_t st = static_cast<hipStream_t>(stream);
     const Factor w = {w_codes, w_scales, ld_words, ld_scales, n};
     const Out out = {y, y_dtype == MV_BF16};
-    const FewCut cut = few_cut(m, n, k, true);
+    const FewCut cut = few_cut(m, n, k, x_dtype == MV_BF16 ? kQuantisedBf16 : kQuantisedF32);
     if (cut.mt)
         return x_dtype == MV_BF16 ? launch_few_values<uint16_t>(cut, x, ld_x, m, w, k, out, ld_y, st)
                                   : launch_few_values<float>(cut, x, ld_x, m, w, k, out, ld_y, st);

@@ -309,3 +309,22 @@ def test_gradients_of_many_tiles(m, n, k):
     x32, dy32 = x.float().cpu().numpy(), dy.float().cpu().numpy()
     check(dx, R.held(dy32), wt, torch.float32)
     check(dw, R.held(np.ascontiguousarray(dy32.T)), R.held(np.ascontiguousarray(x32.T)), torch.float32)
+
+
+@pytest.mark.parametrize("src", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(3, 600, 9000), (2, 530, 13_001), (16, 513, 17_000), (5, 12_300, 2100), (1, 12_500, 4500),
+                                   (12, 4200, 4100), (16, 9000, 4100), (40, 5000, 2500)])
+def test_few_rows_of_values(m, n, k, src):
+    """Several turns of a wavefront, 32 of the many rows, and on both sides of what workgroups quantise for themselves."""
+    rng = np.random.default_rng(m + n + k)
+    x = torch.from_numpy(normal(rng, m, k)).cuda().to(TYPES[src])
+    w_codes, w_scales, w = hold(normal(rng, n, k))
+    out = torch.full((m + 1, n + 2), 7.5, device="cuda")
+    B.mv_mx_linear(x, w_codes, w_scales, out[:m, :n], scratch_of(B.mv_mx_linear_scratch_bytes(m, n, k)))
+    check(out[:m, :n], R.held(x.float().cpu().numpy()), w, torch.float32)
+    assert (out[m:] == 7.5).all() and (out[:, n:] == 7.5).all()
+    codes, scales = torch.zeros_like(w_codes[:1]).expand(m, -1).contiguous(), torch.zeros_like(w_scales[:1]).expand(m, -1).contiguous()
+    B.mv_mx_encode(x, codes, scales)
+    again = torch.zeros((m, n), device="cuda")
+    B.mv_mx_product(codes, scales, w_codes, w_scales, k, again, scratch_of(B.mv_mx_product_scratch_bytes(m, n, k)))
+    check(again, R.held(x.float().cpu().numpy()), w, torch.float32)
