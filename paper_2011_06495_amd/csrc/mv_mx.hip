@@ -249,9 +249,13 @@ __global__ __launch_bounds__(kThreads) void mv_mx_aggregate_kernel(const uint32_
             if (r0 + i >= rows) break;
             float x[8];
             decode8(w[i], s[i], x);
-            const float f = weights ? weights[r0 + i] : 1.0f;
+            if (weights) {
+                const float f = weights[r0 + i];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] += f * x[j];
+                for (int j = 0; j < 8; ++j) x[j] *= f;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += x[j];
         }
     }
 #pragma unroll

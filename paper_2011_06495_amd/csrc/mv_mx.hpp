@@ -141,12 +141,15 @@ __device__ __forceinline__ uint32_t encode8(const float (&x)[8], uint32_t scale)
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], p, 3);
     return w;
 }
+// The way back: the instruction multiplies by the power of two whose exponent field its operand has, with 0 for 2^-127 and 255
+// for a NaN: compared with the definition for all scales and codes.
+__device__ __forceinline__ float factor_of(uint32_t scale) { return __uint_as_float(scale << 23); }
 __device__ __forceinline__ void decode8(uint32_t w, uint32_t scale, float (&x)[8])
 {
-    const float p = scale == kNanScale ? __uint_as_float(0x7FC00000u) : power_of(scale);
-    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
-    const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
-    x[0] = a.x * p, x[1] = a.y * p, x[2] = b.x * p, x[3] = b.y * p, x[4] = c.x * p, x[5] = c.y * p, x[6] = d.x * p, x[7] = d.y * p;
+    const float p = factor_of(scale);
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, p, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, p, 1);
+    const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, p, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, p, 3);
+    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y, x[4] = c.x, x[5] = c.y, x[6] = d.x, x[7] = d.y;
 }
 
 // Of four values: 16 bits.
@@ -160,9 +163,9 @@ __device__ __forceinline__ uint32_t encode4(const float (&x)[4], uint32_t scale)
 }
 __device__ __forceinline__ void decode4(uint32_t w, uint32_t scale, float (&x)[4])
 {
-    const float p = scale == kNanScale ? __uint_as_float(0x7FC00000u) : power_of(scale);
-    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
-    x[0] = a.x * p, x[1] = a.y * p, x[2] = b.x * p, x[3] = b.y * p;
+    const float p = factor_of(scale);
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, p, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, p, 1);
+    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
 }
 
 // The same of bf16 pairs as they are.
