@@ -5,7 +5,7 @@
 // are short.  A lane takes 16 bytes of values, so a wavefront's loads and stores cover one run of memory: four lanes a
 // block of 32 bf16 values, eight lanes one of fp32; the block's largest magnitude is two or three DPP moves away.
 // 16 x 11.2 M fp32 to codes and residual 247 us, 6.2 TB/s; 4096 x 8192 bf16 to codes 20 us, 4.2 TB/s (in a loop with a
-// product whose 67 MB of results are still on their way to memory); the mean of 16 x 11.2 M 33 us, 4.3 TB/s; 8192 x 4096
+// product whose 67 MB of results are still on their way to memory); the mean of 16 x 11.2 M 31 us, 4.5 TB/s; 8192 x 4096
 // codes back to bf16 13 us, 6.5 TB/s, the codes out of the last-level cache.
 #include "mv_mx.hpp"
 

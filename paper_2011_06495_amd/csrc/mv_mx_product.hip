@@ -130,9 +130,9 @@ __global__ __launch_bounds__(kProductThreads) void mv_mx_product_kernel(Factor a
 //
 // A lane of the 32 x 32 x 64 instruction holds half of a row's eight blocks: blocks 4 (lane / 32) + s of step s, whose
 // scales are one word.
-// 4096 x 8192 by 8192, bf16 results: 139 us, 4.0 PFLOP/s.  The instructions alone, out of registers, reach 8.4 on small
-// numbers and 6.2 to 6.7 on random codes, where power bounds them; the rest is the reads from LDS beside them and the end,
-// where 67 MB leave.  With 512 values of k the results are all: 4900 x 512 by 4608 to fp32 26 us with the launch
+// 4096 x 8192 by 8192, bf16 results: 139 us on a cool card to 150, 4.0 to 3.7 PFLOP/s.  The instructions alone, out of
+// registers, reach 8.4 on small numbers and 6.2 to 6.7 on random codes, where power bounds them; the rest is the codes' way
+// into LDS beside them (without it 111), the reads from there and the end, where 67 MB leave.  With 512 values of k the results are all: 4900 x 512 by 4608 to fp32 26 us with the launch
 // that quantises (4), a fill of those 90 MB 15.5.
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
