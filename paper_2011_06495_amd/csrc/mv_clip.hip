@@ -12,7 +12,7 @@
 // there reach 7.0 TB/s on this machine, from memory 6.2).
 // The waits are bounded.  Workgroups start in their order, so those that wait have all started as long as nothing else
 // holds the units; whoever gives up leaves its chunk to the launch behind, which finds all sums there.
-// Groups too large for that are read twice, in two launches; groups of up to 256 KB are a single workgroup's, in one launch.
+// Groups too large for that are read twice, by two launches with one between them that adds up the group's sums; groups of up to 256 KB are a single workgroup's, in one launch.
 //
 // Squares of fp32 and bf16 values are exact in fp64 and cannot leave its range; a lane has a few fp64 sums of its own, the
 // order of all additions follows from the sizes, so a norm does not depend on timing.  Maxima are those of the bit
@@ -274,12 +274,20 @@ __device__ __forceinline__ void write_sum(Sum* s, uint32_t call, double v)
 }
 __device__ __forceinline__ double sum_of(uint64_t hi, uint64_t lo) { return __longlong_as_double((long long)(hi << 32 | (lo & 0xFFFFFFFFu))); }
 
-// A group's value from its chunks' sums, which an earlier launch has left; the same in every workgroup that asks.
-template <bool MAX>
+// A group's value from its chunks' sums, which an earlier launch has left; the same in every workgroup that asks.  AHEAD of
+// a thread's sums are in flight at once; they are added one after the other whatever it is.
+template <bool MAX, int AHEAD>
 __device__ __forceinline__ double group_value(const Lists& l, uint32_t first, uint32_t last, double* lds)
 {
     double v = 0.0;
-    for (uint32_t i = first + threadIdx.x; i < last; i += kThreads) v = joined<MAX>(v, sum_of(l.sums[i].hi, l.sums[i].lo));
+    for (uint32_t at = first + threadIdx.x; at < last; at += AHEAD * kThreads) {
+        Sum s[AHEAD];
+#pragma unroll
+        for (uint32_t k = 0; k < AHEAD; ++k) s[k] = l.sums[min(at + k * kThreads, last - 1)];
+#pragma unroll
+        for (uint32_t k = 0; k < AHEAD; ++k)
+            if (at + k * kThreads < last) v = joined<MAX>(v, sum_of(s[k].hi, s[k].lo));
+    }
     return of_workgroup<MAX, kWaves>(v, lds);
 }
 
@@ -367,14 +375,15 @@ __global__ __launch_bounds__(kThreads, 7) void mv_clip_once(Lists l, float max_n
     });
 }
 
+// A chunk that mv_clip_once has left.
 template <bool MAX>
-__device__ __forceinline__ void scale_chunk(const Lists& l, uint32_t at, const Chunk& c, float max_norm, float* __restrict__ norms,
-                                            float* __restrict__ coefs, double* lds)
+__device__ __forceinline__ void finish_chunk(const Lists& l, uint32_t at, const Chunk& c, float max_norm, float* __restrict__ norms,
+                                             float* __restrict__ coefs, double* lds)
 {
     const uint32_t first = l.group_first[c.group], last = l.group_first[c.group + 1];
     by_kind<kThreads, kRounds>(c, [&](auto& h) {
         h.load(c.src, (int)c.count, (int)threadIdx.x);               // on its way while the factor is found
-        const float norm = norm_of<MAX>(group_value<MAX>(l, first, last, lds));
+        const float norm = norm_of<MAX>(group_value<MAX, 1>(l, first, last, lds));
         const float coef = coef_of(norm, max_norm);
         if (at + 1 == last && threadIdx.x == 0) {
             norms[c.group] = norm;
@@ -405,7 +414,7 @@ __global__ __launch_bounds__(kThreads) void mv_clip_rest(Lists l, float max_norm
     }
     const uint32_t call = l.state->call;
     for (uint32_t at = blockIdx.x; at < l.n_chunks; at += kFixGroups)
-        if (l.late[at] == call) scale_chunk<MAX>(l, at, l.chunks[at], max_norm, norms, coefs, lds);
+        if (l.late[at] == call) finish_chunk<MAX>(l, at, l.chunks[at], max_norm, norms, coefs, lds);
     __syncthreads();
     // the last workgroup to come here
     if (threadIdx.x == 0 && atomicAdd(&l.state->fixed, 1u) == kFixGroups - 1) {
@@ -485,25 +494,33 @@ __global__ __launch_bounds__(kThreads) void mv_clip_gather(Lists l)
     }
 }
 
-// One workgroup per group.
+// One workgroup per group.  For mv_clip_scale it leaves the factor: there each of a group's chunks has a workgroup, and if all
+// of those added up all of its sums, the work would grow with the square of the group.  us of a clip, with that and so: one group
+// of 2^30 bf16 3225, 1210; 2.7e8 fp32 1057, 598; 5.1e7 fp32 112, 98; 1.5e7 fp32, the smallest read twice, 33.7, 34.0.
+constexpr int kSumsAhead = 8;
 template <bool MAX>
 __global__ __launch_bounds__(kThreads) void mv_clip_norm(Lists l, float max_norm, float* __restrict__ norms, float* __restrict__ coefs)
 {
     __shared__ double lds[kWaves];
     const uint32_t g = blockIdx.x;
-    const float norm = norm_of<MAX>(group_value<MAX>(l, l.group_first[g], l.group_first[g + 1], lds));
+    const float norm = norm_of<MAX>(group_value<MAX, kSumsAhead>(l, l.group_first[g], l.group_first[g + 1], lds));
     if (threadIdx.x == 0) {
+        const float coef = coef_of(norm, max_norm);
         norms[g] = norm;
-        if (coefs) coefs[g] = coef_of(norm, max_norm);
+        if (coefs) coefs[g] = coef;
+        l.coefs[g] = __float_as_uint(coef);                       // of call 0: mv_clip_once waits for another's
     }
 }
 
-template <bool MAX>
-__global__ __launch_bounds__(kThreads) void mv_clip_scale(Lists l, float max_norm, float* __restrict__ norms,
-                                                          float* __restrict__ coefs)
+__global__ __launch_bounds__(kThreads) void mv_clip_scale(Lists l)
 {
-    __shared__ double lds[kWaves];
-    scale_chunk<MAX>(l, blockIdx.x, l.chunks[blockIdx.x], max_norm, norms, coefs, lds);
+    const Chunk c = l.chunks[blockIdx.x];
+    by_kind<kThreads, kRounds>(c, [&](auto& h) {
+        h.load(c.src, (int)c.count, (int)threadIdx.x);
+        const float coef = __uint_as_float((uint32_t)l.coefs[c.group]);
+        if (coef == 1.0f && c.src == c.dst) return;
+        h.store(c.dst, (int)c.count, (int)threadIdx.x, coef);
+    });
 }
 
 struct Pairs {
@@ -829,8 +846,8 @@ mv_status mv_clip_grads(mv_clip* c, float max_norm, float* norms, float* coefs, 
         MV_CLIP_LAUNCH(mv_clip_rest, mvc::kFixGroups, mvc::kThreads, max_norm, norms, coefs, c->any_empty);
     } else {
         MV_CLIP_LAUNCH(mv_clip_gather, c->lists.n_chunks, mvc::kThreads);
-        if (c->any_empty) MV_CLIP_LAUNCH(mv_clip_norm, c->lists.n_groups, mvc::kThreads, max_norm, norms, coefs);
-        MV_CLIP_LAUNCH(mv_clip_scale, c->lists.n_chunks, mvc::kThreads, max_norm, norms, coefs);
+        MV_CLIP_LAUNCH(mv_clip_norm, c->lists.n_groups, mvc::kThreads, max_norm, norms, coefs);
+        hipLaunchKernelGGL(mvc::mv_clip_scale, dim3(c->lists.n_chunks), dim3(mvc::kThreads), 0, st, c->lists);
     }
     return done(c);
 }
