@@ -427,8 +427,10 @@ mv_status mv_clip_grads(mv_clip* clip, float max_norm, float* norms, float* coef
 /*
  * Where a group fits the GPU's registers, its gradients are read once: workgroups of one
  * launch then wait for each other's sums, for at most `polls` looks at memory (default
- * 2^16, about 50 ms); what is not done then the launch behind does.  Results never depend
- * on it.  A test hook: 0 makes everyone who does not find what it needs at once give up.
+ * 512, about 0.5 ms); what is not done then the launch behind does, which happens where
+ * another stream's work holds part of the GPU meanwhile and costs a call up to that wait
+ * for each group and a second reading.  Results never depend on it.  A test hook: 0 makes
+ * everyone who does not find what it needs at once give up.
  */
 mv_status mv_clip_set_spin_limit(mv_clip* clip, uint32_t polls);
 

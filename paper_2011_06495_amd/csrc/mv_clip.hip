@@ -11,7 +11,8 @@
 // Memory is the bound; reading a second time, even out of the last-level cache, would be a third of the time (reads from
 // there reach 7.0 TB/s on this machine, from memory 6.2).
 // The waits are bounded.  Workgroups start in their order, so those that wait have all started as long as nothing else
-// holds the units; whoever gives up leaves its chunk to the launch behind, which finds all sums there.
+// holds the units; whoever gives up leaves its chunk to the launch behind, which finds all sums there.  A limit of half a
+// millisecond keeps that cheap where something else does.
 // Groups too large for that are read twice, by two launches with one between them that adds up the group's sums; groups of up to 256 KB are a single workgroup's, in one launch.
 //
 // Squares of fp32 and bf16 values are exact in fp64 and cannot leave its range; a lane has a few fp64 sums of its own, the
@@ -562,7 +563,11 @@ struct mv_clip {
 namespace {
 
 constexpr size_t   kAlign = 256;
-constexpr uint32_t kPolls = 1u << 16;       // looks of about a microsecond each; a group's sums are there within fifty
+// Looks of about a microsecond each.  Alone on the card nobody needs more than 96 (32 x 25.6 M bf16; 64 at 16 x 11.2 M fp32, 24 at
+// 25.6 M); where another stream's work holds units, so that a group's workgroups are not all there at once, this is what they
+// lose before the launch behind takes over.  Two handles on two streams, 4 x 11.2 M fp32 each, 76 us alone, together 820 us
+// (with 2^16 looks 63,500).
+constexpr uint32_t kPolls = 512;
 constexpr uint64_t kMostChunks = 0xFFFFFF;   // a workgroup of 256 threads each: their threads are counted in 32 bits
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
