@@ -779,18 +779,23 @@ struct Cut {
     uint32_t splits, steps_each;
     int64_t  groups() const { return tiles_m * tiles_n * splits; }
 };
+// How many runs the steps are split into, where `beside` tiles of another product share the launch.
+static constexpr int64_t splits_of(int64_t tiles, int64_t steps, int64_t results, int64_t beside)
+{
+    int64_t splits = 512 / tiles < steps / 4 ? 512 / tiles : steps / 4;
+    // many splits only of small results: all of them are written and read again
+    if (splits > 16 && splits * results > (4 << 20)) splits = 16;
+    // never more than alone, which is what the scratch has room for
+    if (beside && splits > 512 / (tiles + beside)) splits = 512 / (tiles + beside);
+    return splits > 1 ? splits : 1;
+}
+static_assert(splits_of(4, 512, 200 * 200, 0) == 16 && splits_of(4, 512, 200 * 200, 4) == 16, "the limit of 16 holds in company, too");
 static Cut cut_of(int64_t m, int64_t n, int64_t k, int mt, int64_t beside = 0)
 {
     auto tiles = [mt](int64_t rows) { return (rows + 64 * mt - 1) / (64 * mt); };
     Cut c = {mt, tiles(m), tiles(n), 1, 0};
     const int64_t steps = (blocks_of(k) + kStepBlocks - 1) / kStepBlocks;
-    if (mt == 2) {
-        int64_t splits = 512 / (c.tiles_m * c.tiles_n + beside);
-        if (splits > steps / 4) splits = steps / 4;
-        // many splits only of small results: all of them are written and read again
-        if (splits > 16 && splits * m * n > (4 << 20)) splits = 16;
-        if (splits > 1) c.splits = (uint32_t)splits;
-    }
+    if (mt == 2) c.splits = (uint32_t)splits_of(c.tiles_m * c.tiles_n, steps, m * n, beside);
     c.steps_each = (uint32_t)((steps + c.splits - 1) / c.splits);
     c.splits = (uint32_t)((steps + c.steps_each - 1) / c.steps_each);
     return c;
