@@ -362,11 +362,12 @@ mv_status mv_quant_decode(const uint32_t* streams, int64_t ld_words, int64_t n, 
  * infinite and coef 0 (dst: NaN where src is infinite or NaN, else 0): look at norm
  * before the result is used, as with any clipping.  A group without elements has norm 0.
  *
- * Tensors are contiguous, aligned to their own element and at most 2^40 elements long;
- * numel 0 (then the pointers may be NULL) is allowed; 2^37 elements in all.  dst is a tensor of its own
- * -- a part of a matrix row at any offset, for instance -- or src itself, if the types agree; apart
- * from that no dst overlaps another tensor.  dst NULL: the tensor only counts for its group's norm;
- * then all tensors' must be NULL, and mv_clip_grads reports MV_ERR_STATE.
+ * Tensors are contiguous and aligned to their own element; numel 0 (then the pointers may be NULL) is
+ * allowed.  A list has fewer than 2^24 chunks: 32 KB of src each, every tensor's rounded up, and one
+ * more for each group that has elements (2^37 fp32 or 2^38 bf16 values, less what rounding takes).
+ * dst is a tensor of its own -- a part of a matrix row at any offset, for instance -- or src itself, if
+ * the types agree; apart from that no dst overlaps another tensor.  dst NULL: the tensor only counts for
+ * its group's norm; then all tensors' must be NULL, and mv_clip_grads reports MV_ERR_STATE.
  */
 typedef struct mv_clip mv_clip; /* opaque */
 
@@ -454,7 +455,13 @@ void      mv_clip_release(mv_clip* clip);
  * block are neither written nor used.  Codes are 16-byte aligned, ld_words a multiple
  * of 4; scales 4-byte aligned, ld_scales a multiple of 4.
  * Values (vals, resid, out, x, y, ...) are fp32 or bf16, aligned to their element, with
- * any row stride >= the row; 1 <= rows, n < 2^31, at most 2^34 - 2^15 values in whole blocks.
+ * any row stride >= the row; 1 <= rows, n < 2^31.  Besides, MV_ERR_INVALID_ARG is what a
+ * call gets beyond
+ *   2^34 - 2^14 values in whole blocks, where rows are quantised or read back;
+ *   2^24 - 1 tiles of 128 rows by 64 columns (bf16: by 128), where columns are quantised;
+ *   2^24 - 1 of such tiles of x, of dy, and of dy's blocks by 32 (bf16: by 128), all added
+ *   up, in mv_mx_linear_grad;
+ * and may get from 2^23 tiles of 128 x 128 results of a product on.
  * All of these calls run on the CURRENT device, are enqueued on `stream` and allocate
  * nothing.  Errors: MV_ERR_INVALID_ARG, MV_ERR_DEVICE.
  */
