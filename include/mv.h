@@ -356,9 +356,9 @@ mv_status mv_quant_decode(const uint32_t* streams, int64_t ld_words, int64_t n, 
  *   coef[g] = min(1, max_norm / (norm[g] + 1e-6))          (fp32)
  *   dst     = src * coef[g]                                (fp32, rounded once to dst's type)
  *
- * Sums of squares are formed in fp64 in an order that depends on the sizes alone, so
- * neither large nor small fp32 values leave the range, and equal inputs give equal
- * norms.  A NaN makes the group's norm, coef and every dst NaN; an infinity makes norm
+ * Sums of squares are formed in fp64, so no square leaves the range, in an order that
+ * follows from the list (all groups' sizes and types) and never from timing: equal lists
+ * of equal values give equal norms.  A NaN makes the group's norm, coef and every dst NaN; an infinity makes norm
  * infinite and coef 0 (dst: NaN where src is infinite or NaN, else 0): look at norm
  * before the result is used, as with any clipping.  A group without elements has norm 0.
  *
@@ -495,8 +495,10 @@ mv_status mv_mx_aggregate(const uint32_t* codes, int64_t ld_words, const uint8_t
 
 /*
  * c[i][j] = sum over k of a[i][k] * b[j][k]: m rows of a, n rows of b, k values each,
- * all in 4 bits along k; fp32 sums in an order that depends on the sizes alone; c fp32
- * or bf16.  scratch: device, 16-byte aligned, >= mv_mx_product_scratch_bytes(m, n, k) (0: may be NULL).
+ * all in 4 bits along k; fp32 sums; c fp32 or bf16.  Here and in a layer's calls the order
+ * of the sums follows from the arguments (sizes, types, strides, which results are asked
+ * for) and never from timing: equal calls give equal results, other ones equal sums up to
+ * rounding.  scratch: device, 16-byte aligned, >= mv_mx_product_scratch_bytes(m, n, k) (0: may be NULL).
  */
 size_t    mv_mx_product_scratch_bytes(int64_t m, int64_t n, int64_t k);
 mv_status mv_mx_product(const uint32_t* a_codes, int64_t ld_aw, const uint8_t* a_scales, int64_t ld_as,

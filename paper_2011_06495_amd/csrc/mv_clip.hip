@@ -16,7 +16,7 @@
 // Groups too large for that are read twice, by two launches with one between them that adds up the group's sums; groups of up to 256 KB are a single workgroup's, in one launch.
 //
 // Squares of fp32 and bf16 values are exact in fp64 and cannot leave its range; a lane has a few fp64 sums of its own, the
-// order of all additions follows from the sizes, so a norm does not depend on timing.  Maxima are those of the bit
+// order of all additions follows from the list's sizes and types, so a norm does not depend on timing.  Maxima are those of the bit
 // patterns without the sign: a NaN's pattern is above infinity's, so a NaN stays.
 #include "../../include/mv.h"
 
