@@ -359,8 +359,9 @@ mv_status mv_quant_decode(const uint32_t* streams, int64_t ld_words, int64_t n, 
  * Sums of squares are formed in fp64, so no square leaves the range, in an order that
  * follows from the list (all groups' sizes and types) and never from timing: equal lists
  * of equal values give equal norms.  A NaN makes the group's norm, coef and every dst NaN; an infinity makes norm
- * infinite and coef 0 (dst: NaN where src is infinite or NaN, else 0): look at norm
- * before the result is used, as with any clipping.  A group without elements has norm 0.
+ * infinite and coef 0 (dst: NaN where src is infinite or NaN, else 0), and so do finite
+ * values whose norm is beyond fp32 (dst: 0): look at norm before the result is used, as
+ * with any clipping.  A group without elements has norm 0.
  *
  * Tensors are contiguous and aligned to their own element; numel 0 (then the pointers may be NULL) is
  * allowed.  A list has fewer than 2^24 chunks: 32 KB of src each, every tensor's rounded up, and one
