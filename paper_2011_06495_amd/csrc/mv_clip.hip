@@ -6,14 +6,17 @@
 // The list of tensors is cut into chunks, sorted by group, when the handle is made.  A chunk fits a workgroup's registers,
 // and a launch's workgroups hold 57 MB together, so a group is read once and written once: its workgroups
 // load their chunks, leave their sums, and wait for the group's last workgroup, which adds the sums up in a fixed order.
-// 16 x 11.2 M fp32 values: 306 us (reading twice 377), 4.7 TB/s; 32 x 25.6 M bf16 780 (871), 4.2; a copy reaches 5.5 to 5.9.
-// What is missing is that a group's reads and its stores hardly overlap: two groups do not fit the registers.
+// 16 x 11.2 M fp32 values: 304 us, 4.7 TB/s; 32 x 25.6 M bf16 760, 4.3; a copy reaches 5.5 to 5.9.
+// What is missing: a group's reads and its stores overlap little, and what each group loses between its last load and its
+// first store is not known.  More registers, 80 MB of chunks, did not help.
 // Memory is the bound; reading a second time, even out of the last-level cache, would be a third of the time (reads from
 // there reach 7.0 TB/s on this machine, from memory 6.2).
 // The waits are bounded.  Workgroups start in their order, so those that wait have all started as long as nothing else
 // holds the units; whoever gives up leaves its chunk to the launch behind, which finds all sums there.  A limit of half a
 // millisecond keeps that cheap where something else does.
-// Groups too large for that are read twice, by two launches with one between them that adds up the group's sums; groups of up to 256 KB are a single workgroup's, in one launch.
+// Groups too large for that are read twice, by two launches with one between them that adds up the group's sums: 25.6 M fp32
+// 53 us (gathering 15.8, the sums 4.6, scaling 30), 5.8 TB/s of the three passes, 2^30 bf16 1.2 ms, 5.4.  Groups of up to 256 KB
+// are a single workgroup's, in one launch.
 //
 // Squares of fp32 and bf16 values are exact in fp64 and cannot leave its range; a lane has a few fp64 sums of its own, the
 // order of all additions follows from the list's sizes and types, so a norm does not depend on timing.  Maxima are those of the bit
@@ -31,7 +34,7 @@ namespace mvc {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 // 16 bytes of a thread each.  Eight leave room for seven workgroups to a unit (66 registers a lane), 57 MB in all; sixteen
-// for five and 80 MB, but no gain: 16 x 11.2 M fp32 306 : 313 us, 32 x 25.6 M bf16 780 : 778, 25.6 M bf16 to fp32 33.5 : 37.8.
+// for five and 80 MB, but no gain: 16 x 11.2 M fp32 307 : 310 us, 32 x 25.6 M bf16 760 : 773, 25.6 M bf16 to fp32 32.6 : 36.9.
 constexpr int kRounds = 8;
 constexpr int kChunkBytes = kThreads * kRounds * 16;
 constexpr int kSmallWaves = 16, kSmallBytes = 64 * 16;                   // of the kernel for small groups: a wavefront, 16 bytes a lane

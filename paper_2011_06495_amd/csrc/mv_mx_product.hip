@@ -814,9 +814,9 @@ inline size_t parts_bytes(int64_t m, int64_t n, int64_t k)
     return splits > 1 ? up256((size_t)splits * (size_t)m * (size_t)quads_of(n) * 16) : 0;
 }
 
-// Results beyond the L2s' 32 MB are stored past them: 4096 x 8192 bf16 by 8192 201 -> 170 us with whole runs of a row, so
-// stored.  Smaller ones, and sums that are added up right away, are a little faster stored as usual: 1000 x 1000 by 1000
-// 10.1 : 10.6 us, 130 x 130 by 8000 14.1 : 16.3.
+// Results of 16 MB and more, which are half of the L2s, are stored past them.  Smaller ones, and sums that are added up right
+// away, are a little faster stored as usual: 1000 x 1000 by 1000 7.8 us, past the caches 8.0; 130 x 130 by 8000 14.1 : 16.3.  From
+// 8 to 67 MB a product alone takes as long either way (4096 x 8192 by 8192 140.6 : 140.5).
 constexpr int64_t kPastBytes = 16 << 20;
 
 // A product that is asked for: c = a b^T, m rows and n rows of k values.

@@ -125,7 +125,7 @@ def test_nan_and_infinity_stay_in_their_group(kind):
 
 
 def test_one_large_group_takes_as_long_as_its_values_in_several():
-    """2^30 bf16 values as one group and as sixteen, each of which is read twice too: 12 bytes of memory a value either way,
+    """2^30 bf16 values as one group and as sixteen, each of which is read twice too: 6 bytes of memory a value either way,
     beside which the sums of its chunks, 16 bytes for each 32 KB, are nothing.  Half as much again is allowed for."""
     n = 1 << 30
     x = torch.randn(n // 16, device="cuda").bfloat16().repeat(16)
