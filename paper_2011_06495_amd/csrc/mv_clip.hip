@@ -14,8 +14,8 @@
 // The waits are bounded.  Workgroups start in their order, so those that wait have all started as long as nothing else
 // holds the units; whoever gives up leaves its chunk to the launch behind, which finds all sums there.  A limit of half a
 // millisecond keeps that cheap where something else does.
-// Groups too large for that are read twice, by two launches with one between them that adds up the group's sums: 25.6 M fp32
-// 53 us (gathering 15.8, the sums 4.6, scaling 30), 5.8 TB/s of the three passes, 2^30 bf16 1.2 ms, 5.4.  Groups of up to 256 KB
+// Groups too large for that are read twice, by two launches, as a rule with one between them that adds up the group's sums: 25.6 M
+// fp32 53 us (gathering 15.8, the sums 4.6, scaling 30), 5.8 TB/s of the three passes, 2^30 bf16 1.2 ms, 5.4.  Groups of up to 256 KB
 // are a single workgroup's, in one launch.
 //
 // Squares of fp32 and bf16 values are exact in fp64 and cannot leave its range; a lane has a few fp64 sums of its own, the
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(kThreads, 7) void mv_clip_once(Lists l, float max_n
     });
 }
 
-// A chunk that mv_clip_once has left.
+// A chunk whose factor nobody has left: its workgroup adds up all of its group's sums.
 template <bool MAX>
 __device__ __forceinline__ void finish_chunk(const Lists& l, uint32_t at, const Chunk& c, float max_norm, float* __restrict__ norms,
                                              float* __restrict__ coefs, double* lds)
@@ -498,9 +498,7 @@ __global__ __launch_bounds__(kThreads) void mv_clip_gather(Lists l)
     }
 }
 
-// One workgroup per group.  For mv_clip_scale it leaves the factor: there each of a group's chunks has a workgroup, and if all
-// of those added up all of its sums, the work would grow with the square of the group.  us of a clip, with that and so: one group
-// of 2^30 bf16 3225, 1210; 2.7e8 fp32 1057, 598; 5.1e7 fp32 112, 98; 1.5e7 fp32, the smallest read twice, 33.7, 34.0.
+// One workgroup per group.  For mv_clip_scale it leaves the factor.
 constexpr int kSumsAhead = 8;
 template <bool MAX>
 __global__ __launch_bounds__(kThreads) void mv_clip_norm(Lists l, float max_norm, float* __restrict__ norms, float* __restrict__ coefs)
@@ -516,6 +514,18 @@ __global__ __launch_bounds__(kThreads) void mv_clip_norm(Lists l, float max_norm
     }
 }
 
+// The second reading: with the factor that mv_clip_norm leaves, or with every workgroup adding up its group's sums.  That saves a
+// launch, but a group's work grows with its square, so it is taken only while all workgroups together read few sums.  us of a
+// clip, adding up and with the launch: one fp32 group of 14.7 M values 30.0, 31.4; 20.5 M 39.9, 41.5; 24 M, 8.6 million sums, 46.9,
+// 47.7; 25.5 M, 9.7 million, 51.2, 50.2; 32 M 64.5, 60.9; four of 15 M, 13.4 million, 108.6, 105.8; one of 2^30 bf16 3225, 1200.
+constexpr uint64_t kSumsRead = 9000000;
+template <bool MAX>
+__global__ __launch_bounds__(kThreads) void mv_clip_add_scale(Lists l, float max_norm, float* __restrict__ norms,
+                                                              float* __restrict__ coefs)
+{
+    __shared__ double lds[kWaves];
+    finish_chunk<MAX>(l, blockIdx.x, l.chunks[blockIdx.x], max_norm, norms, coefs, lds);
+}
 __global__ __launch_bounds__(kThreads) void mv_clip_scale(Lists l)
 {
     const Chunk c = l.chunks[blockIdx.x];
@@ -854,8 +864,11 @@ mv_status mv_clip_grads(mv_clip* c, float max_norm, float* norms, float* coefs, 
         MV_CLIP_LAUNCH(mv_clip_rest, mvc::kFixGroups, mvc::kThreads, max_norm, norms, coefs, c->any_empty);
     } else {
         MV_CLIP_LAUNCH(mv_clip_gather, c->lists.n_chunks, mvc::kThreads);
-        MV_CLIP_LAUNCH(mv_clip_norm, c->lists.n_groups, mvc::kThreads, max_norm, norms, coefs);
-        hipLaunchKernelGGL(mvc::mv_clip_scale, dim3(c->lists.n_chunks), dim3(mvc::kThreads), 0, st, c->lists);
+        const bool add = (uint64_t)c->lists.n_chunks * c->most_chunks <= mvc::kSumsRead;
+        // norms of groups without chunks are its as well
+        if (!add || c->any_empty) MV_CLIP_LAUNCH(mv_clip_norm, c->lists.n_groups, mvc::kThreads, max_norm, norms, coefs);
+        if (add) MV_CLIP_LAUNCH(mv_clip_add_scale, c->lists.n_chunks, mvc::kThreads, max_norm, norms, coefs);
+        else hipLaunchKernelGGL(mvc::mv_clip_scale, dim3(c->lists.n_chunks), dim3(mvc::kThreads), 0, st, c->lists);
     }
     return done(c);
 }

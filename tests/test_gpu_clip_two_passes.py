@@ -9,7 +9,9 @@ pytestmark = pytest.mark.gpu
 
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 GUARD = -12345.5
-LARGE = 15_100_003          # fp32 values: 60 MB, more than the 57 that a launch's workgroups hold
+# fp32 values, 60 MB: more than the 57 that a launch's workgroups hold.  Once and twice as many in each of a call's groups, since
+# the workgroups of small calls of this kind add up their group's sums themselves and those of larger ones are left the factor.
+LARGE = 15_100_003
 
 
 @pytest.fixture(autouse=True)
@@ -53,10 +55,11 @@ def clip(tensors, out, groups, n_groups, kind, max_norm):
 
 @pytest.mark.parametrize("kind", [B.MV_NORM_L2, B.MV_NORM_MAX])
 @pytest.mark.parametrize("src,dst", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"), ("bf16", "bf16")])
-def test_groups_of_all_sizes(src, dst, kind):
+@pytest.mark.parametrize("times", [1, 2])
+def test_groups_of_all_sizes(times, src, dst, kind):
     """A group of one large tensor and odd small ones, a small group, an empty one and a second large one."""
     gen = torch.Generator(device="cuda").manual_seed(kind)
-    large = LARGE if src == "f32" else 2 * LARGE
+    large = times * (LARGE if src == "f32" else 2 * LARGE)
     sizes = [large, 5, 70_001, 1, 3, 0, large + 9]
     groups = [0, 0, 1, 1, 4, 0, 4]                    # groups 2 and 3 have no elements
     tensors = [torch.randn(n + 3, generator=gen, device="cuda")[i % 3:i % 3 + n].to(TYPES[src]) for i, n in enumerate(sizes)]
@@ -82,10 +85,11 @@ def test_groups_of_all_sizes(src, dst, kind):
         at += n + 3
 
 
-def test_types_mixed():
+@pytest.mark.parametrize("times", [1, 2])
+def test_types_mixed(times):
     gen = torch.Generator(device="cuda").manual_seed(5)
     kinds = [("f32", "bf16"), ("bf16", "f32"), ("f32", "f32"), ("bf16", "bf16")]
-    tensors = [torch.randn(LARGE // 3 + 7 * i, generator=gen, device="cuda").to(TYPES[s]) for i, (s, _) in enumerate(kinds)]
+    tensors = [torch.randn(times * LARGE // 3 + 7 * i, generator=gen, device="cuda").to(TYPES[s]) for i, (s, _) in enumerate(kinds)]
     out = [torch.zeros(t.numel(), dtype=TYPES[d], device="cuda") for t, (_, d) in zip(tensors, kinds)]
     want = norm64(tensors, B.MV_NORM_L2)
     norms, coefs = clip(tensors, out, [0] * 4, 1, B.MV_NORM_L2, 0.3 * want)
@@ -95,10 +99,11 @@ def test_types_mixed():
 
 
 @pytest.mark.parametrize("src", ["f32", "bf16"])
-def test_in_place(src):
+@pytest.mark.parametrize("times", [1, 2])
+def test_in_place(times, src):
     """One group's values are clipped where they are, the other's, whose factor is 1, are not touched."""
     gen = torch.Generator(device="cuda").manual_seed(6)
-    n = LARGE if src == "f32" else 2 * LARGE
+    n = times * (LARGE if src == "f32" else 2 * LARGE)
     tensors = [torch.randn(n, generator=gen, device="cuda").to(TYPES[src]) * s for s in (1.0, 0.25)]
     before = [t.clone() for t in tensors]
     norms, coefs = clip(tensors, tensors, [0, 1], 2, B.MV_NORM_L2, 0.5 * norm64(tensors[:1], B.MV_NORM_L2))
