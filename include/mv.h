@@ -529,6 +529,78 @@ mv_status mv_mx_linear_grad(const void* x, int64_t ld_x, const void* dy, int64_t
                             int64_t m, int64_t n, int64_t k, void* dx, int32_t dx_dtype, int64_t ld_dx, void* dw,
                             int32_t dw_dtype, int64_t ld_dw, void* scratch, size_t scratch_bytes, void* stream);
 
+/* ---- 8-bit floating point by blocks of 128 ----------------------------------- */
+
+/*
+ * Every 128 consecutive values of a row (a block; the row's last one may be shorter)
+ * share a power of two, 2^s with s the smallest whole number for which the largest
+ * magnitude is at most 448 * 2^s, and at least -127; a scale byte holds s + 127.  A value
+ * is held as an 8-bit code, sign << 7 | e << 3 | f, for +-(8 + f) 2^(e - 10) * 2^s, or where
+ * e is 0 +-f 2^-9 * 2^s: the nearest one, ties to the even f; no code is 0x7F or 0xFF.  A
+ * block of zeros has s = -127.  A block that holds an infinity or a NaN gets the scale
+ * byte 255 and codes 0: all of it reads as NaN.
+ *
+ * Layout: value k of a row is its byte k.  Rows are whole blocks: mv_f8_row_bytes(n) =
+ * 128 ceil(n / 128) bytes, the codes past n are 0, and mv_f8_row_scales(n) = ceil(n / 128)
+ * rounded up to 4 scale bytes, those past the last block are neither written nor used.
+ * Codes are 16-byte aligned, ld_bytes a multiple of 16; scales 4-byte aligned, ld_scales a
+ * multiple of 4.  Codes that a program makes itself must not be 0x7F or 0xFF.
+ * Values, strides, sizes, devices, streams and errors are those of the 4-bit calls.
+ * MV_ERR_INVALID_ARG is also what a call gets beyond
+ *   2^36 - 2^16 values in whole blocks, where rows are quantised or read back;
+ *   2^24 - 1 tiles of 128 rows by 64 columns (bf16: by 128), where columns are quantised;
+ *   2^24 - 1 of such tiles of x, of dy, and of dy's blocks by 32, all added up, in
+ *   mv_f8_linear_grad;
+ * and may get from 2^23 tiles of 128 x 128 results of a product on.
+ */
+int64_t mv_f8_row_bytes(int64_t n);    /* 0 for n outside 1 .. 2^31-1 */
+int64_t mv_f8_row_scales(int64_t n);
+
+/* codes, scales = the rows of vals. */
+mv_status mv_f8_encode(const void* vals, int32_t dtype, int64_t ld_vals, int64_t rows, int64_t n, uint8_t* codes,
+                       int64_t ld_bytes, uint8_t* scales, int64_t ld_scales, void* stream);
+
+/* codes, scales = the COLUMNS of vals (rows x n): n rows of codes of `rows` values each. */
+mv_status mv_f8_encode_t(const void* vals, int32_t dtype, int64_t ld_vals, int64_t rows, int64_t n, uint8_t* codes,
+                         int64_t ld_bytes, uint8_t* scales, int64_t ld_scales, void* stream);
+
+/* out (rows x n, fp32 or bf16) = what the codes stand for. */
+mv_status mv_f8_decode(const uint8_t* codes, int64_t ld_bytes, const uint8_t* scales, int64_t ld_scales, int64_t rows,
+                       int64_t n, void* out, int32_t dtype, int64_t ld_out, void* stream);
+
+/*
+ * c[i][j] = sum over k of a[i][k] * b[j][k], as mv_mx_product, in 8 bits along k; the order
+ * of the sums follows from the arguments, as there.  An fp32 c is a sum in fp32 (a factor's
+ * value counts to the nearest multiple of 2^-133).  A bf16 c may come from matrix instructions that
+ * add eight neighbouring products at a time on a grid of 2^-13 of the largest one, cut
+ * towards zero, and those sums in fp32: off by at most 7 * 2^-13 of the magnitudes' sum, and by less than
+ * 2^-16 of it for normal values, before it is rounded to bf16.
+ * scratch: device, 16-byte aligned, >= mv_f8_product_scratch_bytes(m, n, k) (0: may be NULL).
+ */
+size_t    mv_f8_product_scratch_bytes(int64_t m, int64_t n, int64_t k);
+mv_status mv_f8_product(const uint8_t* a_codes, int64_t ld_ab, const uint8_t* a_scales, int64_t ld_as,
+                        const uint8_t* b_codes, int64_t ld_bb, const uint8_t* b_scales, int64_t ld_bs, int64_t m,
+                        int64_t n, int64_t k, void* c, int32_t c_dtype, int64_t ld_c, void* scratch,
+                        size_t scratch_bytes, void* stream);
+
+/* A layer with weights w (n x k) held in 8 bits along k:  y (m x n) = q(x) w^T,  q: mv_f8_encode. */
+size_t    mv_f8_linear_scratch_bytes(int64_t m, int64_t n, int64_t k);
+mv_status mv_f8_linear(const void* x, int32_t x_dtype, int64_t ld_x, const uint8_t* w_codes, int64_t ld_bytes,
+                       const uint8_t* w_scales, int64_t ld_scales, int64_t m, int64_t n, int64_t k, void* y,
+                       int32_t y_dtype, int64_t ld_y, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * Its gradients from dy (m x n), as mv_mx_linear_grad's:
+ *   dx (m x k) = q(dy) wt^T            wt: the weights' COLUMNS, k rows of n values (mv_f8_encode_t of w)
+ *   dw (n x k) = qt(dy) qt(x)^T        qt: mv_f8_encode_t
+ * dx or dw may be NULL (then x, or wt_codes and wt_scales, may be too); x and dy have the same type.
+ */
+size_t    mv_f8_linear_grad_scratch_bytes(int64_t m, int64_t n, int64_t k);
+mv_status mv_f8_linear_grad(const void* x, int64_t ld_x, const void* dy, int64_t ld_dy, int32_t dtype,
+                            const uint8_t* wt_codes, int64_t ld_bytes, const uint8_t* wt_scales, int64_t ld_scales,
+                            int64_t m, int64_t n, int64_t k, void* dx, int32_t dx_dtype, int64_t ld_dx, void* dw,
+                            int32_t dw_dtype, int64_t ld_dw, void* scratch, size_t scratch_bytes, void* stream);
+
 /*
  * Measurement aid, not part of the method: enqueues a plain streaming copy of
  * `bytes` (a multiple of 16; dst and src 16-byte aligned DEVICE pointers, not

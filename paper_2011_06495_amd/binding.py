@@ -31,6 +31,9 @@ ABI_SYMBOLS = (
     "mv_mx_row_words", "mv_mx_row_scales", "mv_mx_encode", "mv_mx_encode_t", "mv_mx_decode", "mv_mx_aggregate",
     "mv_mx_product_scratch_bytes", "mv_mx_product", "mv_mx_linear_scratch_bytes", "mv_mx_linear",
     "mv_mx_linear_grad_scratch_bytes", "mv_mx_linear_grad",
+    "mv_f8_row_bytes", "mv_f8_row_scales", "mv_f8_encode", "mv_f8_encode_t", "mv_f8_decode",
+    "mv_f8_product_scratch_bytes", "mv_f8_product", "mv_f8_linear_scratch_bytes", "mv_f8_linear",
+    "mv_f8_linear_grad_scratch_bytes", "mv_f8_linear_grad",
 )
 
 
@@ -155,13 +158,25 @@ def load() -> ctypes.CDLL:
     L.mv_mx_encode_t.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp]
     L.mv_mx_decode.argtypes = [vp, i64, vp, i64, i64, i64, vp, i32, i64, vp]
     L.mv_mx_aggregate.argtypes = [vp, i64, vp, i64, i64, i64, vp, vp, vp]
-    for f in (L.mv_mx_product_scratch_bytes, L.mv_mx_linear_scratch_bytes, L.mv_mx_linear_grad_scratch_bytes):
+    L.mv_f8_row_bytes.argtypes = [i64]
+    L.mv_f8_row_bytes.restype = i64
+    L.mv_f8_row_scales.argtypes = [i64]
+    L.mv_f8_row_scales.restype = i64
+    L.mv_f8_encode.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp]
+    L.mv_f8_encode_t.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp]
+    L.mv_f8_decode.argtypes = [vp, i64, vp, i64, i64, i64, vp, i32, i64, vp]
+    for f in (L.mv_mx_product_scratch_bytes, L.mv_mx_linear_scratch_bytes, L.mv_mx_linear_grad_scratch_bytes,
+              L.mv_f8_product_scratch_bytes, L.mv_f8_linear_scratch_bytes, L.mv_f8_linear_grad_scratch_bytes):
         f.argtypes = [i64, i64, i64]
         f.restype = sz
     L.mv_mx_product.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, vp, sz, vp]
     L.mv_mx_linear.argtypes = [vp, i32, i64, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, vp, sz, vp]
     L.mv_mx_linear_grad.argtypes = [vp, i64, vp, i64, i32, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, vp, i32, i64,
                                     vp, sz, vp]
+    L.mv_f8_product.argtypes, L.mv_f8_linear.argtypes = L.mv_mx_product.argtypes, L.mv_mx_linear.argtypes
+    L.mv_f8_linear_grad.argtypes = L.mv_mx_linear_grad.argtypes
+    for f in (L.mv_f8_encode, L.mv_f8_encode_t, L.mv_f8_decode, L.mv_f8_product, L.mv_f8_linear, L.mv_f8_linear_grad):
+        f.restype = i32
     for f in (L.mv_clip_begin, L.mv_clip_bind, L.mv_clip_norms, L.mv_clip_grads, L.mv_clip_set_spin_limit, L.mv_clip_end, L.mv_mx_encode,
               L.mv_mx_encode_t, L.mv_mx_decode, L.mv_mx_aggregate, L.mv_mx_product, L.mv_mx_linear, L.mv_mx_linear_grad):
         f.restype = i32
@@ -685,3 +700,117 @@ def mv_mx_linear_grad(x, dy, wt_codes, wt_scales, dx, dw, scratch, stream=None) 
                                   *_scratch_of(scratch, device), _stream_handle(stream, dy))
     if st != MV_OK:
         raise MvError(st, "mv_mx_linear_grad")
+
+
+# ---- 8-bit floating point by blocks of 128 ----------------------------------
+
+
+def mv_f8_row_bytes(n: int) -> int:
+    return int(load().mv_f8_row_bytes(n))
+
+
+def mv_f8_row_scales(n: int) -> int:
+    return int(load().mv_f8_row_scales(n))
+
+
+def _bytes(codes, scales, rows: int, n: int, device: int, what: str = "codes"):
+    """(address, row stride) of 8-bit codes and their scales, for `rows` rows of n values."""
+    (r, length), (q, places) = codes.shape, scales.shape
+    (ld_c, step_c), (ld_s, step_s) = codes.stride(), scales.stride()
+    blocks = (n + 127) // 128
+    if (r < rows or q < rows or length < 128 * blocks or places < (blocks + 3) // 4 * 4 or step_c != 1 or step_s != 1
+            or codes.get_device() != device or scales.get_device() != device or codes.element_size() != 1
+            or scales.element_size() != 1):
+        raise ValueError("%s and scales have to be %d rows of mv_f8_row_bytes(%d) and mv_f8_row_scales(%d) bytes or more, on the "
+                         "same GPU" % (what, rows, n, n))
+    return codes.data_ptr(), ld_c, scales.data_ptr(), ld_s
+
+
+def mv_f8_encode(vals, codes, scales, stream=None) -> None:
+    """vals: rows x n float32 or bfloat16; codes: rows x mv_f8_row_bytes(n) uint8 (out); scales: rows x
+    mv_f8_row_scales(n) uint8 (out)."""
+    rows, n = vals.shape
+    device = vals.get_device()
+    v, d, ld = _matrix(vals, "vals", rows, n, device)
+    st = (_lib or load()).mv_f8_encode(v, d, ld, rows, n, *_bytes(codes, scales, rows, n, device), _stream_handle(stream, vals))
+    if st != MV_OK:
+        raise MvError(st, "mv_f8_encode")
+
+
+def mv_f8_encode_t(vals, codes, scales, stream=None) -> None:
+    """The columns of vals (rows x n): codes: n x mv_f8_row_bytes(rows), scales: n x mv_f8_row_scales(rows) (out)."""
+    rows, n = vals.shape
+    device = vals.get_device()
+    v, d, ld = _matrix(vals, "vals", rows, n, device)
+    st = (_lib or load()).mv_f8_encode_t(v, d, ld, rows, n, *_bytes(codes, scales, n, rows, device), _stream_handle(stream, vals))
+    if st != MV_OK:
+        raise MvError(st, "mv_f8_encode_t")
+
+
+def mv_f8_decode(codes, scales, out, stream=None) -> None:
+    """out: rows x n float32 or bfloat16 (out), what the codes stand for."""
+    rows, n = out.shape
+    device = out.get_device()
+    o, d, ld = _matrix(out, "out", rows, n, device)
+    st = (_lib or load()).mv_f8_decode(*_bytes(codes, scales, rows, n, device), rows, n, o, d, ld, _stream_handle(stream, out))
+    if st != MV_OK:
+        raise MvError(st, "mv_f8_decode")
+
+
+def mv_f8_product_scratch_bytes(m: int, n: int, k: int) -> int:
+    return (_lib or load()).mv_f8_product_scratch_bytes(m, n, k)
+
+
+def mv_f8_product(a_codes, a_scales, b_codes, b_scales, k: int, out, scratch=None, stream=None) -> None:
+    """out (m x n, float32 or bfloat16) = a b^T: a of m rows and b of n rows, k values each, in 8 bits along k.
+    scratch: mv_f8_product_scratch_bytes(m, n, k) bytes."""
+    m, n = out.shape
+    device = out.get_device()
+    o, d, ld = _matrix(out, "out", m, n, device)
+    st = (_lib or load()).mv_f8_product(*_bytes(a_codes, a_scales, m, k, device, "a_codes"), *_bytes(b_codes, b_scales, n, k, device, "b_codes"),
+                              m, n, k, o, d, ld, *_scratch_of(scratch, device), _stream_handle(stream, out))
+    if st != MV_OK:
+        raise MvError(st, "mv_f8_product")
+
+
+def mv_f8_linear_scratch_bytes(m: int, n: int, k: int) -> int:
+    return (_lib or load()).mv_f8_linear_scratch_bytes(m, n, k)
+
+
+def mv_f8_linear(x, w_codes, w_scales, out, scratch, stream=None) -> None:
+    """out (m x n) = q(x) w^T: x m x k, rounded to 8 bits as mv_f8_encode does; w: n rows of k values in 8 bits."""
+    m, k = x.shape
+    n = out.shape[1]
+    device = out.get_device()
+    a, xd, ld_x = _matrix(x, "x", m, k, device)
+    o, d, ld = _matrix(out, "out", m, n, device)
+    st = (_lib or load()).mv_f8_linear(a, xd, ld_x, *_bytes(w_codes, w_scales, n, k, device, "w_codes"), m, n, k, o, d, ld,
+                             *_scratch_of(scratch, device), _stream_handle(stream, out))
+    if st != MV_OK:
+        raise MvError(st, "mv_f8_linear")
+
+
+def mv_f8_linear_grad_scratch_bytes(m: int, n: int, k: int) -> int:
+    return (_lib or load()).mv_f8_linear_grad_scratch_bytes(m, n, k)
+
+
+def mv_f8_linear_grad(x, dy, wt_codes, wt_scales, dx, dw, scratch, stream=None) -> None:
+    """dx (m x k) = q(dy) wt^T and dw (n x k) = qt(dy) qt(x)^T of mv_f8_linear's product; wt: the weights' columns, k
+    rows of n values in 8 bits.  dx (with wt_codes and wt_scales) or dw (with x) may be None; x and dy have one type."""
+    m, n = dy.shape
+    device = dy.get_device()
+    k = dx.shape[1] if dx is not None else x.shape[1]
+    g, yd, ld_dy = _matrix(dy, "dy", m, n, device)
+    a, ld_x, w, o, od, ld_dx, p, pd, ld_dw = 0, 0, (0, 0, 0, 0), 0, 0, 0, 0, 0, 0
+    if dx is not None:
+        w = _bytes(wt_codes, wt_scales, k, n, device, "wt_codes")
+        o, od, ld_dx = _matrix(dx, "dx", m, k, device)
+    if dw is not None:
+        a, xd, ld_x = _matrix(x, "x", m, k, device)
+        if xd != yd:
+            raise ValueError("x and dy have to be of one type")
+        p, pd, ld_dw = _matrix(dw, "dw", n, k, device)
+    st = (_lib or load()).mv_f8_linear_grad(a, ld_x, g, ld_dy, yd, *w, m, n, k, o, od, ld_dx, p, pd, ld_dw,
+                                  *_scratch_of(scratch, device), _stream_handle(stream, dy))
+    if st != MV_OK:
+        raise MvError(st, "mv_f8_linear_grad")

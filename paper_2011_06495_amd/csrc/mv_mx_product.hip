@@ -7,13 +7,11 @@
 // hold does not matter as long as both factors agree.  So a group takes four consecutive blocks of each 16: 64
 // consecutive bytes of codes for four instructions, and their four scales in one word.
 #include "mv_mx.hpp"
+#include "mv_product.hpp"
 
 #include <type_traits>
 
 namespace mvx {
-
-typedef int   i32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 struct Factor {
     const uint32_t* codes;
@@ -47,35 +45,6 @@ __device__ __forceinline__ void load_four(const Factor& f, int64_t row, int64_t 
     }
     v.scales = w;
 }
-
-// Where results go: fp32 or bf16, rounded once.
-struct Out {
-    void*    p;
-    uint32_t bf16;
-    __device__ __forceinline__ void put(int64_t at, float x) const
-    {
-        if (bf16) static_cast<uint16_t*>(p)[at] = (uint16_t)narrow(x);
-        else static_cast<float*>(p)[at] = x;
-    }
-    // four consecutive ones of which `live` are left
-    __device__ __forceinline__ void put4(int64_t at, int64_t live, const f32x4& v) const
-    {
-        typedef uint16_t u16x4u __attribute__((ext_vector_type(4), aligned(2)));
-        if (live >= 4) {
-            if (bf16)
-                *reinterpret_cast<u16x4u*>(static_cast<uint16_t*>(p) + at) =
-                    u16x4u{(uint16_t)narrow(v.x), (uint16_t)narrow(v.y), (uint16_t)narrow(v.z), (uint16_t)narrow(v.w)};
-            else
-                *reinterpret_cast<f32x4u*>(static_cast<float*>(p) + at) = v;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 3; ++e)
-                if (e < live) put(at + e, v[e]);
-        }
-    }
-};
-
-inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 constexpr int kTile = 64;           // rows of each factor that a wavefront takes
 constexpr int kProductThreads = 256;
@@ -135,12 +104,8 @@ __global__ __launch_bounds__(kProductThreads) void mv_mx_product_kernel(Factor a
 // into LDS beside them (without it 111), the reads from there and the end, where 67 MB leave.  With 512 values of k the results are all: 4900 x 512 by 4608 to fp32 26 us with the launch
 // that quantises (4), a fill of those 90 MB 15.5.
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
 constexpr int kStepBlocks = 8;
 constexpr int kScalePitch = 20;     // bytes between the rows' scales in LDS: 16 and a word against bank conflicts
-
-constexpr int kNoLoads = 0x0F70;    // s_waitcnt: none of the vector loads in flight, the other counters as they are
 
 template <int S>
 __device__ __forceinline__ f32x16 mfma32(const u32x4& a, uint32_t a_scale, const u32x4& b, uint32_t b_scale, f32x16 c)
@@ -148,16 +113,6 @@ __device__ __forceinline__ f32x16 mfma32(const u32x4& a, uint32_t a_scale, const
     const i32x8 x = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, y = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, S, (int)a_scale, S, (int)b_scale);
 }
-
-// One or two products of a launch, the first workgroups are the first one's.  A launch from the host takes a microsecond
-// longer with 400 bytes of arguments than with 8, so a single product's have room for one only.
-template <typename P, bool PAIR>
-struct Launch {
-    P        products[PAIR ? 2 : 1];
-    uint32_t firsts;
-    __device__ __forceinline__ const P& product() const { return products[PAIR && blockIdx.x >= firsts ? 1 : 0]; }
-    __device__ __forceinline__ uint32_t id() const { return PAIR && blockIdx.x >= firsts ? blockIdx.x - firsts : blockIdx.x; }
-};
 
 // One product and how it is cut: tiles_m x tiles_n tiles, `splits` runs of steps_each steps each.  With several splits c is
 // fp32 and holds their sums one after the other, split_c apart.
@@ -168,17 +123,6 @@ struct Product {
     int64_t  ld_c, split_c;
     uint32_t past;                  // store past the caches
 };
-
-// Which tile a workgroup takes: consecutive workgroups run on eight dies with an L2 of their own, so a die gets a run of
-// consecutive tiles, and those go down eight tiles of a before they go along b.
-__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn)
-{
-    const uint32_t all = tiles_m * tiles_n, each = all / 8, more = all % 8, die = id % 8;
-    const uint32_t t = die * each + min(die, more) + id / 8;
-    const uint32_t band = t / (8 * tiles_n), first = band * 8, high = min(8u, tiles_m - first), in = t - first * tiles_n;
-    tm = first + in % high;
-    tn = in / high;
-}
 
 // A wavefront's share of one instruction's blocks: rows of a and of b.
 template <int MT, int NT>
@@ -391,29 +335,11 @@ __global__ __launch_bounds__(64 * WM * WN, BUFFERS == 1 ? 3 : 2) void mv_mx_prod
     }
 }
 
-// c = the sum of the splits: a group of `lanes` threads takes four results, each thread every lanes-th split, and their
-// sums are added in order.
 __global__ __launch_bounds__(256) void mv_mx_product_join_kernel(const float* __restrict__ parts, uint32_t splits, uint32_t lanes,
                                                                  int64_t m, int64_t n, int64_t split_c, int64_t quads, Out c,
                                                                  int64_t ld_c)
 {
-    __shared__ f32x4 sums[256];
-    const uint32_t per = 256 / lanes, lane = threadIdx.x / per;          // a group's threads lie `per` apart
-    const int64_t at = (int64_t)blockIdx.x * per + threadIdx.x % per;
-    const int64_t i = at / quads, j = at % quads * 4;
-    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (i < m) {
-        const float* p = parts + i * (quads * 4) + j;
-#pragma unroll 4
-        for (uint32_t s = lane; s < splits; s += lanes) sum += *reinterpret_cast<const f32x4*>(p + s * split_c);
-    }
-    if (lanes > 1) {                                                     // uniform
-        sums[threadIdx.x] = sum;
-        __syncthreads();
-        if (lane) return;
-        for (uint32_t l = 1; l < lanes; ++l) sum += sums[l * per + threadIdx.x];
-    }
-    if (i < m) c.put4(i * ld_c + j, n - j, sum);
+    join_splits(parts, splits, lanes, m, n, split_c, quads, c, ld_c);
 }
 
 // ---- few rows of one factor ------------------------------------------------------------------------------------------
@@ -807,17 +733,11 @@ static Cut cut_of(int64_t m, int64_t n, int64_t k, int mt, int64_t beside = 0)
 constexpr int64_t kFewSteps = 4, kUnits = 256;
 inline bool few_steps(int64_t k) { return blocks_of(k) <= kFewSteps * kStepBlocks; }
 static bool large(int64_t m, int64_t n) { return ((m + 255) / 256) * ((n + 255) / 256) >= 192; }
-inline int64_t quads_of(int64_t n) { return (n + 3) / 4; }
 inline size_t parts_bytes(int64_t m, int64_t n, int64_t k)
 {
     const uint32_t splits = cut_of(m, n, k, 2).splits;
     return splits > 1 ? up256((size_t)splits * (size_t)m * (size_t)quads_of(n) * 16) : 0;
 }
-
-// Results of 16 MB and more, which are half of the L2s, are stored past them.  Smaller ones, and sums that are added up right
-// away, are a little faster stored as usual: 1000 x 1000 by 1000 7.8 us, past the caches 8.0; 130 x 130 by 8000 14.1 : 16.3.  From
-// 8 to 67 MB a product alone takes as long either way (4096 x 8192 by 8192 140.6 : 140.5).
-constexpr int64_t kPastBytes = 16 << 20;
 
 // A product that is asked for: c = a b^T, m rows and n rows of k values.
 struct Wanted {
@@ -972,12 +892,6 @@ static mv_status launch_few_values(const FewCut& cut, const void* x, int64_t ld_
     const FewProduct<X> p = few_product(w, Few<X>{static_cast<const X*>(x), ld_x, nullptr, 0, (uint32_t)m}, k, y, 1, ld_y);
     return launch_few(&p, &cut, 1, st);
 }
-
-inline bool scratch_valid(const void* p, size_t have, size_t need)
-{
-    return need == 0 || (p && have >= need && (reinterpret_cast<uintptr_t>(p) & 15) == 0);
-}
-inline bool sizes_valid(int64_t m, int64_t n, int64_t k) { return size_valid(m) && size_valid(n) && size_valid(k); }
 
 }  // namespace mvx
 
