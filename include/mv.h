@@ -601,6 +601,94 @@ mv_status mv_f8_linear_grad(const void* x, int64_t ld_x, const void* dy, int64_t
                             int64_t m, int64_t n, int64_t k, void* dx, int32_t dx_dtype, int64_t ld_dx, void* dw,
                             int32_t dw_dtype, int64_t ld_dw, void* scratch, size_t scratch_bytes, void* stream);
 
+/* ---- layer norm ---------------------------------------------------------------- */
+
+/*
+ * For every row x of n values (fp32 or bf16, aligned to its element, any row stride >= n):
+ *
+ *   mean = sum(x) / n,  rstd = 1 / sqrt(sum((x - mean)^2) / n + eps)
+ *   y    = (x - mean) rstd gamma + beta            rounded once to y's type
+ *
+ * gamma, beta: n values of one type, or NULL for 1 and 0 (either).  mean, rstd: rows fp32
+ * out, what the backward pass takes; either may be NULL.  y may be x itself, with its type
+ * and stride.  Sums are fp32; the squares are those of differences from the mean, so rows far from
+ * zero keep their digits.  A row that holds an infinity or a NaN, or whose sums leave fp32, has no
+ * finite results, and no other row is touched by it.  eps >= 0 and finite; with eps 0 a row of
+ * equal values has an infinite rstd, or one as large as its mean's rounding makes it.
+ *
+ * These calls run on the CURRENT device, are enqueued on `stream` and allocate nothing.
+ * 1 <= rows, n < 2^31.  The order of all sums follows from sizes and types: equal calls
+ * give equal results.  Errors: MV_ERR_INVALID_ARG, MV_ERR_DEVICE.
+ */
+mv_status mv_layernorm_forward(const void* x, int32_t x_dtype, int64_t ld_x, int64_t rows, int64_t n, const void* gamma,
+                               const void* beta, int32_t weight_dtype, float eps, void* y, int32_t y_dtype, int64_t ld_y,
+                               float* mean, float* rstd, void* stream);
+
+/*
+ * The gradients, with h = (x - mean) rstd and d = dy gamma:
+ *
+ *   dx     = rstd (d - sum(d) / n - h sum(d h) / n)     rounded once to dx's type
+ *   dgamma = sum over rows of dy h,  dbeta = sum over rows of dy      (n fp32 each)
+ *
+ * x and dy have the same type; mean, rstd as the forward pass left them.  dx, dgamma and
+ * dbeta may each be NULL, not all three; dx may be dy or x itself, with its type and stride.
+ * scratch: device, 16-byte aligned, >= mv_layernorm_scratch_bytes(rows, n).
+ */
+size_t    mv_layernorm_scratch_bytes(int64_t rows, int64_t n);   /* 0 for sizes outside 1 .. 2^31-1 */
+mv_status mv_layernorm_backward(const void* x, int64_t ld_x, const void* dy, int64_t ld_dy, int32_t dtype, int64_t rows,
+                                int64_t n, const void* gamma, int32_t weight_dtype, const float* mean, const float* rstd,
+                                void* dx, int32_t dx_dtype, int64_t ld_dx, float* dgamma, float* dbeta, void* scratch,
+                                size_t scratch_bytes, void* stream);
+
+/* ---- distillation from a teacher's top logits ---------------------------------- */
+
+/*
+ * A worker that learns from a teacher gets, for each row of its own n logits z, the
+ * teacher's best ones: `top` coordinates idx[j] and logits t[j].  With a temperature T > 0,
+ *
+ *   q = softmax(z / T),  s = softmax(z),  p = softmax(t / T) over the row's list
+ *   loss  = soft T^2 sum_j p_j (log p_j - log q[idx_j])  +  hard (-log s[label])
+ *   dz[v] = g ( soft T (P q[v] - sum_{j: idx_j = v} p_j)  +  hard (s[v] - [v = label]) )
+ *
+ * An entry whose idx is outside 0 .. n-1 is not in the list (so shorter lists are filled
+ * with -1), one whose t is -infinity has p = 0 and no part in the sums; P is 1, or 0 for a
+ * list with neither, which has no first term.  A coordinate listed twice counts twice.  A label
+ * outside 0 .. n-1, or labels NULL, has no second term; neither has a term a weight of 0.
+ * A row without terms has loss 0 and dz 0, whatever its logits are.  A logit of
+ * -infinity has q = s = 0 (an infinite loss where the teacher lists it); NaN, +infinity or
+ * nothing but -infinity among a row's logits, and NaN or +infinity in its list, make loss and
+ * dz NaN, of this row only.
+ *
+ *   logits      rows x n, fp32 or bf16, any row stride >= n
+ *   idx, t      rows x top; int32, and fp32 or bf16; any row strides >= top; top 0 .. 4096,
+ *               with 0 (or soft 0) both may be NULL
+ *   labels      rows int32 or NULL
+ *   loss        rows fp32 out; may be NULL where dz is wanted
+ *   stats       rows x 3 fp32 out or NULL: the largest z, sum exp((z - largest) / T) and
+ *               sum exp(z - largest); 0 for a sum that no row needs (soft 0 or top 0; hard 0
+ *               or labels NULL)
+ *   grad        rows fp32 or NULL for 1: g, the gradient that arrives at each loss
+ *   dz          rows x n out, fp32 or bf16, or NULL; may be logits itself, with its type
+ *               and stride
+ *
+ * mv_distill_loss forms loss and, where dz is wanted, the gradient in the same call;
+ * mv_distill_grad forms the gradient alone from the stats of a call with the same logits,
+ * lists, labels and weights.  Sums are fp32 in an order that follows from sizes and types.
+ * soft and hard are finite, T is 2^-60 .. 2^60.  1 <= rows, n < 2^31.  Runs on the CURRENT
+ * device, enqueued on `stream`; allocates nothing.  scratch: device, 16-byte aligned,
+ * >= mv_distill_scratch_bytes(rows, n) (0: may be NULL).
+ * Errors: MV_ERR_INVALID_ARG, MV_ERR_DEVICE.
+ */
+size_t    mv_distill_scratch_bytes(int64_t rows, int64_t n);
+mv_status mv_distill_loss(const void* logits, int32_t dtype, int64_t ld_z, int64_t rows, int64_t n, const int32_t* idx,
+                          int64_t ld_idx, const void* t, int32_t t_dtype, int64_t ld_t, int64_t top, const int32_t* labels,
+                          float temperature, float soft, float hard, float* loss, float* stats, const float* grad, void* dz,
+                          int32_t dz_dtype, int64_t ld_dz, void* scratch, size_t scratch_bytes, void* stream);
+mv_status mv_distill_grad(const void* logits, int32_t dtype, int64_t ld_z, int64_t rows, int64_t n, const int32_t* idx,
+                          int64_t ld_idx, const void* t, int32_t t_dtype, int64_t ld_t, int64_t top, const int32_t* labels,
+                          float temperature, float soft, float hard, const float* stats, const float* grad, void* dz,
+                          int32_t dz_dtype, int64_t ld_dz, void* stream);
+
 /*
  * Measurement aid, not part of the method: enqueues a plain streaming copy of
  * `bytes` (a multiple of 16; dst and src 16-byte aligned DEVICE pointers, not

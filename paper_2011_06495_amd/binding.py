@@ -34,6 +34,8 @@ ABI_SYMBOLS = (
     "mv_f8_row_bytes", "mv_f8_row_scales", "mv_f8_encode", "mv_f8_encode_t", "mv_f8_decode",
     "mv_f8_product_scratch_bytes", "mv_f8_product", "mv_f8_linear_scratch_bytes", "mv_f8_linear",
     "mv_f8_linear_grad_scratch_bytes", "mv_f8_linear_grad",
+    "mv_layernorm_forward", "mv_layernorm_scratch_bytes", "mv_layernorm_backward",
+    "mv_distill_scratch_bytes", "mv_distill_loss", "mv_distill_grad",
 )
 
 
@@ -175,7 +177,16 @@ def load() -> ctypes.CDLL:
                                     vp, sz, vp]
     L.mv_f8_product.argtypes, L.mv_f8_linear.argtypes = L.mv_mx_product.argtypes, L.mv_mx_linear.argtypes
     L.mv_f8_linear_grad.argtypes = L.mv_mx_linear_grad.argtypes
-    for f in (L.mv_f8_encode, L.mv_f8_encode_t, L.mv_f8_decode, L.mv_f8_product, L.mv_f8_linear, L.mv_f8_linear_grad):
+    L.mv_layernorm_forward.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, f32, vp, i32, i64, vp, vp, vp]
+    L.mv_layernorm_backward.argtypes = [vp, i64, vp, i64, i32, i64, i64, vp, i32, vp, vp, vp, i32, i64, vp, vp, vp, sz, vp]
+    listed = [vp, i32, i64, i64, i64, vp, i64, vp, i32, i64, i64, vp, f32, f32, f32]
+    L.mv_distill_loss.argtypes = listed + [vp, vp, vp, vp, i32, i64, vp, sz, vp]
+    L.mv_distill_grad.argtypes = listed + [vp, vp, vp, i32, i64, vp]
+    for f in (L.mv_layernorm_scratch_bytes, L.mv_distill_scratch_bytes):
+        f.argtypes = [i64, i64]
+        f.restype = sz
+    for f in (L.mv_f8_encode, L.mv_f8_encode_t, L.mv_f8_decode, L.mv_f8_product, L.mv_f8_linear, L.mv_f8_linear_grad,
+              L.mv_layernorm_forward, L.mv_layernorm_backward, L.mv_distill_loss, L.mv_distill_grad):
         f.restype = i32
     for f in (L.mv_clip_begin, L.mv_clip_bind, L.mv_clip_norms, L.mv_clip_grads, L.mv_clip_set_spin_limit, L.mv_clip_end, L.mv_mx_encode,
               L.mv_mx_encode_t, L.mv_mx_decode, L.mv_mx_aggregate, L.mv_mx_product, L.mv_mx_linear, L.mv_mx_linear_grad):
@@ -814,3 +825,115 @@ def mv_f8_linear_grad(x, dy, wt_codes, wt_scales, dx, dw, scratch, stream=None) 
                                   *_scratch_of(scratch, device), _stream_handle(stream, dy))
     if st != MV_OK:
         raise MvError(st, "mv_f8_linear_grad")
+
+
+# ---- layer norm ---------------------------------------------------------------
+
+
+def _weights(a, b, n: int, device: int):
+    """(address of gamma, address of beta, mv_dtype) of float32 or bfloat16 vectors of one type, either may be None."""
+    d, at = None, []
+    for t, what in ((a, "gamma"), (b, "beta")):
+        if t is None:
+            at.append(0)
+            continue
+        kind = _value_type(t, what)
+        if t.numel() != n or not t.is_contiguous() or t.get_device() != device or (d is not None and kind != d):
+            raise ValueError("%s has to be %d contiguous values on the same GPU, of the other weights' type" % (what, n))
+        d = kind
+        at.append(t.data_ptr())
+    return at[0], at[1], MV_F32 if d is None else d
+
+
+def mv_layernorm_forward(x, gamma, beta, eps: float, out, mean=None, rstd=None, stream=None) -> None:
+    """out (rows x n, float32 or bfloat16; may be x) = the layer norm of x's rows; gamma, beta: n float32 or bfloat16 values
+    or None; mean, rstd: rows float32 (out) or None, for mv_layernorm_backward."""
+    rows, n = x.shape
+    device = x.get_device()
+    a, xd, ld_x = _matrix(x, "x", rows, n, device)
+    o, od, ld_o = _matrix(out, "out", rows, n, device)
+    st = (_lib or load()).mv_layernorm_forward(a, xd, ld_x, rows, n, *_weights(gamma, beta, n, device), eps, o, od, ld_o,
+                                               _float32(mean, "mean", rows, device), _float32(rstd, "rstd", rows, device),
+                                               _stream_handle(stream, x))
+    if st != MV_OK:
+        raise MvError(st, "mv_layernorm_forward")
+
+
+def mv_layernorm_scratch_bytes(rows: int, n: int) -> int:
+    return (_lib or load()).mv_layernorm_scratch_bytes(rows, n)
+
+
+def mv_layernorm_backward(x, dy, gamma, mean, rstd, dx, dgamma, dbeta, scratch, stream=None) -> None:
+    """The gradients of mv_layernorm_forward's x (dx: rows x n, may be dy or x), gamma and beta (n float32 each) from dy; each
+    may be None.  x and dy have one type; scratch: mv_layernorm_scratch_bytes(rows, n) bytes."""
+    rows, n = x.shape
+    device = x.get_device()
+    a, xd, ld_x = _matrix(x, "x", rows, n, device)
+    g, yd, ld_dy = _matrix(dy, "dy", rows, n, device)
+    if xd != yd:
+        raise ValueError("x and dy have to be of one type")
+    o, od, ld_o = _matrix(dx, "dx", rows, n, device) if dx is not None else (0, 0, 0)
+    w, _, wd = _weights(gamma, None, n, device)
+    st = (_lib or load()).mv_layernorm_backward(a, ld_x, g, ld_dy, xd, rows, n, w, wd, _float32(mean, "mean", rows, device),
+                                                _float32(rstd, "rstd", rows, device), o, od, ld_o, _float32(dgamma, "dgamma", n, device),
+                                                _float32(dbeta, "dbeta", n, device), *_scratch_of(scratch, device),
+                                                _stream_handle(stream, x))
+    if st != MV_OK:
+        raise MvError(st, "mv_layernorm_backward")
+
+
+# ---- distillation from a teacher's top logits ---------------------------------
+
+
+def _int32(t, what: str, shape, device: int) -> int:
+    """Address of an int32 tensor of this shape on the GPU whose last dimension lies in one piece; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype.itemsize != 4 or t.dtype.is_floating_point or tuple(t.shape) != shape or t.get_device() != device or (
+            shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError("%s has to be int32 of shape %s on the same GPU, its rows in one piece" % (what, shape))
+    return t.data_ptr()
+
+
+def _listed(logits, idx, top, labels):
+    """The arguments that both calls begin with, up to the labels, and the GPU."""
+    rows, n = logits.shape
+    device = logits.get_device()
+    z, zd, ld_z = _matrix(logits, "logits", rows, n, device)
+    i, ld_i, t, td, ld_t, k = 0, 0, 0, 0, 0, 0
+    if idx is not None and idx.shape[1] > 0:
+        k = idx.shape[1]
+        i, ld_i = _int32(idx, "idx", (rows, k), device), idx.stride(0) if rows > 1 else max(idx.stride(0), k)
+        t, td, ld_t = _matrix(top, "top", rows, k, device)
+    return (z, zd, ld_z, rows, n, i, ld_i, t, td, ld_t, k, _int32(labels, "labels", (rows,), device)), device
+
+
+def mv_distill_scratch_bytes(rows: int, n: int) -> int:
+    return (_lib or load()).mv_distill_scratch_bytes(rows, n)
+
+
+def mv_distill_loss(logits, idx, top, labels, temperature: float, soft: float, hard: float, loss, scratch=None, stats=None, dz=None,
+                    grad=None, stream=None) -> None:
+    """loss: rows float32 (out; may be None where dz is wanted); logits: rows x n float32 or bfloat16; idx, top: the teacher's
+    coordinates (rows x k int32, any other than 0 .. n-1 is no entry) and logits (rows x k float32 or bfloat16), or both None;
+    labels: rows int32 or None; stats: rows x 3 float32 (out) or None, for mv_distill_grad; dz: rows x n (out; may be logits)
+    or None, with grad, rows float32, the gradients that arrive at the losses, None for 1."""
+    at, device = _listed(logits, idx, top, labels)
+    rows, n = at[3], at[4]
+    o, od, ld_o = _matrix(dz, "dz", rows, n, device) if dz is not None else (0, 0, 0)
+    st = (_lib or load()).mv_distill_loss(*at, temperature, soft, hard, _float32(loss, "loss", rows, device),
+                                          _float32(stats, "stats", 3 * rows, device), _float32(grad, "grad", rows, device), o, od, ld_o,
+                                          *_scratch_of(scratch, device), _stream_handle(stream, logits))
+    if st != MV_OK:
+        raise MvError(st, "mv_distill_loss")
+
+
+def mv_distill_grad(logits, idx, top, labels, temperature: float, soft: float, hard: float, stats, dz, grad=None, stream=None) -> None:
+    """dz of mv_distill_loss from the stats of a call with the same arguments."""
+    at, device = _listed(logits, idx, top, labels)
+    rows, n = at[3], at[4]
+    o, od, ld_o = _matrix(dz, "dz", rows, n, device)
+    st = (_lib or load()).mv_distill_grad(*at, temperature, soft, hard, _float32(stats, "stats", 3 * rows, device),
+                                          _float32(grad, "grad", rows, device), o, od, ld_o, _stream_handle(stream, logits))
+    if st != MV_OK:
+        raise MvError(st, "mv_distill_grad")

@@ -9,10 +9,11 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libmv.so")
 SOURCES = [os.path.join(CSRC, "mv_api.hip"), os.path.join(CSRC, "mv_codec.hip"),
            os.path.join(CSRC, "mv_quant.hip"), os.path.join(CSRC, "mv_clip.hip"), os.path.join(CSRC, "mv_mx.hip"),
-           os.path.join(CSRC, "mv_mx_product.hip"), os.path.join(CSRC, "mv_f8.hip"), os.path.join(CSRC, "mv_f8_product.hip")]
+           os.path.join(CSRC, "mv_mx_product.hip"), os.path.join(CSRC, "mv_f8.hip"), os.path.join(CSRC, "mv_f8_product.hip"),
+           os.path.join(CSRC, "mv_layernorm.hip"), os.path.join(CSRC, "mv_distill.hip")]
 HEADERS = [os.path.join(CSRC, h) for h in ("mv_kernels.hpp", "mv_common.hpp", "mv_stream.hpp", "mv_select.hpp",
                                                "mv_votes.hpp", "mv_mask.hpp", "mv_add_drop.hpp", "mv_random_select.hpp",
-                                               "mv_small.hpp", "mv_mx.hpp", "mv_product.hpp", "mv_f8.hpp")] + [
+                                               "mv_small.hpp", "mv_mx.hpp", "mv_product.hpp", "mv_f8.hpp", "mv_rows.hpp")] + [
            os.path.join(os.path.dirname(_HERE), "include", "mv.h")]
 
 HIPCC_FLAGS = [

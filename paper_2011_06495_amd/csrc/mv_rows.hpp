@@ -1,0 +1,179 @@
+// Kernels that work row by row (layer norm, distillation): a row's values in registers, and sums over a row's threads.
+#pragma once
+
+#include "mv_mx.hpp"
+
+namespace mvr {
+
+using mvx::dtype_valid;
+using mvx::size_valid;
+using mvx::u32x4;
+using mvx::values_valid;
+
+constexpr float kInf = __builtin_inff();
+constexpr int   kNoLoads = 0x0F70;      // s_waitcnt: none of the vector loads in flight, the other counters as they are
+
+// A row is LANES threads' (64, 256 or 1024); thread t has chunks t, t + LANES, ... of 16 bytes.
+template <typename T>
+constexpr int kChunk = 16 / (int)sizeof(T);
+
+// Rows go round a workgroup's groups of LANES threads.
+template <int LANES>
+constexpr int kThreadsOf = LANES < 256 ? 256 : LANES;
+
+template <typename T>
+struct Chunk;
+template <>
+struct Chunk<float> {
+    float x[4];
+    __device__ __forceinline__ void load(const float* p, int64_t live) { mvx::load4(p, live, x); }
+    __device__ __forceinline__ float at(int i) const { return x[i]; }
+};
+template <>
+struct Chunk<uint16_t> {
+    uint32_t x[4];
+    __device__ __forceinline__ void load(const uint16_t* p, int64_t live) { mvx::load8(p, live, x); }
+    __device__ __forceinline__ float at(int i) const { return i & 1 ? __uint_as_float(x[i / 2] & 0xFFFF0000u) : mvx::widen(x[i / 2]); }
+};
+
+// Chunk-sized runs of fp32 or bf16 at any address, in a type that only the call knows.
+struct Any {
+    const void* p;
+    uint32_t    bf16;
+    template <int V>
+    __device__ __forceinline__ void load(int64_t at, int64_t live, float (&x)[V]) const
+    {
+#pragma unroll
+        for (int h = 0; h < V; h += 4) {
+            if (!bf16) {
+                float y[4];
+                mvx::load4(static_cast<const float*>(p) + at + h, live - h, y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[h + i] = y[i];
+            } else {
+                typedef uint16_t u16x4u __attribute__((ext_vector_type(4), aligned(2)));
+                const uint16_t* q = static_cast<const uint16_t*>(p) + at + h;
+                if (live - h >= 4) {
+                    const u16x4u w = *reinterpret_cast<const u16x4u*>(q);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[h + i] = mvx::widen(w[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[h + i] = h + i < live ? mvx::widen(q[i]) : 0.0f;
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ float at(int64_t i) const
+    {
+        return bf16 ? mvx::widen(static_cast<const uint16_t*>(p)[i]) : static_cast<const float*>(p)[i];
+    }
+};
+struct AnyOut {
+    void*    p;
+    uint32_t bf16;
+    template <int V>
+    __device__ __forceinline__ void store(int64_t at, int64_t live, const float (&x)[V]) const
+    {
+        if (!bf16) {
+#pragma unroll
+            for (int h = 0; h < V; h += 4) mvx::store4(static_cast<float*>(p) + at + h, live - h, x + h, V == 4);
+        } else if constexpr (V == 8) {
+            mvx::store8(static_cast<uint16_t*>(p) + at, live, x);
+        } else {
+            typedef uint16_t u16x4u __attribute__((ext_vector_type(4), aligned(2)));
+            uint16_t* q = static_cast<uint16_t*>(p) + at;
+            if (live >= 4) {
+                const u16x4u w = {(uint16_t)mvx::narrow(x[0]), (uint16_t)mvx::narrow(x[1]), (uint16_t)mvx::narrow(x[2]),
+                                  (uint16_t)mvx::narrow(x[3])};
+                __builtin_nontemporal_store(w, reinterpret_cast<u16x4u*>(q));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < live) q[i] = (uint16_t)mvx::narrow(x[i]);
+            }
+        }
+    }
+    __device__ __forceinline__ void put(int64_t i, float x) const
+    {
+        if (bf16) static_cast<uint16_t*>(p)[i] = (uint16_t)mvx::narrow(x);
+        else static_cast<float*>(p)[i] = x;
+    }
+};
+
+template <int CTRL>
+__device__ __forceinline__ float moved(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float lane_of(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+// Over a wavefront, the same in all lanes: pairs, fours, eights and sixteens of lanes by DPP, then those four.
+__device__ __forceinline__ float wave_sum(float v)
+{
+    v += moved<0xB1>(v);
+    v += moved<0x4E>(v);
+    v += moved<0x141>(v);
+    v += moved<0x140>(v);
+    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
+__device__ __forceinline__ float wave_max(float v)                       // of what is no NaN
+{
+    v = fmaxf(v, moved<0xB1>(v));
+    v = fmaxf(v, moved<0x4E>(v));
+    v = fmaxf(v, moved<0x141>(v));
+    v = fmaxf(v, moved<0x140>(v));
+    return fmaxf(fmaxf(lane_of(v, 0), lane_of(v, 16)), fmaxf(lane_of(v, 32), lane_of(v, 48)));
+}
+
+// Sums and maxima over the LANES threads of a row; all threads of the workgroup call these together.  Two calls in a row
+// use different halves of the LDS, so one barrier each is enough.
+template <int LANES>
+struct Across {
+    static constexpr int kWaves = LANES / 64;
+    float (*held)[2][kWaves];           // two halves of two values a wavefront
+    int   half = 0;
+    __device__ __forceinline__ explicit Across(float (*lds)[2][kWaves]) : held(lds) {}
+    __device__ __forceinline__ void sum2(float& a, float& b)
+    {
+        a = wave_sum(a), b = wave_sum(b);
+        if constexpr (LANES > 64) {
+            const int wave = threadIdx.x / 64;
+            if ((threadIdx.x & 63) == 0) held[half][0][wave] = a, held[half][1][wave] = b;
+            __syncthreads();
+            a = b = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) a += held[half][0][w], b += held[half][1][w];
+            half ^= 1;
+        }
+    }
+    __device__ __forceinline__ float sum(float a)
+    {
+        a = wave_sum(a);
+        if constexpr (LANES > 64) {
+            if ((threadIdx.x & 63) == 0) held[half][0][threadIdx.x / 64] = a;
+            __syncthreads();
+            a = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) a += held[half][0][w];
+            half ^= 1;
+        }
+        return a;
+    }
+    __device__ __forceinline__ float max(float a)
+    {
+        a = wave_max(a);
+        if constexpr (LANES > 64) {
+            if ((threadIdx.x & 63) == 0) held[half][0][threadIdx.x / 64] = a;
+            __syncthreads();
+            a = held[half][0][0];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) a = fmaxf(a, held[half][0][w]);
+            half ^= 1;
+        }
+        return a;
+    }
+};
+
+inline mv_status launched() { return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE; }
+
+}  // namespace mvr
