@@ -4,19 +4,26 @@
 //   loss  = soft T^2 sum p (log p - log q)  +  hard (-log s[label])
 //   dz[v] = g ( soft T (P q[v] - p listed for v)  +  hard (s[v] - [v = label]) )
 //
-// Only the logits are long, so memory bounds it: z is read once and dz written once where a row fits its workgroup's
-// registers, and then a row is: its maximum, its sums of exponentials, its list, and dz from the registers.  Longer rows are
-// cut into ranges, a workgroup each: their maxima and sums, which a second kernel joins and makes the loss of, and dz in a third.
+// Only the logits are long, so memory bounds it, and next to it the exponentials: two for each logit, or four where both
+// terms are wanted and T is not 1 (of T = 2 the second one is the first one's square).  Where dz is wanted with the loss and a
+// row fits a workgroup's registers, z is read once: its maximum, its sums, and dz from the registers, which take the next row's
+// logits as they become free.  Otherwise rows, or ranges of rows where there are few, stream by for their maxima and sums,
+// each thread's joined at the end, and once more for dz.
 //
-// dz has the same formula everywhere but at the listed coordinates and the label.  Those are written behind the rest of
-// their row, or range, by the workgroup that wrote it: one thread for each entry, which adds up what the list has for its
-// coordinate, in the list's order, where it is the first to name it.
+// A row's list is the first wavefront's, while the others have the logits.  dz has the same formula everywhere but at the
+// listed coordinates and the label.  Those are written behind the rest by the wavefront that wrote them before: one lane for
+// each entry, which adds up what the list has for its coordinate, in the list's order, where it is the first to name it.
 #include "mv_rows.hpp"
+
+#include <type_traits>
 
 namespace mvr {
 
 constexpr int64_t kMostTop = 4096;
 constexpr float   kLog2e = 1.44269504088896340736f;
+
+// Which exponentials the terms need: one, two, or one and its square.
+enum { kOne, kTwo, kSquare };
 
 struct Distill {
     const void*    z;
@@ -27,7 +34,7 @@ struct Distill {
     int64_t        ld_t;
     uint32_t       top;                 // 0: no first term
     const int32_t* labels;              // NULL: no second term
-    float          inv_t;               // 1 / T
+    float          inv_t, scale;        // 1 / T; what an exponent of the first kind is multiplied with, for a power of 2
     float          soft_loss, soft_grad, hard;      // soft T^2, soft T
     float *        loss, *stats;
     const float *  grad, *had;          // had: the stats of the call for the loss
@@ -39,95 +46,196 @@ struct Distill {
 };
 
 __device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, kInf); }    // one instruction
 
-// A row's list in LDS: coordinates, p, and the logits there; and what the row's terms come to.
+// The largest of a lane's logits.  Pairs of bf16 as they are: as whole numbers non-negative ones have their order, and are
+// above negative ones, which have the opposite order.
+template <typename T>
+struct Largest;
+template <>
+struct Largest<float> {
+    float most = -kInf;
+    __device__ __forceinline__ void look(const Chunk<float>& c)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = larger(c.x[i], most);
+    }
+    __device__ __forceinline__ float value() const { return most; }
+};
+template <>
+struct Largest<uint16_t> {
+    typedef int16_t  i16x2 __attribute__((ext_vector_type(2)));
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    i16x2 most = {-32768, -32768};
+    u16x2 least = {0xFF80u, 0xFF80u};   // -infinity
+    __device__ __forceinline__ void look(const Chunk<uint16_t>& c)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            most = __builtin_elementwise_max(most, __builtin_bit_cast(i16x2, c.x[i]));
+            least = __builtin_elementwise_min(least, __builtin_bit_cast(u16x2, c.x[i]));
+        }
+    }
+    __device__ __forceinline__ float value() const
+    {
+        const int16_t  m = most.x > most.y ? most.x : most.y;
+        const uint16_t l = least.x < least.y ? least.x : least.y;
+        return mvx::widen(m >= 0 ? (uint16_t)m : l);
+    }
+};
+
+// A logit's exponentials.
+template <int TERMS>
+struct Pair {
+    float a, b;
+    __device__ __forceinline__ Pair(float x, float scale)
+    {
+        a = power(x * scale);
+        b = TERMS == kTwo ? power(x * kLog2e) : TERMS == kSquare ? a * a : 0.0f;
+    }
+};
+template <typename T, int TERMS>
+__device__ __forceinline__ void add_up(const Chunk<T>& c, float largest, float scale, float& a, float& b)
+{
+#pragma unroll
+    for (int i = 0; i < kChunk<T>; ++i) {
+        const Pair<TERMS> e(c.at(i) - largest, scale);
+        a += e.a;
+        if (TERMS != kOne) b += e.b;
+    }
+}
+
+// ---- the list ------------------------------------------------------------------------------------------------------
+
+// A row's list in LDS: coordinates, p, and the logits there; entry `room` is the label.
 struct List {
     int32_t* idx;
     float *  p, *z;
 };
+__host__ __device__ constexpr uint32_t room_of(uint32_t top) { return (top + 3) / 4 * 4; }
+__host__ __device__ constexpr size_t   list_bytes(uint32_t top) { return (size_t)(room_of(top) + 4) * 12; }
+__device__ __forceinline__ List list_at(void* lds, uint32_t top)
+{
+    const uint32_t each = room_of(top) + 4;
+    int32_t* idx = static_cast<int32_t*>(lds);
+    return {idx, reinterpret_cast<float*>(idx + each), reinterpret_cast<float*>(idx + 2 * each)};
+}
+
+// An entry of the list on its way.
+struct Entry {
+    int32_t at;                         // -1: none
+    float   t, z;
+    __device__ __forceinline__ void name(const Distill& d, int64_t row, uint32_t j)
+    {
+        at = -1, t = -kInf, z = 0.0f;
+        if (j < d.top) {
+            at = d.idx[row * d.ld_idx + j];
+            t = d.t.at(row * d.ld_t + j);
+        } else if (j == room_of(d.top) && d.labels) {
+            at = d.labels[row];
+        }
+        if (at < 0 || at >= d.n) at = -1, t = -kInf;
+    }
+    template <typename T>
+    __device__ __forceinline__ void look(const T* row)
+    {
+        if (at >= 0) z = sizeof(T) == 2 ? mvx::widen(reinterpret_cast<const uint16_t*>(row)[at]) : reinterpret_cast<const float*>(row)[at];
+    }
+    __device__ __forceinline__ void keep(const List& l, uint32_t j) const { l.idx[j] = at, l.p[j] = t, l.z[j] = z; }
+};
+
+// What a row's terms come to, but for the sums over its logits.
 struct Terms {
-    float soft, hard;                   // weights of q and s in dz: 0 where the row has no such term
-    float largest, inv_a, inv_b;        // 1 / sum of exp((z - largest) / T) and of exp(z - largest)
-    float g;
+    float   soft;                       // P: 0 where there is no first term, else 1, or NaN
+    float   cross;                      // sum p (log p - (z - largest) / T)
+    float   share;                      // sum p, as rounding has it
+    float   label_z;
     int32_t label;                      // -1: none
 };
 
-__host__ __device__ constexpr size_t list_bytes(uint32_t top) { return ((size_t)top + 3) / 4 * 4 * 12; }
-__device__ __forceinline__ List list_at(void* lds, uint32_t top)
+// A wavefront makes p of the list: `first` is its lanes' first entries, the others are fetched here.  With the rows of
+// coordinates [from, to) only, logits elsewhere are not looked at.
+template <typename T>
+__device__ __forceinline__ Terms take_list(const Distill& d, const List& l, int64_t row, const T* z, Entry first, float largest, int64_t from,
+                                           int64_t to)
 {
-    const uint32_t room = (top + 3) / 4 * 4;
-    int32_t* idx = static_cast<int32_t*>(lds);
-    return {idx, reinterpret_cast<float*>(idx + room), reinterpret_cast<float*>(idx + 2 * room)};
-}
-
-// Fetches a row's list, and the logits it names where `logits` is a row.  Returns, in all threads, the teacher's largest logit.
-template <int LANES, typename T>
-__device__ __forceinline__ float fetch_list(const Distill& d, const List& l, int64_t row, bool live_row, const T* logits,
-                                            Across<LANES>& across)
-{
-    const uint32_t t = threadIdx.x % LANES, room = (d.top + 3) / 4 * 4;
-    float most = -kInf;
-    for (uint32_t j = t; j < room; j += LANES) {
-        int32_t at = -1;
-        float   v = -kInf, z = 0.0f;
-        if (live_row && j < d.top) {
-            at = d.idx[row * d.ld_idx + j];
-            if (at < 0 || at >= d.n) at = -1;
-            if (at >= 0) {
-                v = d.t.at(row * d.ld_t + j);
-                if (logits) z = sizeof(T) == 2 ? mvx::widen(reinterpret_cast<const uint16_t*>(logits)[at])
-                                               : reinterpret_cast<const float*>(logits)[at];
-            }
-        }
-        l.idx[j] = at, l.p[j] = v, l.z[j] = z;
-        most = fmaxf(most, v);
+    const uint32_t lane = threadIdx.x & 63u, all = room_of(d.top) + 1;
+    float most = first.t;
+    if (lane < all) first.keep(l, lane);
+    for (uint32_t j = lane + 64; j < all; j += 64) {
+        Entry e;
+        e.name(d, row, j);
+        if (e.at >= from && e.at < to) e.look(z);
+        e.keep(l, j);
+        most = fmaxf(most, e.t);
     }
-    return across.max(most);
-}
-// The sum of exp((t - most) / T): its log, and what the p made of it come to: 0 where there are none, else 1, or NaN.
-template <int LANES>
-__device__ __forceinline__ float total_p(const Distill& d, const List& l, float most, float& log_sum, Across<LANES>& across)
-{
-    const uint32_t t = threadIdx.x % LANES;
+    most = wave_max(most);
     float sum = 0.0f;
-    for (uint32_t j = t; j < d.top; j += LANES) {
+    for (uint32_t j = lane; j < d.top; j += 64) {
         const float v = l.p[j];
         if (v != -kInf) sum += expf((v - most) * d.inv_t);               // NaN among them, or +infinity: NaN
     }
-    sum = across.sum(sum);
-    log_sum = logf(sum);
-    return sum == 0.0f ? 0.0f : sum * 0.0f + 1.0f;
-}
-
-// sum p (log p - log q) over the list; p replaces the teacher's logits in LDS.
-template <int LANES>
-__device__ __forceinline__ float soft_loss(const Distill& d, const List& l, float most, float log_sum, float largest, float log_a,
-                                           Across<LANES>& across)
-{
-    const uint32_t t = threadIdx.x % LANES;
-    float sum = 0.0f;
-    for (uint32_t j = t; j < d.top; j += LANES) {
+    sum = wave_sum(sum);
+    const float log_sum = logf(sum);
+    Terms w = {sum == 0.0f ? 0.0f : sum * 0.0f + 1.0f, 0.0f, 0.0f, 0.0f, -1};
+    for (uint32_t j = lane; j < all - 1; j += 64) {
         const float v = l.p[j];
         float p = 0.0f;
         if (v != -kInf) {
             const float log_p = (v - most) * d.inv_t - log_sum;
             p = expf(log_p);
-            if (p != 0.0f) sum += p * (log_p - ((l.z[j] - largest) * d.inv_t - log_a));
+            if (p != 0.0f) w.cross += p * (log_p - (l.z[j] - largest) * d.inv_t), w.share += p;
         }
         l.p[j] = p;
     }
-    return across.sum(sum);
+    w.cross = wave_sum(w.cross), w.share = wave_sum(w.share);
+    __builtin_amdgcn_wave_barrier();
+    w.label = l.idx[all - 1], w.label_z = l.z[all - 1];                  // another lane's: LDS is in order within a wavefront
+    return w;
+}
+__device__ __forceinline__ float loss_of(const Distill& d, const Terms& w, float largest, float a, float b)
+{
+    float loss = 0.0f;
+    if (w.soft != 0.0f) loss = d.soft_loss * (w.cross + logf(a) * w.share) * w.soft;
+    if (w.label >= 0) loss += d.hard * (logf(b) - (w.label_z - largest));
+    return loss;
 }
 
-// dz where the list or the label names a coordinate of [first, last).
-template <int LANES>
-__device__ __forceinline__ void patch(const Distill& d, const List& l, const Terms& w, int64_t row, int64_t first, int64_t last, float label_z)
+// dz away from the list: a e_a + b e_b.
+struct Weights {
+    float a, b, largest, g;
+    bool  any;                          // is there a term at all
+    template <int TERMS>
+    __device__ __forceinline__ float of(const Pair<TERMS>& e) const
+    {
+        return TERMS == kOne ? a * e.a : TERMS == kTwo ? __builtin_fmaf(b, e.b, a * e.a) : __builtin_fmaf(b, e.a, a) * e.a;
+    }
+};
+template <int TERMS>
+__device__ __forceinline__ Weights weights_of(const Distill& d, float soft, int32_t label, float g, float largest, float a, float b)
+{
+    const float first = soft != 0.0f ? g * (soft * d.soft_grad) / a : 0.0f, second = label >= 0 ? g * d.hard / b : 0.0f;
+    return {TERMS == kOne ? first + second : first, second, largest, g, soft != 0.0f || label >= 0};
+}
+template <typename T, int TERMS>
+__device__ __forceinline__ void plain_grad(const Chunk<T>& c, const Weights& w, float scale, float (&y)[kChunk<T>])
+{
+#pragma unroll
+    for (int i = 0; i < kChunk<T>; ++i) y[i] = w.any ? w.of(Pair<TERMS>(c.at(i) - w.largest, scale)) : 0.0f;
+}
+
+// dz at what the list and the label name among the coordinates from `from` to `to` that this wavefront wrote before: chunks go
+// round THREADS threads.
+template <typename T, int THREADS, int TERMS>
+__device__ __forceinline__ void patch(const Distill& d, const List& l, const Weights& w, int64_t row, int32_t label, int64_t from, int64_t to)
 {
     typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-    const uint32_t t = threadIdx.x % LANES, room = w.soft != 0.0f ? (d.top + 3) / 4 * 4 : 0u;
-    for (uint32_t j = t; j < room + 1; j += LANES) {
-        const int32_t at = j < room ? l.idx[j] : w.label;                // behind the list: the label
-        if (at < first || at >= last) continue;                          // none is -1
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x % THREADS / 64, room = room_of(d.top);
+    if (!w.any) return;
+    for (uint32_t j = lane; j < room + 1; j += 64) {
+        const int32_t at = l.idx[j];
+        if (at < from || at >= to) continue;                             // none is -1
+        if ((uint32_t)(at - (int32_t)from) / (64 * kChunk<T>) % (THREADS / 64) != wave) continue;
         float p = 0.0f;
         bool  named = false;                                             // by an entry before
         for (uint32_t i = 0; i < room; i += 4) {
@@ -140,241 +248,308 @@ __device__ __forceinline__ void patch(const Distill& d, const List& l, const Ter
                 }
         }
         if (named) continue;
-        const float z = (j < room ? l.z[j] : label_z) - w.largest;
-        float v = 0.0f;
-        if (w.soft != 0.0f) v = w.soft * (power(z * d.inv_t * kLog2e) * w.inv_a - p);
-        if (w.hard != 0.0f) v += w.hard * (power(z * kLog2e) * w.inv_b - (at == w.label ? 1.0f : 0.0f));
-        d.dz.put(row * d.ld_dz + at, w.g * v);
+        const float off = d.soft_grad * p + (at == label ? d.hard : 0.0f);
+        d.dz.put(row * d.ld_dz + at, w.of(Pair<TERMS>(l.z[j] - w.largest, d.scale)) - w.g * off);
     }
 }
 
-// dz of a chunk before its patches.
-template <int V>
-__device__ __forceinline__ void plain_grad(const Terms& w, float scale, bool any, const float (&z)[V], float (&to)[V])
-{
-    const float a = w.g * w.soft * w.inv_a, b = w.g * w.hard * w.inv_b;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float x = z[i] - w.largest;
-        float v = 0.0f;
-        if (w.soft != 0.0f) v = a * power(x * scale);
-        if (w.hard != 0.0f) v += b * power(x * kLog2e);
-        to[i] = any ? v : 0.0f;
-    }
-}
+// ---- a row in registers ------------------------------------------------------------------------------------------------
 
-// A row in registers: LANES threads, C chunks each.
-template <typename T, int LANES, int C>
-__global__ __launch_bounds__(kThreadsOf<LANES>) void mv_distill_kernel(Distill d)
+// LANES threads with up to C whole chunks each, and one that the row may end in.  Chunks that a row does not have are
+// -infinity, which costs less than to ask for each whether it is there.
+template <typename T, int LANES, int C, int TERMS>
+__global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distill d)
 {
-    constexpr int V = kChunk<T>, kRows = kThreadsOf<LANES> / LANES;
-    __shared__ float sums[kRows][2][2][LANES / 64];
+    constexpr int V = kChunk<T>, kRows = kThreadsOf<LANES> / LANES, kWaves = LANES / 64;
+    __shared__ float tops[kWaves], sums[2][kWaves];
+    __shared__ Terms shared;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    const uint32_t t = threadIdx.x % LANES, mine = threadIdx.x / LANES;
-    Across<LANES> across(sums[mine]);
+    const uint32_t t = threadIdx.x % LANES, mine = __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(t / 64);
     const List list = list_at(lds + mine * list_bytes(d.top), d.top);
-    const float scale = d.inv_t * kLog2e;
-    for (int64_t first = (int64_t)blockIdx.x * kRows; first < d.rows; first += (int64_t)gridDim.x * kRows) {
-        const int64_t row = first + mine;
-        const bool live_row = row < d.rows;
-        const T* z = static_cast<const T*>(d.z) + row * d.ld_z;
-        Chunk<T> held[C];
+    const int n = (int)d.n, full = n / (LANES * V), rest = n - full * (LANES * V) - (int)t * V;
+    Chunk<T> held[C], tail;
+    auto row_at = [&](int64_t row) { return static_cast<const T*>(d.z) + row * d.ld_z; };
+    // in one scalar comparison each time, not in sixteen masks that are kept
+    auto there = [&](int c) {
+        int f = full;
+        asm("" : "+s"(f));
+        return c < f;
+    };
+    auto fetch = [&](const T* z, int c) { held[c].load(z + c * (LANES * V) + t * V, V); };
+    auto fetch_tail = [&](const T* z) { tail.load_low(z + full * (LANES * V) + t * V, rest); };
+    int64_t row = (int64_t)blockIdx.x * kRows + mine;
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    if (row < d.rows) {
+        const T* z = row_at(row);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int64_t col = (int64_t)(c * LANES + t) * V;
-            held[c].load(z + col, live_row ? d.n - col : 0);
+            held[c].clear();
+            if (there(c)) fetch(z, c);
         }
-        const float most = d.top ? fetch_list<LANES>(d, list, row, live_row, z, across) : -kInf;
-        int32_t label = live_row && d.labels ? d.labels[row] : -1;
-        if (label >= d.n) label = -1;
-        const float label_z = label >= 0 ? Any{d.z, sizeof(T) == 2}.at(row * d.ld_z + label) : 0.0f;
-        float largest = -kInf;
+        fetch_tail(z);
+    }
+    for (; row < d.rows; row += step) {
+        Entry entry;
+        if (wave == 0) entry.name(d, row, t);
+        Largest<T> most;
+        most.look(tail);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int64_t live = live_row ? d.n - (int64_t)(c * LANES + t) * V : 0;
-#pragma unroll
-            for (int i = 0; i < V; ++i) largest = fmaxf(largest, i < live ? held[c].at(i) : -kInf);
-        }
-        largest = across.max(largest);
-        float a = 0.0f, b = 0.0f;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int64_t live = live_row ? d.n - (int64_t)(c * LANES + t) * V : 0;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float x = i < live ? held[c].at(i) - largest : -kInf;
-                if (d.top) a += power(x * scale);
-                if (d.labels) b += power(x * kLog2e);
-            }
-        }
-        __builtin_amdgcn_s_waitcnt(kNoLoads);                       // dz may be z: all that is read of the row is here
-        across.sum2(a, b);
-        if (live_row && t == 0 && d.stats) {
-            d.stats[3 * row] = largest;
-            d.stats[3 * row + 1] = a;
-            d.stats[3 * row + 2] = b;
-        }
-        float log_sum = 0.0f, loss = 0.0f;
-        const float total = d.top ? total_p<LANES>(d, list, most, log_sum, across) : 0.0f;
-        const bool soft = total != 0.0f;
-        if (d.top) {
-            const float sum = soft_loss<LANES>(d, list, most, log_sum, largest, logf(a), across);
-            if (soft) loss = d.soft_loss * sum;
-        }
-        if (label >= 0) loss += d.hard * (logf(b) - (label_z - largest));
-        if (live_row && t == 0 && d.loss) d.loss[row] = loss;
-        if (d.dz.p) {                                                    // uniform
-            const Terms w = {total * d.soft_grad, label >= 0 ? d.hard : 0.0f, largest, 1.0f / a, 1.0f / b,
-                             d.grad && live_row ? d.grad[row] : 1.0f, label};
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const int64_t col = (int64_t)(c * LANES + t) * V;
-                float x[V], y[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) x[i] = held[c].at(i);
-                plain_grad(w, scale, soft || label >= 0, x, y);
-                if (live_row) d.dz.store(row * d.ld_dz + col, d.n - col, y);
-            }
-            __builtin_amdgcn_s_waitcnt(0);                               // all of a row is written before its patches
+        for (int c = 0; c < C; ++c)
+            most.look(held[c]);
+        float largest = wave_max(most.value());
+        if (wave == 0) entry.look(row_at(row));
+        if constexpr (kWaves > 1) {
+            if ((t & 63u) == 0) tops[wave] = largest;
             __syncthreads();
-            if (live_row) patch<LANES>(d, list, w, row, 0, d.n, label_z);
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) largest = larger(tops[w], largest);
         }
-        __syncthreads();                                                 // the list is read before the next row's
+        float a = 0.0f, b = 0.0f;
+        add_up<T, TERMS>(tail, largest, d.scale, a, b);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            add_up<T, TERMS>(held[c], largest, d.scale, a, b);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        a = wave_sum(a);
+        if (TERMS != kOne) b = wave_sum(b);
+        Terms w;
+        if (wave == 0) w = take_list(d, list, row, row_at(row), entry, largest, 0, d.n);
+        __builtin_amdgcn_s_waitcnt(kNoLoads);                            // dz may be z: all that is read of the row is here
+        if constexpr (kWaves > 1) {
+            if ((t & 63u) == 0) sums[0][wave] = a, sums[1][wave] = b;
+            if (t == 0) shared = w;
+            __syncthreads();
+            a = b = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) a += sums[0][i], b += sums[1][i];
+            w = shared;
+        }
+        if (TERMS == kOne) b = a;
+        if (t == 0) {
+            if (d.loss) d.loss[row] = loss_of(d, w, largest, a, b);
+            if (d.stats) {
+                d.stats[3 * row] = largest;
+                d.stats[3 * row + 1] = d.top ? a : 0.0f;
+                d.stats[3 * row + 2] = d.labels ? b : 0.0f;
+            }
+        }
+        const Weights weights = weights_of<TERMS>(d, w.soft, w.label, d.grad ? d.grad[row] : 1.0f, largest, a, b);
+        const bool more = row + step < d.rows;
+        const T* next = row_at(row + step);
+        if (d.dz.p) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (there(c)) {
+                    float y[V];
+                    held[c].forget();                                    // what was made of it for the sums is not kept
+                    plain_grad<T, TERMS>(held[c], weights, d.scale, y);
+                    d.dz.store(row * d.ld_dz + c * (LANES * V) + t * V, V, y);
+                    if (more) fetch(next, c);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            float y[V];
+            plain_grad<T, TERMS>(tail, weights, d.scale, y);
+            d.dz.store(row * d.ld_dz + full * (LANES * V) + t * V, rest, y);
+            if (more) fetch_tail(next);
+            patch<T, LANES, TERMS>(d, list, weights, row, w.label, 0, d.n);
+        } else if (more) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (there(c)) fetch(next, c);
+            fetch_tail(next);
+        }
     }
 }
 
-// ---- long rows, in ranges ----------------------------------------------------------------------------------------------
+// ---- rows that stream by ---------------------------------------------------------------------------------------------
 
-constexpr int kRangeThreads = 512;
-
-// Largest and sums of a range: each thread's as it goes, joined at the end.
+constexpr int kStreamThreads = 512;
 template <typename T>
-__global__ __launch_bounds__(kRangeThreads) void mv_distill_range_kernel(Distill d)
+constexpr int kAhead = sizeof(T) == 2 ? 2 : 4;                           // chunks of a turn
+
+// A thread's largest and sums of [first, last) of a row: each turn's largest first, what was added up before scaled down to it.
+template <typename T, int TERMS>
+__device__ __forceinline__ void stream(const T* z, int64_t first, int64_t last, float scale, float& largest, float& a, float& b)
 {
-    constexpr int V = kChunk<T>;
-    __shared__ float sums[2][2][kRangeThreads / 64];
-    Across<kRangeThreads> across(sums);
-    const float scale = d.inv_t * kLog2e;
+    constexpr int V = kChunk<T>, G = kAhead<T>;
+    constexpr int64_t kTurn = (int64_t)kStreamThreads * V * G;
+    largest = -kInf, a = b = 0.0f;
+    for (int64_t at = first; at < last; at += kTurn) {
+        Chunk<T> c[G];
+        const T* p = z + at + threadIdx.x * V;
+        if (at + kTurn <= last) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) c[g].load(p + g * (kStreamThreads * V), V);
+        } else {
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const int64_t live = last - at - threadIdx.x * V - g * (kStreamThreads * V);
+                c[g].load_low(p + g * (kStreamThreads * V), live < 0 ? 0 : live < V ? (int)live : V);
+            }
+        }
+        Largest<T> most;
+#pragma unroll
+        for (int g = 0; g < G; ++g) most.look(c[g]);
+        const float top = most.value();
+        if (top > largest) {                                             // from -infinity: of nothing
+            const float down = largest - top;
+            a *= power(down * scale);
+            if (TERMS != kOne) b *= power(down * kLog2e);
+            largest = top;
+        }
+        const float base = largest == -kInf ? 0.0f : largest;
+#pragma unroll
+        for (int g = 0; g < G; ++g) add_up<T, TERMS>(c[g], base, scale, a, b);
+    }
+}
+// Joined over the workgroup; sums of nothing but -infinity are 0.
+template <int TERMS>
+__device__ __forceinline__ void join(Across<kStreamThreads>& across, float scale, float& largest, float& a, float& b)
+{
+    const float top = across.max(largest), down = largest - (top == -kInf ? 0.0f : top);
+    a *= power(down * scale);
+    if (TERMS != kOne) b *= power(down * kLog2e);
+    across.sum2(a, b);
+    if (TERMS == kOne) b = a;
+    largest = top;
+}
+
+// The loss of whole rows, a workgroup each.
+template <typename T, int TERMS>
+__global__ __launch_bounds__(kStreamThreads) void mv_distill_loss_kernel(Distill d)
+{
+    __shared__ float sums[2][2][kStreamThreads / 64];
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    Across<kStreamThreads> across(sums);
+    const List list = list_at(lds, d.top);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    for (int64_t row = blockIdx.x; row < d.rows; row += gridDim.x) {
+        const T* z = static_cast<const T*>(d.z) + row * d.ld_z;
+        Entry entry;
+        if (wave == 0 && d.loss) {
+            entry.name(d, row, threadIdx.x);
+            entry.look(z);
+        }
+        float largest, a, b;
+        stream<T, TERMS>(z, 0, d.n, d.scale, largest, a, b);
+        join<TERMS>(across, d.scale, largest, a, b);
+        // a row of nothing but -infinity has no sums
+        if (largest == -kInf) a = b = __builtin_nanf("");
+        if (wave == 0) {
+            if (d.loss) {
+                const Terms w = take_list(d, list, row, z, entry, largest, 0, d.n);
+                if (threadIdx.x == 0) d.loss[row] = loss_of(d, w, largest, a, b);
+            }
+            if (threadIdx.x == 0 && d.stats) {
+                d.stats[3 * row] = largest;
+                d.stats[3 * row + 1] = d.top ? a : 0.0f;
+                d.stats[3 * row + 2] = d.labels ? b : 0.0f;
+            }
+        }
+    }
+}
+
+// Largest and sums of a range.
+template <typename T, int TERMS>
+__global__ __launch_bounds__(kStreamThreads) void mv_distill_range_kernel(Distill d)
+{
+    __shared__ float sums[2][2][kStreamThreads / 64];
+    Across<kStreamThreads> across(sums);
     const int64_t all = d.rows * d.ranges;
     for (int64_t at = blockIdx.x; at < all; at += gridDim.x) {
         const int64_t row = at / d.ranges, first = at % d.ranges * d.range, last = first + d.range < d.n ? first + d.range : d.n;
-        const T* z = static_cast<const T*>(d.z) + row * d.ld_z;
-        float largest = -kInf, a = 0.0f, b = 0.0f;
-        for (int64_t col = first + (int64_t)threadIdx.x * V; col < last; col += kRangeThreads * V) {
-            Chunk<T> c;
-            c.load(z + col, last - col);
-            const int64_t live = last - col;
-            float x[V], top = largest;
-#pragma unroll
-            for (int i = 0; i < V; ++i) top = fmaxf(top, x[i] = i < live ? c.at(i) : -kInf);
-            const float base = top == -kInf ? 0.0f : top, old = largest - base;          // -infinity: nothing yet
-            if (top > largest) a *= power(old * scale), b *= power(old * kLog2e);
-            largest = top;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                if (d.top) a += power((x[i] - base) * scale);
-                if (d.labels) b += power((x[i] - base) * kLog2e);
-            }
-        }
-        const float top = across.max(largest), old = largest - (top == -kInf ? 0.0f : top);
-        a *= power(old * scale), b *= power(old * kLog2e);
-        across.sum2(a, b);
+        float largest, a, b;
+        stream<T, TERMS>(static_cast<const T*>(d.z) + row * d.ld_z, first, last, d.scale, largest, a, b);
+        join<TERMS>(across, d.scale, largest, a, b);
         if (threadIdx.x == 0) {
             float* to = d.parts + 4 * at;
-            to[0] = top, to[1] = a, to[2] = b;
+            to[0] = largest, to[1] = a, to[2] = b;
         }
-        __syncthreads();
     }
 }
 
-// A row's ranges joined, and its loss.
-constexpr int kJoinThreads = 256;
-template <typename T>
-__global__ __launch_bounds__(kJoinThreads) void mv_distill_join_kernel(Distill d)
+// A row's ranges joined, and its loss: a wavefront each.
+template <typename T, int TERMS>
+__global__ __launch_bounds__(64) void mv_distill_join_kernel(Distill d)
 {
-    __shared__ float sums[2][2][kJoinThreads / 64];
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    Across<kJoinThreads> across(sums);
     const List list = list_at(lds, d.top);
-    const float scale = d.inv_t * kLog2e;
     for (int64_t row = blockIdx.x; row < d.rows; row += gridDim.x) {
+        const T* z = static_cast<const T*>(d.z) + row * d.ld_z;
+        Entry entry;
+        if (d.loss) {
+            entry.name(d, row, threadIdx.x);
+            entry.look(z);
+        }
         const float* part = d.parts + 4 * row * d.ranges;
         float largest = -kInf, a = 0.0f, b = 0.0f;
-        for (uint32_t r = threadIdx.x; r < d.ranges; r += kJoinThreads) largest = fmaxf(largest, part[4 * r]);
-        largest = across.max(largest);
-        for (uint32_t r = threadIdx.x; r < d.ranges; r += kJoinThreads) {
-            const float old = part[4 * r] - largest;
-            a += part[4 * r + 1] * power(old * scale);
-            b += part[4 * r + 2] * power(old * kLog2e);
+        for (uint32_t r = threadIdx.x; r < d.ranges; r += 64) largest = fmaxf(largest, part[4 * r]);
+        largest = wave_max(largest);
+        for (uint32_t r = threadIdx.x; r < d.ranges; r += 64) {
+            const float down = part[4 * r] - largest;                    // of nothing but -infinity: NaN
+            a += part[4 * r + 1] * power(down * d.scale);
+            b += part[4 * r + 2] * power(down * (TERMS == kOne ? d.scale : kLog2e));
         }
-        across.sum2(a, b);
-        if (threadIdx.x == 0) {
-            float* to = d.stats + 3 * row;
-            to[0] = largest, to[1] = a, to[2] = b;
+        a = wave_sum(a), b = wave_sum(b);
+        if (d.loss) {
+            const Terms w = take_list(d, list, row, z, entry, largest, 0, d.n);
+            if (threadIdx.x == 0) d.loss[row] = loss_of(d, w, largest, a, b);
         }
-        if (!d.loss) continue;                                           // uniform
-        const T* z = static_cast<const T*>(d.z) + row * d.ld_z;
-        float log_sum = 0.0f, loss = 0.0f;
-        if (d.top) {
-            const float most = fetch_list<kJoinThreads>(d, list, row, true, z, across);
-            const bool soft = total_p<kJoinThreads>(d, list, most, log_sum, across) != 0.0f;
-            const float sum = soft_loss<kJoinThreads>(d, list, most, log_sum, largest, logf(a), across);
-            if (soft) loss = d.soft_loss * sum;
+        if (threadIdx.x == 0 && d.stats) {
+            d.stats[3 * row] = largest;
+            d.stats[3 * row + 1] = d.top ? a : 0.0f;
+            d.stats[3 * row + 2] = d.labels ? b : 0.0f;
         }
-        const int32_t label = d.labels ? d.labels[row] : -1;
-        if (label >= 0 && label < d.n) loss += d.hard * (logf(b) - (Any{d.z, sizeof(T) == 2}.at(row * d.ld_z + label) - largest));
-        if (threadIdx.x == 0) d.loss[row] = loss;
-        __syncthreads();
     }
 }
 
 // dz of a range, from the row's stats.
-template <typename T>
-__global__ __launch_bounds__(kRangeThreads) void mv_distill_grad_kernel(Distill d)
+template <typename T, int TERMS>
+__global__ __launch_bounds__(kStreamThreads) void mv_distill_grad_kernel(Distill d)
 {
-    constexpr int V = kChunk<T>;
-    __shared__ float sums[2][2][kRangeThreads / 64];
+    constexpr int V = kChunk<T>, G = kAhead<T>;
+    constexpr int64_t kTurn = (int64_t)kStreamThreads * V * G;
+    __shared__ Terms shared;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    Across<kRangeThreads> across(sums);
     const List list = list_at(lds, d.top);
-    const float scale = d.inv_t * kLog2e;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int64_t all = d.rows * d.ranges;
     for (int64_t at = blockIdx.x; at < all; at += gridDim.x) {
         const int64_t row = at / d.ranges, first = at % d.ranges * d.range, last = first + d.range < d.n ? first + d.range : d.n;
         const T* z = static_cast<const T*>(d.z) + row * d.ld_z;
-        float total = 0.0f;
-        if (d.top) {
-            // logits are asked for only where this range names them: others may have been written over
-            const uint32_t room = (d.top + 3) / 4 * 4;
-            const float most = fetch_list<kRangeThreads, T>(d, list, row, true, nullptr, across);
-            for (uint32_t j = threadIdx.x; j < room; j += kRangeThreads)
-                if (list.idx[j] >= first && list.idx[j] < last) list.z[j] = Any{d.z, sizeof(T) == 2}.at(row * d.ld_z + list.idx[j]);
-            float log_sum;
-            total = total_p<kRangeThreads>(d, list, most, log_sum, across);
-            for (uint32_t j = threadIdx.x; j < d.top; j += kRangeThreads)
-                list.p[j] = list.p[j] == -kInf ? 0.0f : expf((list.p[j] - most) * d.inv_t - log_sum);
-        }
-        int32_t label = d.labels ? d.labels[row] : -1;
-        if (label >= d.n) label = -1;
-        const float label_z = label >= first && label < last ? Any{d.z, sizeof(T) == 2}.at(row * d.ld_z + label) : 0.0f;
         const float* had = d.had + 3 * row;
-        const Terms w = {total * d.soft_grad, label >= 0 ? d.hard : 0.0f, had[0], 1.0f / had[1], 1.0f / had[2],
-                         d.grad ? d.grad[row] : 1.0f, label};
-        __builtin_amdgcn_s_waitcnt(kNoLoads);                            // dz may be z: the list's and the label's are here
-        __syncthreads();
-        for (int64_t col = first + (int64_t)threadIdx.x * V; col < last; col += kRangeThreads * V) {
-            Chunk<T> c;
-            c.load(z + col, last - col);
-            float x[V], y[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) x[i] = c.at(i);
-            plain_grad(w, scale, total != 0.0f || label >= 0, x, y);
-            d.dz.store(row * d.ld_dz + col, last - col, y);
+        const float largest = had[0];
+        if (wave == 0) {
+            Entry entry;
+            entry.name(d, row, threadIdx.x);
+            if (entry.at >= first && entry.at < last) entry.look(z);     // logits elsewhere may have been written over
+            const Terms w = take_list(d, list, row, z, entry, largest, first, last);
+            if (threadIdx.x == 0) shared = w;
+            __builtin_amdgcn_s_waitcnt(kNoLoads);                        // dz may be z: the list's logits are here
         }
-        __builtin_amdgcn_s_waitcnt(0);                                   // all of the range is written before its patches
         __syncthreads();
-        patch<kRangeThreads>(d, list, w, row, first, last, label_z);
-        __syncthreads();
+        const Weights w = weights_of<TERMS>(d, shared.soft, shared.label, d.grad ? d.grad[row] : 1.0f, largest, had[1], had[2]);
+        const int32_t label = shared.label;
+        for (int64_t col = first; col < last; col += kTurn) {
+            Chunk<T> c[G];
+            int live[G];
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const int64_t left = last - col - threadIdx.x * V - g * (kStreamThreads * V);
+                live[g] = left < 0 ? 0 : left < V ? (int)left : V;
+                c[g].load(z + col + threadIdx.x * V + g * (kStreamThreads * V), live[g]);
+            }
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                float y[V];
+                plain_grad<T, TERMS>(c[g], w, d.scale, y);
+                d.dz.store(row * d.ld_dz + col + threadIdx.x * V + g * (kStreamThreads * V), live[g], y);
+            }
+        }
+        patch<T, kStreamThreads, TERMS>(d, list, w, row, label, first, last);
+        __syncthreads();                                                 // the list and the terms are read before the next ones
     }
 }
 
@@ -384,14 +559,15 @@ struct Lanes {
 };
 static Lanes lanes_of(int64_t n, int32_t dtype, int64_t top)
 {
-    const int64_t wide = dtype == MV_BF16 ? 8 : 4, chunks = (n + wide - 1) / wide;
-    for (int i = top > 1024 ? 1 : 0; i < 3; ++i)                         // four rows' lists in one workgroup's LDS: 48 KB
-        for (int c = i ? 4 : 1; c <= (i == 2 ? 16 : i ? 8 : 4); c *= i ? 2 : 4)
-            if (chunks <= ((int64_t)64 << (2 * i)) * c) return {64 << (2 * i), c};
+    const int64_t wide = dtype == MV_BF16 ? 8 : 4, chunks = n / wide;
+    if (chunks < 64 * 4 && top <= 1024) return {64, 4};                  // four rows' lists in one workgroup's LDS: 48 KB
+    for (int lanes : {256, 512, 1024})
+        for (int c : {12, 16})
+            if (chunks < (int64_t)lanes * (c + 1)) return {lanes, c};    // the tail is one more
     return {0, 0};
 }
 
-// Ranges of long rows: of 16,384 values or more, as few as give the card a thousand workgroups.
+// Ranges of rows: of 16,384 values or more, as few as give the card a thousand workgroups.
 constexpr int64_t kRangeLeast = 16384, kRangeGroups = 1024;
 struct Ranges {
     uint32_t count;
@@ -406,33 +582,40 @@ static Ranges ranges_of(int64_t rows, int64_t n)
 }
 inline uint32_t grid_of(int64_t groups, int64_t most) { return (uint32_t)(groups < most ? groups : most); }
 
-template <typename T, int LANES, int C>
+template <typename T, int LANES, int C, int TERMS>
 static void held(const Distill& d, hipStream_t st)
 {
     constexpr int kRows = kThreadsOf<LANES> / LANES;
-    hipLaunchKernelGGL((mv_distill_kernel<T, LANES, C>), dim3(grid_of((d.rows + kRows - 1) / kRows, 1 << 20)), dim3(kThreadsOf<LANES>),
-                       kRows * list_bytes(d.top), st, d);
+    // as many as run at once, sixteen wavefronts to a unit
+    hipLaunchKernelGGL((mv_distill_kernel<T, LANES, C, TERMS>), dim3(grid_of((d.rows + kRows - 1) / kRows, 256 * 1024 / kThreadsOf<LANES>)),
+                       dim3(kThreadsOf<LANES>), kRows * list_bytes(d.top), st, d);
 }
-template <typename T>
+template <typename T, int TERMS>
 static void grad(Distill d, hipStream_t st)
 {
     const Ranges r = ranges_of(d.rows, d.n);
     d.ranges = r.count, d.range = r.length;
-    hipLaunchKernelGGL(mv_distill_grad_kernel<T>, dim3(grid_of(d.rows * r.count, 1 << 20)), dim3(kRangeThreads), list_bytes(d.top), st, d);
+    hipLaunchKernelGGL((mv_distill_grad_kernel<T, TERMS>), dim3(grid_of(d.rows * r.count, 1 << 20)), dim3(kStreamThreads), list_bytes(d.top),
+                       st, d);
 }
-template <typename T>
+template <typename T, int TERMS>
 static void loss(Distill d, const Lanes& l, hipStream_t st)
 {
-    if (l.lanes == 64) return l.chunks == 1 ? held<T, 64, 1>(d, st) : held<T, 64, 4>(d, st);
-    if (l.lanes == 256) return l.chunks == 4 ? held<T, 256, 4>(d, st) : held<T, 256, 8>(d, st);
-    if (l.lanes == 1024) return l.chunks == 4 ? held<T, 1024, 4>(d, st) : l.chunks == 8 ? held<T, 1024, 8>(d, st) : held<T, 1024, 16>(d, st);
+    if (l.lanes == 64) return held<T, 64, 4, TERMS>(d, st);
+    if (d.dz.p && l.lanes == 256) return l.chunks == 12 ? held<T, 256, 12, TERMS>(d, st) : held<T, 256, 16, TERMS>(d, st);
+    if (d.dz.p && l.lanes == 512) return l.chunks == 12 ? held<T, 512, 12, TERMS>(d, st) : held<T, 512, 16, TERMS>(d, st);
+    if (d.dz.p && l.lanes == 1024) return l.chunks == 12 ? held<T, 1024, 12, TERMS>(d, st) : held<T, 1024, 16, TERMS>(d, st);
     const Ranges r = ranges_of(d.rows, d.n);
     d.ranges = r.count, d.range = r.length;
-    hipLaunchKernelGGL(mv_distill_range_kernel<T>, dim3(grid_of(d.rows * r.count, 1 << 20)), dim3(kRangeThreads), 0, st, d);
-    hipLaunchKernelGGL(mv_distill_join_kernel<T>, dim3(grid_of(d.rows, 1 << 20)), dim3(kJoinThreads), list_bytes(d.top), st, d);
+    if (r.count == 1 || !d.parts) {
+        hipLaunchKernelGGL((mv_distill_loss_kernel<T, TERMS>), dim3(grid_of(d.rows, 1 << 20)), dim3(kStreamThreads), list_bytes(d.top), st, d);
+    } else {
+        hipLaunchKernelGGL((mv_distill_range_kernel<T, TERMS>), dim3(grid_of(d.rows * r.count, 1 << 20)), dim3(kStreamThreads), 0, st, d);
+        hipLaunchKernelGGL((mv_distill_join_kernel<T, TERMS>), dim3(grid_of(d.rows, 1 << 20)), dim3(64), list_bytes(d.top), st, d);
+    }
     if (d.dz.p) {
         d.had = d.stats;
-        grad<T>(d, st);
+        grad<T, TERMS>(d, st);
     }
 }
 
@@ -456,9 +639,19 @@ static bool fill(Distill& d, const void* logits, int32_t dtype, int64_t ld_z, in
     d.idx = idx, d.ld_idx = ld_idx, d.t = {t, t_dtype == MV_BF16}, d.ld_t = ld_t, d.top = listed ? (uint32_t)top : 0u;
     d.labels = hard != 0.0f ? labels : nullptr;
     d.inv_t = 1.0f / temperature;
+    d.scale = d.top ? d.inv_t * kLog2e : kLog2e;                         // without a first term: of the second
     d.soft_grad = soft * temperature, d.soft_loss = soft * temperature * temperature, d.hard = hard;
     d.grad = g, d.dz = {dz, dz_dtype == MV_BF16}, d.ld_dz = ld_dz;
     return true;
+}
+
+template <typename F>
+static mv_status with_terms(const Distill& d, float temperature, F launch)
+{
+    if (!d.top || !d.labels || temperature == 1.0f) launch(std::integral_constant<int, kOne>{});
+    else if (temperature == 2.0f) launch(std::integral_constant<int, kSquare>{});
+    else launch(std::integral_constant<int, kTwo>{});
+    return launched();
 }
 
 }  // namespace mvr
@@ -468,8 +661,9 @@ extern "C" {
 size_t mv_distill_scratch_bytes(int64_t rows, int64_t n)
 {
     using namespace mvr;
-    // fp32 rows are the first to be too long
-    return size_valid(rows) && size_valid(n) && !lanes_of(n, MV_F32, 0).lanes ? parts_bytes(rows, n) + stats_bytes(rows) : 0;
+    if (!size_valid(rows) || !size_valid(n)) return 0;
+    // what is cut into ranges, and what no type's rows of are held
+    return ranges_of(rows, n).count > 1 || !lanes_of(n, MV_F32, 0).lanes ? parts_bytes(rows, n) + stats_bytes(rows) : 0;
 }
 
 mv_status mv_distill_loss(const void* logits, int32_t dtype, int64_t ld_z, int64_t rows, int64_t n, const int32_t* idx, int64_t ld_idx,
@@ -486,14 +680,15 @@ mv_status mv_distill_loss(const void* logits, int32_t dtype, int64_t ld_z, int64
     if (need && (!scratch || scratch_bytes < need || (reinterpret_cast<uintptr_t>(scratch) & 15))) return MV_ERR_INVALID_ARG;
     d.loss = loss, d.stats = stats;
     const Lanes l = lanes_of(n, dtype, d.top);
-    if (!l.lanes) {
+    if (need) {
         d.parts = static_cast<float*>(scratch);
-        if (!stats) d.stats = reinterpret_cast<float*>(static_cast<char*>(scratch) + parts_bytes(rows, n));
+        if (!stats && !l.lanes) d.stats = reinterpret_cast<float*>(static_cast<char*>(scratch) + parts_bytes(rows, n));
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dtype == MV_BF16) mvr::loss<uint16_t>(d, l, st);
-    else mvr::loss<float>(d, l, st);
-    return launched();
+    return with_terms(d, temperature, [&](auto terms) {
+        if (dtype == MV_BF16) mvr::loss<uint16_t, decltype(terms)::value>(d, l, st);
+        else mvr::loss<float, decltype(terms)::value>(d, l, st);
+    });
 }
 
 mv_status mv_distill_grad(const void* logits, int32_t dtype, int64_t ld_z, int64_t rows, int64_t n, const int32_t* idx, int64_t ld_idx,
@@ -507,9 +702,10 @@ mv_status mv_distill_grad(const void* logits, int32_t dtype, int64_t ld_z, int64
         return MV_ERR_INVALID_ARG;
     d.had = stats;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dtype == MV_BF16) mvr::grad<uint16_t>(d, st);
-    else mvr::grad<float>(d, st);
-    return launched();
+    return with_terms(d, temperature, [&](auto terms) {
+        if (dtype == MV_BF16) mvr::grad<uint16_t, decltype(terms)::value>(d, st);
+        else mvr::grad<float, decltype(terms)::value>(d, st);
+    });
 }
 
 }  // extern "C"

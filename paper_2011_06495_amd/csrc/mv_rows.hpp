@@ -26,12 +26,33 @@ struct Chunk;
 template <>
 struct Chunk<float> {
     float x[4];
+    // what is not there: -infinity
+    __device__ __forceinline__ void clear() { x[0] = x[1] = x[2] = x[3] = -kInf; }
+    // To the compiler: other values from here on.
+    __device__ __forceinline__ void forget() { asm("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3])); }
+    __device__ __forceinline__ void load_low(const float* p, int live)
+    {
+        if (live >= 4) mvx::load4(p, 4, x);
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = i < live ? p[i] : -kInf;
+    }
     __device__ __forceinline__ void load(const float* p, int64_t live) { mvx::load4(p, live, x); }
     __device__ __forceinline__ float at(int i) const { return x[i]; }
 };
 template <>
 struct Chunk<uint16_t> {
     uint32_t x[4];
+    __device__ __forceinline__ void clear() { x[0] = x[1] = x[2] = x[3] = 0xFF80FF80u; }
+    __device__ __forceinline__ void forget() { asm("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3])); }
+    __device__ __forceinline__ void load_low(const uint16_t* p, int live)
+    {
+        if (live >= 8) mvx::load8(p, 8, x);
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                x[i] = (2 * i < live ? p[2 * i] : 0xFF80u) | (2 * i + 1 < live ? (uint32_t)p[2 * i + 1] : 0xFF80u) << 16;
+    }
     __device__ __forceinline__ void load(const uint16_t* p, int64_t live) { mvx::load8(p, live, x); }
     __device__ __forceinline__ float at(int i) const { return i & 1 ? __uint_as_float(x[i / 2] & 0xFFFF0000u) : mvx::widen(x[i / 2]); }
 };
