@@ -46,6 +46,12 @@ struct Distill {
 };
 
 __device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x); }
+// A lane's number that nothing is made of beforehand, where registers are short.
+__device__ __forceinline__ uint32_t fresh(uint32_t lane)
+{
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
 __device__ __forceinline__ float larger(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, kInf); }    // one instruction
 
 // The largest of a lane's logits.  Pairs of bf16 as they are: as whole numbers non-negative ones have their order, and are
@@ -159,7 +165,7 @@ template <typename T>
 __device__ __forceinline__ Terms take_list(const Distill& d, const List& l, int64_t row, const T* z, Entry first, float largest, int64_t from,
                                            int64_t to)
 {
-    const uint32_t lane = threadIdx.x & 63u, all = room_of(d.top) + 1;
+    const uint32_t lane = fresh(threadIdx.x & 63u), all = room_of(d.top) + 1;
     float most = first.t;
     if (lane < all) first.keep(l, lane);
     for (uint32_t j = lane + 64; j < all; j += 64) {
@@ -230,7 +236,8 @@ template <typename T, int THREADS, int TERMS>
 __device__ __forceinline__ void patch(const Distill& d, const List& l, const Weights& w, int64_t row, int32_t label, int64_t from, int64_t to)
 {
     typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x % THREADS / 64, room = room_of(d.top);
+    const uint32_t lane = fresh(threadIdx.x & 63u), room = room_of(d.top);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x % THREADS / 64);
     if (!w.any) return;
     for (uint32_t j = lane; j < room + 1; j += 64) {
         const int32_t at = l.idx[j];
@@ -255,8 +262,8 @@ __device__ __forceinline__ void patch(const Distill& d, const List& l, const Wei
 
 // ---- a row in registers ------------------------------------------------------------------------------------------------
 
-// LANES threads with up to C whole chunks each, and one that the row may end in.  Chunks that a row does not have are
-// -infinity, which costs less than to ask for each whether it is there.
+// LANES threads with up to C whole chunks each, and one that the row may end in.  With no more than a hundred registers
+// beside them: whole chunks come and go through buffers, and chunks that a row does not have are 0 and left out.
 template <typename T, int LANES, int C, int TERMS>
 __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distill d)
 {
@@ -269,25 +276,22 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
     const List list = list_at(lds + mine * list_bytes(d.top), d.top);
     const int n = (int)d.n, full = n / (LANES * V), rest = n - full * (LANES * V) - (int)t * V;
     Chunk<T> held[C], tail;
-    auto row_at = [&](int64_t row) { return static_cast<const T*>(d.z) + row * d.ld_z; };
     // in one scalar comparison each time, not in sixteen masks that are kept
     auto there = [&](int c) {
         int f = full;
         asm("" : "+s"(f));
         return c < f;
     };
-    auto fetch = [&](const T* z, int c) { held[c].load(z + c * (LANES * V) + t * V, V); };
+    auto row_at = [&](int64_t row) { return static_cast<const T*>(d.z) + row * d.ld_z; };
     auto fetch_tail = [&](const T* z) { tail.load_low(z + full * (LANES * V) + t * V, rest); };
     int64_t row = (int64_t)blockIdx.x * kRows + mine;
     const int64_t step = (int64_t)gridDim.x * kRows;
-    if (row < d.rows) {
-        const T* z = row_at(row);
+    if (row >= d.rows) return;                                           // a wavefront's own row, or the whole workgroup's
+    {
+        const RowOf z(row_at(row), full * (LANES * 16));
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            held[c].clear();
-            if (there(c)) fetch(z, c);
-        }
-        fetch_tail(z);
+        for (int c = 0; c < C; ++c) held[c].take(z.load(t * 16, c * (LANES * 16)));
+        fetch_tail(row_at(row));
     }
     for (; row < d.rows; row += step) {
         Entry entry;
@@ -296,7 +300,7 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
         most.look(tail);
 #pragma unroll
         for (int c = 0; c < C; ++c)
-            most.look(held[c]);
+            if (there(c)) most.look(held[c]);
         float largest = wave_max(most.value());
         if (wave == 0) entry.look(row_at(row));
         if constexpr (kWaves > 1) {
@@ -308,10 +312,8 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
         float a = 0.0f, b = 0.0f;
         add_up<T, TERMS>(tail, largest, d.scale, a, b);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            add_up<T, TERMS>(held[c], largest, d.scale, a, b);
-            __builtin_amdgcn_sched_barrier(0);
-        }
+        for (int c = 0; c < C; ++c)
+            if (there(c)) add_up<T, TERMS>(held[c], largest, d.scale, a, b);
         a = wave_sum(a);
         if (TERMS != kOne) b = wave_sum(b);
         Terms w;
@@ -336,30 +338,27 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
             }
         }
         const Weights weights = weights_of<TERMS>(d, w.soft, w.label, d.grad ? d.grad[row] : 1.0f, largest, a, b);
+        // each chunk's registers take the next row's as soon as its own is written; behind the last row there is nothing
         const bool more = row + step < d.rows;
-        const T* next = row_at(row + step);
-        if (d.dz.p) {
+        const RowOf next(row_at(more ? row + step : row), more ? full * (LANES * 16) : 0);
+        const RowOf dz(static_cast<char*>(d.dz.p) + row * d.ld_dz * (d.dz.bf16 ? 2 : 4), d.dz.p ? full * (LANES * V) * (d.dz.bf16 ? 2 : 4) : 0);
 #pragma unroll
-            for (int c = 0; c < C; ++c)
-                if (there(c)) {
-                    float y[V];
-                    held[c].forget();                                    // what was made of it for the sums is not kept
-                    plain_grad<T, TERMS>(held[c], weights, d.scale, y);
-                    d.dz.store(row * d.ld_dz + c * (LANES * V) + t * V, V, y);
-                    if (more) fetch(next, c);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+        for (int c = 0; c < C; ++c) {
+            if (there(c)) {
+                float y[V];
+                held[c].forget();                                        // what was made of it for the sums is not kept
+                plain_grad<T, TERMS>(held[c], weights, d.scale, y);
+                dz.store<LANES>(y, t, c, d.dz.bf16);
+            }
+            held[c].take(next.load(t * 16, c * (LANES * 16)));
+        }
+        if (d.dz.p) {
             float y[V];
             plain_grad<T, TERMS>(tail, weights, d.scale, y);
             d.dz.store(row * d.ld_dz + full * (LANES * V) + t * V, rest, y);
-            if (more) fetch_tail(next);
             patch<T, LANES, TERMS>(d, list, weights, row, w.label, 0, d.n);
-        } else if (more) {
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-                if (there(c)) fetch(next, c);
-            fetch_tail(next);
         }
+        if (more) fetch_tail(row_at(row + step));
     }
 }
 
@@ -562,8 +561,7 @@ static Lanes lanes_of(int64_t n, int32_t dtype, int64_t top)
     const int64_t wide = dtype == MV_BF16 ? 8 : 4, chunks = n / wide;
     if (chunks < 64 * 4 && top <= 1024) return {64, 4};                  // four rows' lists in one workgroup's LDS: 48 KB
     for (int lanes : {256, 512, 1024})
-        for (int c : {12, 16})
-            if (chunks < (int64_t)lanes * (c + 1)) return {lanes, c};    // the tail is one more
+        if (chunks < (int64_t)lanes * 17) return {lanes, 16};            // the tail is one more
     return {0, 0};
 }
 
@@ -602,9 +600,9 @@ template <typename T, int TERMS>
 static void loss(Distill d, const Lanes& l, hipStream_t st)
 {
     if (l.lanes == 64) return held<T, 64, 4, TERMS>(d, st);
-    if (d.dz.p && l.lanes == 256) return l.chunks == 12 ? held<T, 256, 12, TERMS>(d, st) : held<T, 256, 16, TERMS>(d, st);
-    if (d.dz.p && l.lanes == 512) return l.chunks == 12 ? held<T, 512, 12, TERMS>(d, st) : held<T, 512, 16, TERMS>(d, st);
-    if (d.dz.p && l.lanes == 1024) return l.chunks == 12 ? held<T, 1024, 12, TERMS>(d, st) : held<T, 1024, 16, TERMS>(d, st);
+    if (d.dz.p && l.lanes == 256) return held<T, 256, 16, TERMS>(d, st);
+    if (d.dz.p && l.lanes == 512) return held<T, 512, 16, TERMS>(d, st);
+    if (d.dz.p && l.lanes == 1024) return held<T, 1024, 16, TERMS>(d, st);
     const Ranges r = ranges_of(d.rows, d.n);
     d.ranges = r.count, d.range = r.length;
     if (r.count == 1 || !d.parts) {

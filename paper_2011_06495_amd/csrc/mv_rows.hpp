@@ -27,7 +27,11 @@ template <>
 struct Chunk<float> {
     float x[4];
     // what is not there: -infinity
-    __device__ __forceinline__ void clear() { x[0] = x[1] = x[2] = x[3] = -kInf; }
+    __device__ __forceinline__ void take(const u32x4& w)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]);
+    }
     // To the compiler: other values from here on.
     __device__ __forceinline__ void forget() { asm("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3])); }
     __device__ __forceinline__ void load_low(const float* p, int live)
@@ -43,7 +47,11 @@ struct Chunk<float> {
 template <>
 struct Chunk<uint16_t> {
     uint32_t x[4];
-    __device__ __forceinline__ void clear() { x[0] = x[1] = x[2] = x[3] = 0xFF80FF80u; }
+    __device__ __forceinline__ void take(const u32x4& w)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = w[i];
+    }
     __device__ __forceinline__ void forget() { asm("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3])); }
     __device__ __forceinline__ void load_low(const uint16_t* p, int live)
     {
@@ -119,6 +127,42 @@ struct AnyOut {
     {
         if (bf16) static_cast<uint16_t*>(p)[i] = (uint16_t)mvx::narrow(x);
         else static_cast<float*>(p)[i] = x;
+    }
+};
+
+// A row's whole chunks as a buffer: an offset of the lane's own and one that all share, and no addresses in between.  What lies
+// behind them reads as 0 and is not written.
+struct RowOf {
+    __amdgpu_buffer_rsrc_t buf;
+    __device__ __forceinline__ RowOf(const void* p, int bytes)
+        : buf(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000))
+    {
+    }
+    __device__ __forceinline__ u32x4 load(uint32_t mine, uint32_t all) const
+    {
+        return __builtin_amdgcn_raw_buffer_load_b128(buf, mine, all, 0);
+    }
+    __device__ __forceinline__ void store(const u32x4& w, uint32_t mine, uint32_t all) const
+    {
+        __builtin_amdgcn_raw_buffer_store_b128(w, buf, mine, all, 2);    // past the caches
+    }
+    // V values at chunk `c` of LANES threads, fp32 or bf16.
+    template <int LANES, int V>
+    __device__ __forceinline__ void store(const float (&y)[V], uint32_t t, int c, bool bf16) const
+    {
+        if (!bf16) {
+#pragma unroll
+            for (int h = 0; h < V; h += 4)
+                store(u32x4{__float_as_uint(y[h]), __float_as_uint(y[h + 1]), __float_as_uint(y[h + 2]), __float_as_uint(y[h + 3])},
+                      t * (V * 4) + h * 4, c * (LANES * V * 4));
+        } else {
+            uint32_t w[V / 2];
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) w[i] = mvx::narrow(y[2 * i]) | mvx::narrow(y[2 * i + 1]) << 16;
+            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+            if constexpr (V == 8) store(u32x4{w[0], w[1], w[2], w[3]}, t * 16, c * (LANES * 16));
+            else __builtin_amdgcn_raw_buffer_store_b64(u32x2{w[0], w[1]}, buf, t * 8, c * (LANES * 8), 2);
+        }
     }
 };
 
