@@ -37,11 +37,12 @@ __device__ __forceinline__ i32x8 whole(const Half& h)
 {
     return i32x8{(int)h.lo.x, (int)h.lo.y, (int)h.lo.z, (int)h.lo.w, (int)h.hi.x, (int)h.hi.y, (int)h.hi.z, (int)h.hi.w};
 }
-// c += a b over one instruction's bytes, scale byte S of each word; the two zeros say that both factors are of this kind.
-template <int S>
+// c += a b over one instruction's bytes, with byte SA, or SB, of a word of scales; the two zeros say that both factors are of
+// this kind.
+template <int SA, int SB>
 __device__ __forceinline__ f32x16 mfma32(const Half& a, uint32_t a_scale, const Half& b, uint32_t b_scale, f32x16 c)
 {
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(a), whole(b), c, 0, 0, S, (int)a_scale, S, (int)b_scale);
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(a), whole(b), c, 0, 0, SA, (int)a_scale, SB, (int)b_scale);
 }
 
 // The same 32 values as bf16, with their scale.
@@ -55,11 +56,10 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi, float factor)
     const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, factor, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, factor, true);
     return bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
-// S: which byte of the word the scale is.
-template <int S>
+// The scale is the lowest byte of the word.
 __device__ __forceinline__ Wide widen(const Half& h, uint32_t scale)
 {
-    const float f = mvx::factor_of(scale >> (8 * S) & 0xFFu);
+    const float f = mvx::factor_of(scale & 0xFFu);
     return Wide{{widen(h.lo.x, h.lo.y, f), widen(h.lo.z, h.lo.w, f), widen(h.hi.x, h.hi.y, f), widen(h.hi.z, h.hi.w, f)}};
 }
 __device__ __forceinline__ f32x4 mfma(const Wide& a, const Wide& b, f32x4 c)
@@ -99,10 +99,10 @@ __global__ __launch_bounds__(kProductThreads) void mv_f8_product_kernel(Factor a
         }
         Wide yw[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) yw[u] = widen<0>(y[u], ys[u]);
+        for (int u = 0; u < 4; ++u) yw[u] = widen(y[u], ys[u]);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const Wide xw = widen<0>(x[t], xs[t]);
+            const Wide xw = widen(x[t], xs[t]);
 #pragma unroll
             for (int u = 0; u < 4; ++u) acc[t][u] = mfma(yw[u], xw, acc[t][u]);
         }
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(64 * WM * WN, BUFFERS == 1 ? 3 : 2) void mv_f8_prod
     constexpr int kM = 32 * MT * WM, kN = 32 * NT * WN, kRows = kM + kN;
     typedef uint8_t Codes[kRows * kBlock];
     __shared__ __attribute__((aligned(1024))) Codes even;
-    __shared__ uint16_t scales[2][kRows];
+    __shared__ __attribute__((aligned(4))) uint16_t scales[2][kRows];
     const uint32_t t = threadIdx.x, lane = t & 63u, wave = __builtin_amdgcn_readfirstlane(t / 64);
     const Product& p = l.product();
     const Factor a = p.a, b = p.b;
@@ -169,23 +169,26 @@ __global__ __launch_bounds__(64 * WM * WN, BUFFERS == 1 ? 3 : 2) void mv_f8_prod
     const __amdgpu_buffer_rsrc_t b_buf = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint8_t*>(b.codes + j0 * b.ld_bytes), 0, (int)((uint32_t)(b_rows - 1) * b_pitch + blocks * kBlock), 0x00020000);
     static_assert(kM / kWaves % 16 == 0 && kN / kWaves % 16 == 0, "rows from a multiple of 16 on");
-    const uint32_t row_in = lane >> 3, unit0 = (lane & 7u) ^ (row_in >> 1), unit1 = unit0 ^ 4u;      // of every second eight rows
-    const uint32_t a_at = (wave * (kM / kWaves) + row_in) * a_pitch, b_at = (wave * (kN / kWaves) + row_in) * b_pitch;
+    const uint32_t row_in = lane >> 3, unit = (lane & 7u) ^ (row_in >> 1);       // of every second eight rows unit ^ 4
+    uint32_t other = unit & 4u ? 0u - 64u : 64u;
+    uint32_t a_at = (wave * (kM / kWaves) + row_in) * a_pitch + unit * 16, b_at = (wave * (kN / kWaves) + row_in) * b_pitch + unit * 16;
     auto load_codes = [&](uint32_t k, Codes& to) {
         const uint32_t step = step0 + k;
-        // The whole offset is the lane's own, for the bounds to hold: beyond every buffer where there is no such block.
+        // The whole offset is the lane's own, for the bounds to hold: beyond every buffer where there is no such block.  It is
+        // made anew each time: eight registers that are kept for it are eight too many.
         const uint32_t at = step * kBlock;
         const bool live = step < end;
+        asm volatile("" : "+v"(a_at), "+v"(b_at), "+v"(other));
 #pragma unroll
         for (int i = 0; i < kM / kWaves / 8; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 a_buf, (__attribute__((address_space(3))) void*)(to + (wave * (kM / kWaves) + i * 8) * kBlock), 16,
-                live ? a_at + i * 8 * a_pitch + at + (i % 2 ? unit1 : unit0) * 16 : 0x80000000u, 0, 0, 0);
+                live ? (i % 2 ? a_at + other : a_at) + (i * 8 * a_pitch + at) : 0x80000000u, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < kN / kWaves / 8; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 b_buf, (__attribute__((address_space(3))) void*)(to + (kM + wave * (kN / kWaves) + i * 8) * kBlock), 16,
-                live ? b_at + i * 8 * b_pitch + at + (i % 2 ? unit1 : unit0) * 16 : 0x80000000u, 0, 0, 0);
+                live ? (i % 2 ? b_at + other : b_at) + (i * 8 * b_pitch + at) : 0x80000000u, 0, 0, 0);
     };
     // A thread has one row's scales, of a the first wavefronts, of b the others: one load for two steps, which reads zeros
     // where the rows end, and what lies behind a row's last block.
@@ -200,14 +203,15 @@ __global__ __launch_bounds__(64 * WM * WN, BUFFERS == 1 ? 3 : 2) void mv_f8_prod
     auto fetch_scales = [&](uint32_t k) { next = __builtin_amdgcn_raw_buffer_load_b16(sc_buf, sc_at + step0 + k, 0, 0); };
     auto keep_scales = [&](uint32_t k) {
         const int live = (int)end - (int)(step0 + k);
-        scales[k / 2 % 2][t] = (uint16_t)(next & (live >= 2 ? 0xFFFFu : live == 1 ? 0xFFu : 0u));
+        // rows 32 apart side by side
+        scales[k / 2 % 2][(t & ~63u) + (t & 31u) * 2 + (t >> 5 & 1u)] = (uint16_t)(next & (live >= 2 ? 0xFFFFu : live == 1 ? 0xFFu : 0u));
     };
 
     const uint32_t in = lane & 31u, half = lane >> 5;
     const uint32_t a_row = wave / WN * (32 * MT) + in, b_row = kM + wave % WN * (32 * NT) + in;
     f32x16 acc[MT][NT] = {};
     Half x[MT], y[2][NT];
-    uint32_t as[MT], bs[NT];
+    uint32_t as[MT / 2], bs[NT / 2], next_as[MT / 2], next_bs[NT / 2];     // two rows' scales of two steps in each
     // bytes of half step s: units 4 s + half and two more
     const uint32_t turn = lane >> 1 & 7u;
     auto read = [&](const Codes& from, uint32_t row, uint32_t s, Half& h) {
@@ -218,23 +222,24 @@ __global__ __launch_bounds__(64 * WM * WN, BUFFERS == 1 ? 3 : 2) void mv_f8_prod
 #pragma unroll
         for (int j = 0; j < NT; ++j) read(from, b_row + 32 * j, s, to[j]);
     };
-    auto read_scales = [&](uint32_t k) {
-        const uint16_t* sc = scales[k / 2 % 2];
+    auto read_scales = [&](uint32_t k, uint32_t (&a_to)[MT / 2], uint32_t (&b_to)[NT / 2]) {
+        typedef uint32_t __attribute__((may_alias)) pair;
+        const pair* sc = reinterpret_cast<const pair*>(scales[k / 2 % 2]);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) as[i] = sc[a_row + 32 * i];
+        for (int i = 0; i < MT / 2; ++i) a_to[i] = sc[((a_row & ~63u) >> 1) + 32 * i + in];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) bs[j] = sc[b_row + 32 * j];
+        for (int j = 0; j < NT / 2; ++j) b_to[j] = sc[((b_row & ~63u) >> 1) + 32 * j + in];
     };
     // The products of half a step, whose rows are here; each row's next half is asked for right behind its last product.
-    auto products = [&](auto scale_byte, const Half (&with)[NT], const Codes& then, uint32_t then_s) {
-        constexpr int S = decltype(scale_byte)::value;
+    auto products = [&](auto step, const Half (&with)[NT], const Codes& then, uint32_t then_s) {
+        constexpr int S = decltype(step)::value;
         if constexpr (WIDE) {
             Wide yw[NT];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) yw[j] = widen<S>(with[j], bs[j]);
+            for (int j = 0; j < NT; ++j) yw[j] = widen(with[j], bs[j / 2] >> (8 * S + 16 * (j % 2)));
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                const Wide xw = widen<S>(x[i], as[i]);
+                const Wide xw = widen(x[i], as[i / 2] >> (8 * S + 16 * (i % 2)));
                 read(then, a_row + 32 * i, then_s, x[i]);
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
@@ -243,11 +248,16 @@ __global__ __launch_bounds__(64 * WM * WN, BUFFERS == 1 ? 3 : 2) void mv_f8_prod
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {
+            static_assert(NT == 2 && MT % 2 == 0, "pairs of rows");
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mfma32<S>(with[j], bs[j], x[i], as[i], acc[i][j]);
+            for (int i = 0; i < MT; i += 2) {
+                acc[i][0] = mfma32<S, S>(with[0], bs[0], x[i], as[i / 2], acc[i][0]);
+                acc[i][1] = mfma32<2 + S, S>(with[1], bs[0], x[i], as[i / 2], acc[i][1]);
                 read(then, a_row + 32 * i, then_s, x[i]);
+                __builtin_amdgcn_sched_barrier(0);
+                acc[i + 1][0] = mfma32<S, 2 + S>(with[0], bs[0], x[i + 1], as[i / 2], acc[i + 1][0]);
+                acc[i + 1][1] = mfma32<2 + S, 2 + S>(with[1], bs[0], x[i + 1], as[i / 2], acc[i + 1][1]);
+                read(then, a_row + 32 * i + 32, then_s, x[i + 1]);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -266,12 +276,12 @@ __global__ __launch_bounds__(64 * WM * WN, BUFFERS == 1 ? 3 : 2) void mv_f8_prod
                 keep_scales(k);
             }
             all_here();
-            read_scales(k);
+            read_scales(k, as, bs);
             if (k % 2) {
 #pragma unroll
-                for (int i = 0; i < MT; ++i) as[i] >>= 8;
+                for (int i = 0; i < MT / 2; ++i) as[i] >>= 8;
 #pragma unroll
-                for (int j = 0; j < NT; ++j) bs[j] >>= 8;
+                for (int j = 0; j < NT / 2; ++j) bs[j] >>= 8;
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i) read(even, a_row + 32 * i, 0, x[i]);
@@ -292,7 +302,7 @@ __global__ __launch_bounds__(64 * WM * WN, BUFFERS == 1 ? 3 : 2) void mv_f8_prod
 #pragma unroll
         for (int i = 0; i < MT; ++i) read(even, a_row + 32 * i, 0, x[i]);
         read_y(even, 0, y[0]);
-        read_scales(0);
+        read_scales(0, as, bs);
         // Two steps a turn.  In the middle of a step all wavefronts have read its buffer, so there the next loads into it
         // begin, and the second half's products cover the way of the next step's first rows from LDS.  The turn has no branches:
         // behind the last step zeros are loaded.
@@ -310,8 +320,12 @@ __global__ __launch_bounds__(64 * WM * WN, BUFFERS == 1 ? 3 : 2) void mv_f8_prod
             all_here();
             load_codes(k + 3, odd);
             read_y(even, 0, y[0]);
+            read_scales(k + 2, next_as, next_bs);
             products(second, y[1], even, 0);
-            read_scales(k + 2);
+#pragma unroll
+            for (int i = 0; i < MT / 2; ++i) as[i] = next_as[i];
+#pragma unroll
+            for (int j = 0; j < NT / 2; ++j) bs[j] = next_bs[j];
         }
         __builtin_amdgcn_s_waitcnt(kNoLoads);
     }
@@ -472,9 +486,9 @@ struct Turn {
 template <int S, int NT>
 __device__ __forceinline__ void add(const Turn<NT>& now, const Half (&x)[kTurn], uint32_t xs, f32x4 (&acc)[NT])
 {
-    const Wide xw = widen<S>(x[S], xs);
+    const Wide xw = widen(x[S], xs >> (8 * S));
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = mfma(widen<S>(now.codes[t][S], now.scales[t]), xw, acc[t]);
+    for (int t = 0; t < NT; ++t) acc[t] = mfma(widen(now.codes[t][S], now.scales[t] >> (8 * S)), xw, acc[t]);
 }
 
 // A workgroup: 16 MT few rows, 16 NT of the many.
