@@ -377,11 +377,13 @@ __global__ __launch_bounds__(256) void mv_f8_product_join_kernel(const float* __
 // ---- few rows of one factor ------------------------------------------------------------------------------------------
 //
 // Up to 16 rows of one factor ("few"; up to 64 where they are values) against many of the other ("many"), whose
-// codes are the bytes to read.  A workgroup takes 16 NT of the many rows and all of k, its wavefronts turns of four
+// codes are the bytes to read.  A workgroup takes 16 of the many rows and all of k, its wavefronts turns of four
 // blocks; what they have is added up through LDS in the wavefronts' order.  Lane l of an instruction holds row l % 16
 // and the 16-byte units l / 16 and l / 16 + 4 of the block, so the four lanes of a row read 64 bytes in a row.  The four
-// scales of a row and turn are one word.  The few rows' codes and scales are in LDS: copied there, or quantised by every
-// workgroup for itself, four lanes a block, while the first turn's codes are on their way.
+// scales of a row and turn are one word.  The few rows' codes are read as the many's are, out of the caches; values are
+// quantised by every workgroup for itself, four lanes a block, into LDS, while the first turn's codes are on their way.
+// Loads in flight are what it lives on, and those of many wavefronts with one turn each are worth more than two turns each of
+// the half of them: 5 x 8192 bf16 by 16,384 31.6 us (two turns 37.7, and 32 of the many rows to a workgroup 41.0).
 
 constexpr int kTurn = 4;            // blocks
 constexpr int kFewWaves = 8;
@@ -394,22 +396,10 @@ struct Few {                        // X: uint8_t: codes; uint16_t or float: bf1
     uint32_t       count;
 };
 
-// A quarter of a block of the few rows on its way, 32 values or codes: fetched, and then made codes and scale of, the four
-// quarters of a block by four consecutive lanes.
+// A quarter of a block of the few rows on its way, 32 values: fetched, and then made codes and scale of, the four quarters of a
+// block by four consecutive lanes.
 template <typename X>
 struct Quarter;
-template <>
-struct Quarter<uint8_t> {
-    u32x4    w[2];
-    uint32_t scale;
-    __device__ __forceinline__ void fetch(const Few<uint8_t>& f, uint32_t row, uint32_t block, uint32_t q, int64_t)
-    {
-        const u32x4* p = reinterpret_cast<const u32x4*>(f.rows + row * f.ld + (int64_t)block * kBlock + q * 32);
-        w[0] = p[0], w[1] = p[1];
-        scale = f.scales[row * f.ld_scales + block];
-    }
-    __device__ __forceinline__ void finish(u32x4 (&codes)[2], uint32_t& s) const { codes[0] = w[0], codes[1] = w[1], s = scale; }
-};
 template <>
 struct Quarter<float> {
     float x[4][8];
@@ -461,8 +451,8 @@ struct Quarter<uint16_t> {
     }
 };
 
-// LDS of the few rows: `count` rows of `turns` x 4 blocks, rows 16 bytes longer against bank conflicts, then a word of
-// scales for each row and turn.
+// LDS of the few rows' values: `count` rows of `turns` x 4 blocks of codes, rows 16 bytes longer against bank conflicts, then a
+// word of scales for each row and turn.
 __host__ __device__ constexpr uint32_t few_pitch(uint32_t turns) { return turns * (kTurn * kBlock) + 16; }
 __host__ __device__ constexpr uint32_t few_bytes(uint32_t count, uint32_t turns) { return count * (few_pitch(turns) + turns * kTurn); }
 
@@ -477,131 +467,114 @@ struct FewProduct {
     int64_t  step_many, step_few;
 };
 
-// A lane's codes and scales of a turn of the many rows; and block S of them times the same of 16 few rows.
-template <int NT>
+// A lane's codes and scales of a turn of a row.  Of its last turn's blocks that there are not the last one is read again: loads
+// that may be left out leave open how many are on their way, and a wait for earlier ones becomes one for all.
 struct Turn {
-    Half     codes[NT][kTurn];
-    uint32_t scales[NT];
-};
-template <int S, int NT>
-__device__ __forceinline__ void add(const Turn<NT>& now, const Half (&x)[kTurn], uint32_t xs, f32x4 (&acc)[NT])
-{
-    const Wide xw = widen(x[S], xs >> (8 * S));
+    Half     codes[kTurn];
+    uint32_t scales;
+    __device__ __forceinline__ void load(const uint8_t* row, const uint8_t* row_scales, uint32_t block, uint32_t blocks)
+    {
+        scales = *reinterpret_cast<const uint32_t*>(row_scales + block);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = mfma(widen(now.codes[t][S], now.scales[t] >> (8 * S)), xw, acc[t]);
+        for (uint32_t b = 0; b < kTurn; ++b) {
+            const uint8_t* p = row + (int64_t)min(block + b, blocks - 1) * kBlock;
+            codes[b].lo = *reinterpret_cast<const u32x4*>(p);
+            codes[b].hi = *reinterpret_cast<const u32x4*>(p + 64);
+        }
+    }
+};
+// Its products with the same of the few rows, a block at a time, and those of the last turn as far as there are any.
+template <int S = 0>
+__device__ __forceinline__ void add(const Turn& a, const uint8_t* p, uint32_t scales, int live, f32x4& c)
+{
+    if constexpr (S < kTurn) {
+        if (S == 0 || live > S) {
+            const Half x = {*reinterpret_cast<const u32x4*>(p + S * kBlock), *reinterpret_cast<const u32x4*>(p + S * kBlock + 64)};
+            c = mfma(widen(a.codes[S], a.scales >> (8 * S)), widen(x, scales >> (8 * S)), c);
+            add<S + 1>(a, p, scales, live, c);
+        }
+    }
 }
 
-// A workgroup: 16 MT few rows, 16 NT of the many.
-template <int MT, int NT, typename X, bool PAIR>
-__global__ __launch_bounds__(64 * kFewWaves) void mv_f8_product_few_kernel(Launch<FewProduct<X>, PAIR> l)
+// A workgroup: 16 MT few rows, 16 of the many.
+template <int MT, typename X, bool PAIR>
+__global__ __launch_bounds__(64 * kFewWaves, MT == 1 ? 4 : 2) void mv_f8_product_few_kernel(Launch<FewProduct<X>, PAIR> l)
 {
+    constexpr bool kCodes = std::is_same_v<X, uint8_t>;
+    static_assert(!kCodes || MT == 1, "codes: up to 16 rows");
     const FewProduct<X>& p = l.product();
     const uint32_t id = l.id();
     const Factor many = p.many;
     const Few<X> few = p.few;
     const uint32_t blocks = p.blocks;
-    const int64_t k = p.k, j0 = (int64_t)id * (16 * NT);
+    const int64_t k = p.k, j0 = (int64_t)id * 16;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
     const uint32_t in = lane & 15u, g = lane / 16;
     extern __shared__ __attribute__((aligned(16))) uint8_t held[];
     const uint32_t turns = (blocks + kTurn - 1) / kTurn, row_blocks = turns * kTurn, pitch = few_pitch(turns);
     uint8_t* held_scales = held + few.count * pitch;
 
-    // Loads come back in their order, so what goes into LDS is asked for first ...
-    Quarter<X> mine;
-    const uint32_t quarters = few.count * row_blocks * 4;
-    auto fetch = [&](uint32_t at) {
-        const uint32_t row = at / (4 * row_blocks), block = at / 4 - row * row_blocks;
-        if (at < quarters && block < blocks) mine.fetch(few, row, block, at % 4, k);
-    };
-    auto hold = [&](uint32_t at) {
-        if (at >= quarters) return;
-        const uint32_t row = at / (4 * row_blocks), block = at / 4 - row * row_blocks, q = at % 4;
-        u32x4 codes[2] = {{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
-        uint32_t scale = 127;
-        if (block < blocks) mine.finish(codes, scale);                   // all four lanes of a block
-        *reinterpret_cast<u32x4*>(held + row * pitch + block * kBlock + q * 32) = codes[0];
-        *reinterpret_cast<u32x4*>(held + row * pitch + block * kBlock + q * 32 + 16) = codes[1];
-        if (q == 0) held_scales[row * row_blocks + block] = (uint8_t)scale;
-    };
-    fetch(threadIdx.x);
-    // ... then codes and scales, of two turns; codes behind the last block are some block's, and meet zeros of the few rows,
-    // and scales there are 1
-    const uint8_t* rows[NT];
-    const uint8_t* row_scales[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int64_t j = j0 + 16 * t + in, row = j < many.rows ? j : many.rows - 1;
-        rows[t] = many.codes + row * many.ld_bytes + g * 16;
-        row_scales[t] = many.scales + row * many.ld_scales;
-    }
-    Turn<NT> one, two;
-    auto load = [&](uint32_t block, Turn<NT>& to) {
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            to.scales[t] = *reinterpret_cast<const uint32_t*>(row_scales[t] + block);
-#pragma unroll
-            for (int s = 0; s < kTurn; ++s) {
-                const uint8_t* from = rows[t] + (int64_t)min(block + s, blocks - 1) * kBlock;
-                to.codes[t][s].lo = *reinterpret_cast<const u32x4*>(from);
-                to.codes[t][s].hi = *reinterpret_cast<const u32x4*>(from + 64);
-            }
-        }
-    };
-    const uint32_t step = waves * kTurn;
+    const int64_t row = j0 + in < many.rows ? j0 + in : many.rows - 1;
+    const uint8_t *codes = many.codes + row * many.ld_bytes + g * 16, *scales = many.scales + row * many.ld_scales;
     uint32_t block = wave * kTurn;
-    if (block < blocks) load(block, one);
-    hold(threadIdx.x);
-    if (block + step < blocks) load(block + step, two);
-    for (uint32_t at = threadIdx.x + blockDim.x; at < quarters; at += blockDim.x) {
-        fetch(at);
-        hold(at);
-    }
-    __syncthreads();
-    f32x4 acc[MT][NT] = {};
-    auto products = [&](Turn<NT>& now) {
-        const int live = (int)blocks - (int)block;
-        const uint32_t real = live >= 4 ? 0xFFFFFFFFu : (1u << (8 * live)) - 1u;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) now.scales[t] = (now.scales[t] & real) | (0x7F7F7F7Fu & ~real);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const uint32_t row = min(16 * i + in, few.count - 1);
-            const uint8_t* from = held + row * pitch + block * kBlock + g * 16;
-            Half x[kTurn];
-#pragma unroll
-            for (int s = 0; s < kTurn; ++s) {
-                x[s].lo = *reinterpret_cast<const u32x4*>(from + s * kBlock);
-                x[s].hi = *reinterpret_cast<const u32x4*>(from + s * kBlock + 64);
-            }
-            const uint32_t xs = *reinterpret_cast<const uint32_t*>(held_scales + row * row_blocks + block);
-            add<0>(now, x, xs, acc[i]);
-            add<1>(now, x, xs, acc[i]);
-            add<2>(now, x, xs, acc[i]);
-            add<3>(now, x, xs, acc[i]);
+    Turn now;
+    f32x4 acc[MT] = {};
+    if constexpr (kCodes) {
+        const int64_t few_row = min(in, few.count - 1);
+        const uint8_t *few_codes = few.rows + few_row * few.ld + g * 16, *few_scales = few.scales + few_row * few.ld_scales;
+        for (; block < blocks; block += waves * kTurn) {
+            const int live = (int)(blocks - block);
+            now.load(codes, scales, block, blocks);
+            add(now, few_codes + (int64_t)block * kBlock, *reinterpret_cast<const uint32_t*>(few_scales + block), live, acc[0]);
         }
-    };
-    while (block < blocks) {
-        products(one);
-        if (block + 2 * step < blocks) load(block + 2 * step, one);
-        block += step;
-        if (block >= blocks) break;
-        products(two);
-        if (block + 2 * step < blocks) load(block + 2 * step, two);
-        block += step;
+    } else {
+        // Loads come back in their order, so what goes into LDS is asked for first.
+        Quarter<X> mine;
+        const uint32_t quarters = few.count * row_blocks * 4;
+        auto fetch = [&](uint32_t at) {
+            const uint32_t r = at / (4 * row_blocks), b = at / 4 - r * row_blocks;
+            if (at < quarters && b < blocks) mine.fetch(few, r, b, at % 4, k);
+        };
+        auto hold = [&](uint32_t at) {
+            const uint32_t r = at / (4 * row_blocks), b = at / 4 - r * row_blocks, q = at % 4;
+            if (at >= quarters || b >= blocks) return;                   // all four lanes of a block
+            u32x4 made[2];
+            uint32_t scale;
+            mine.finish(made, scale);
+            *reinterpret_cast<u32x4*>(held + r * pitch + b * kBlock + q * 32) = made[0];
+            *reinterpret_cast<u32x4*>(held + r * pitch + b * kBlock + q * 32 + 16) = made[1];
+            if (q == 0) held_scales[r * row_blocks + b] = (uint8_t)scale;
+        };
+        fetch(threadIdx.x);
+        now.load(codes, scales, min(block, (blocks - 1) / kTurn * kTurn), blocks);
+        hold(threadIdx.x);
+        for (uint32_t at = threadIdx.x + blockDim.x; at < quarters; at += blockDim.x) {
+            fetch(at);
+            hold(at);
+        }
+        __syncthreads();
+        while (block < blocks) {
+            const int live = (int)(blocks - block);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const uint32_t r = min(16 * i + in, few.count - 1);
+                const uint32_t few_word = *reinterpret_cast<const uint32_t*>(held_scales + r * row_blocks + block);
+                add(now, held + r * pitch + block * kBlock + g * 16, few_word, live, acc[i]);
+            }
+            block += waves * kTurn;
+            if (block < blocks) now.load(codes, scales, block, blocks);
+        }
+        __syncthreads();
     }
-    __syncthreads();
     f32x4* sums = reinterpret_cast<f32x4*>(held);                         // wavefront, tile, lane
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) sums[((wave * MT + i) * NT + t) * 64 + lane] = acc[i][t];
+    for (int i = 0; i < MT; ++i) sums[(wave * MT + i) * 64 + lane] = acc[i];
     __syncthreads();
-    for (uint32_t at = threadIdx.x; at < MT * NT * 64; at += blockDim.x) {
+    for (uint32_t at = threadIdx.x; at < MT * 64; at += blockDim.x) {
         f32x4 v = sums[at];
-        for (uint32_t w = 1; w < waves; ++w) v += sums[w * MT * NT * 64 + at];
-        const uint32_t i = at / (64 * NT) * 16 + (at & 15u);
-        const int64_t j = j0 + at / 64 % NT * 16 + (at >> 4 & 3u) * 4, to = j * p.step_many + i * p.step_few;
+        for (uint32_t w = 1; w < waves; ++w) v += sums[w * MT * 64 + at];
+        const uint32_t i = at / 64 * 16 + (at & 15u);
+        const int64_t j = j0 + (at >> 4 & 3u) * 4, to = j * p.step_many + i * p.step_few;
         if (i >= few.count) continue;
         if (p.step_many == 1) {
             if (j < many.rows) p.c.put4(to, many.rows - j, v);
@@ -616,33 +589,35 @@ __global__ __launch_bounds__(64 * kFewWaves) void mv_f8_product_few_kernel(Launc
 constexpr int64_t  kFewRows = 16, kFewValues = 64;
 constexpr uint32_t kFewLds = 144 * 1024;
 
-// Whether and how the kernel for few rows takes a product: up to 16 rows of codes, and up to 64 of values as long as what all
-// workgroups quantise together, each for itself, is bounded, fp32 at a third of bf16.
-constexpr int64_t kQuantisedBf16 = 36000000, kQuantisedF32 = 12000000;
+// Whether and how the kernel for few rows takes a product: up to 16 rows of codes (with
+// 32 it is faster for some sizes and slower for others: 32 x 4096 by 4096 12.2 us, in tiles 13.8, 8192 by 8192 29.7, in tiles 21.5), and up to 64 of values where quantising them
+// in every workgroup costs less than a launch that does it once, which is where all of them together have few.
+// bf16 us in one launch, and in two: 2 x 4096 by 4096, 2 million values to all workgroups, 6.7 (9.1); 32 x 2048 by 2048, 8 M, 8.4
+// (11.9); 1 x 8192 by 16,384, 8 M, 26.7 (27.9); 3 x 8192 by 8192, 13 M, 16.3 (16.1); 16 x 4096 by 4096, 17 M, 10.0 (9.1); 5 x
+// 8192 by 16,384, 42 M, 36.2 (32.2); beyond 16 rows 64 x 1024 by 4096, 17 M, 9.3 (11.8).  fp32: 8 x 2048 by 4096, 4 M, 7.6 (9.0);
+// 1 x 8192 by 8192, 4 M, 16.4 (15.5); 2 x 8192 by 8192, 8 M, 17.8 (15.9); 20 x 2048 by 4000, 10 M, 10.8 (13.4).
+constexpr int64_t kQuantisedBf16 = 12000000, kQuantisedF32 = 5000000;
 struct FewCut {
-    int      mt, nt;                // 0: it does not
+    int      mt;                    // 0: it does not
     uint32_t groups, lds, waves;
 };
 static FewCut few_cut(int64_t few, int64_t many, int64_t k, int64_t quantised)     // most values to quantise; 0: codes
 {
     const bool values = quantised > 0;
     if (few > (values ? kFewValues : kFewRows)) return FewCut{};
+    if (values && few > 16) quantised *= 2;
     const int64_t turns = (blocks_of(k) + kTurn - 1) / kTurn;
     FewCut c = {};
     c.mt = few <= 16 ? 1 : few <= 32 ? 2 : 4;
-    // Workgroups of 16 rows as long as all of them run at once, three to a unit; beyond that 32 rows, which share what a
-    // workgroup spends on the few rows.
-    c.nt = c.mt == 1 && many > 12288 ? 2 : 1;
-    const int64_t groups = (many + 16 * c.nt - 1) / (16 * c.nt);
-    if (turns >= 4096 || groups > kMostGroups / 4 || (values && groups * few * k > quantised)) return FewCut{};
+    const int64_t groups = (many + 15) / 16;
+    if (groups > kMostGroups / 4 || (values && (turns >= 4096 || groups * few * k > quantised))) return FewCut{};
     c.groups = (uint32_t)groups;
-    // a wavefront for each turn, or for each 16 blocks of the few rows
-    const int64_t waves = few > 4 ? few * turns / 4 + 1 : turns;
+    // a wavefront for each turn, or for each 16 blocks of the few rows' values
+    const int64_t waves = values && few > 4 ? few * turns / 4 + 1 : turns;
     c.waves = (uint32_t)(waves < kFewWaves ? waves : kFewWaves);
-    const uint32_t sums = c.waves * c.mt * c.nt * 1024;
-    const int64_t lds = few_bytes(1, (uint32_t)turns) * few;
-    if (few <= kFewRows ? lds > kFewLds : c.groups > 256 || lds > kFewLds) return FewCut{};
-    c.lds = (uint32_t)lds < sums ? sums : (uint32_t)lds;
+    const int64_t sums = c.waves * c.mt * 1024, lds = values ? few_bytes(1, (uint32_t)turns) * few : 0;
+    if (lds > kFewLds || (values && few > 16 && c.groups > 256)) return FewCut{};
+    c.lds = (uint32_t)(lds < sums ? sums : lds);
     return c;
 }
 
@@ -652,30 +627,29 @@ static FewProduct<X> few_product(const Factor& many, const Few<X>& few, int64_t 
 {
     return {many, few, (uint32_t)blocks_of(k), k, c, step_many, step_few};
 }
-// One product, or two whose cuts have the same mt and nt.
-template <int MT, int NT, typename X>
+// One product, or two of codes.
+template <int MT, typename X>
 static void launch_few_of(const FewProduct<X>* p, const FewCut* cut, int n, hipStream_t st)
 {
     const dim3 threads(64 * (n == 2 && cut[1].waves > cut[0].waves ? cut[1].waves : cut[0].waves));
-    const uint32_t lds = n == 2 && cut[1].lds > cut[0].lds ? cut[1].lds : cut[0].lds;
+    const uint32_t lds = n == 2 ? threads.x * 16 : cut[0].lds;
     if constexpr (std::is_same_v<X, uint8_t>) {
         if (n == 2) {
-            hipLaunchKernelGGL((mv_f8_product_few_kernel<MT, NT, X, true>), dim3(cut[0].groups + cut[1].groups), threads, lds, st,
+            hipLaunchKernelGGL((mv_f8_product_few_kernel<MT, X, true>), dim3(cut[0].groups + cut[1].groups), threads, lds, st,
                                Launch<FewProduct<X>, true>{{p[0], p[1]}, cut[0].groups});
             return;
         }
     }
-    hipLaunchKernelGGL((mv_f8_product_few_kernel<MT, NT, X, false>), dim3(cut[0].groups), threads, lds, st,
+    hipLaunchKernelGGL((mv_f8_product_few_kernel<MT, X, false>), dim3(cut[0].groups), threads, lds, st,
                        Launch<FewProduct<X>, false>{{p[0]}, cut[0].groups});
 }
 template <typename X>
 static mv_status launch_few(const FewProduct<X>* p, const FewCut* cut, int n, hipStream_t st)
 {
-    if (cut[0].nt == 2) launch_few_of<1, 2>(p, cut, n, st);
-    else if (cut[0].mt == 1) launch_few_of<1, 1>(p, cut, n, st);
+    if (cut[0].mt == 1) launch_few_of<1>(p, cut, n, st);
     else if constexpr (!std::is_same_v<X, uint8_t>) {                   // codes: up to 16 rows only
-        if (cut[0].mt == 2) launch_few_of<2, 1>(p, cut, n, st);
-        else launch_few_of<4, 1>(p, cut, n, st);
+        if (cut[0].mt == 2) launch_few_of<2>(p, cut, n, st);
+        else launch_few_of<4>(p, cut, n, st);
     }
     return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
 }
@@ -803,7 +777,7 @@ static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
         few[i] = few_codes_cut(w[i], few_a[i]);
         if (few[i].mt) fp[i] = few_codes(w[i], few_a[i]);
     }
-    if (n == 2 && few[0].mt && few[0].mt == few[1].mt && few[0].nt == few[1].nt) return launch_few(fp, few, 2, st);
+    if (n == 2 && few[0].mt && few[1].mt) return launch_few(fp, few, 2, st);
     Cut  cut[2] = {};
     bool tiled[2] = {};
     for (int i = 0; i < n; ++i) {
