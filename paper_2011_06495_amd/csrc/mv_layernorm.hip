@@ -5,7 +5,8 @@
 //
 // Memory bounds both: a row is read once, into registers, and written once.  A workgroup takes row after row, with gamma and
 // beta (for the gradients: gamma, and the sums for dgamma and dbeta) of its threads' columns in registers, and the next row
-// on its way meanwhile.
+// on its way meanwhile.  16,384 x 8192 bf16 forward 101 us, 5.3 TB/s, fp32 198, 5.4; backward 162 and 298, 5.0 and 5.4, the
+// join of the workgroups' sums (4 to 5 us) among them.
 //
 // The mean is formed first and the squares are those of the differences from it; what the mean's own rounding left over,
 // the differences' mean, is taken off them and out of the variance, so rows far from zero keep their digits.
@@ -64,11 +65,14 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) void mv_layernorm_kernel(Forward
     const int64_t step = (int64_t)gridDim.x * kRows;
     fetch(row);
     for (int64_t first = (int64_t)blockIdx.x * kRows; first < f.rows; first += step, row += step) {
-        float v[C][V], sum = 0.0f;
+        Chunk<T> v[C];
+        float sum = 0.0f;
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+        for (int c = 0; c < C; ++c) {
+            v[c] = next[c];
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum += v[c][i] = next[c].at(i);
+            for (int i = 0; i < V; ++i) sum += v[c].at(i);
+        }
         fetch(row + step);
         const float mean = across.sum(sum) * share;
         float more = 0.0f, squares = 0.0f;
@@ -77,9 +81,9 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) void mv_layernorm_kernel(Forward
             const int64_t live = f.n - (int64_t)(c * LANES + t) * V;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                v[c][i] = i < live ? v[c][i] - mean : 0.0f;
-                more += v[c][i];
-                squares = __builtin_fmaf(v[c][i], v[c][i], squares);
+                const float off = i < live ? v[c].at(i) - mean : 0.0f;
+                more += off;
+                squares = __builtin_fmaf(off, off, squares);
             }
         }
         across.sum2(more, squares);
@@ -94,8 +98,9 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) void mv_layernorm_kernel(Forward
         for (int c = 0; c < C; ++c) {
             const int64_t col = (int64_t)(c * LANES + t) * V;
             float y[V];
+            v[c].forget();                               // as they came: their differences would take twice the registers
 #pragma unroll
-            for (int i = 0; i < V; ++i) y[i] = __builtin_fmaf((v[c][i] - more) * rstd, gamma[c][i], beta[c][i]);
+            for (int i = 0; i < V; ++i) y[i] = __builtin_fmaf(((v[c].at(i) - mean) - more) * rstd, gamma[c][i], beta[c][i]);
             f.y.store(row * f.ld_y + col, f.n - col, y);
         }
     }
@@ -194,22 +199,21 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) void mv_layernorm_grad_kernel(Ba
     for (int64_t first = (int64_t)blockIdx.x * kRows; first < b.rows; first += step, row += step) {
         const bool live_row = row < b.rows;
         const float mean = live_row ? b.mean[row] : 0.0f, rstd = live_row ? b.rstd[row] : 0.0f;
-        float h[C][V], d[C][V], along = 0.0f, both = 0.0f;
+        Chunk<T> vx[C], vdy[C];
+        float along = 0.0f, both = 0.0f;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int64_t live = live_row ? b.n - (int64_t)(c * LANES + t) * V : 0;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float g = next_dy[c].at(i);
-                h[c][i] = i < live ? (next_x[c].at(i) - mean) * rstd : 0.0f;
-                dgamma[c][i] = __builtin_fmaf(g, h[c][i], dgamma[c][i]);
-                dbeta[c][i] += g;
-                d[c][i] = g * gamma[c][i];
-                along += d[c][i];
-                both = __builtin_fmaf(d[c][i], h[c][i], both);
-            }
-        }
+        for (int c = 0; c < C; ++c) vx[c] = next_x[c], vdy[c] = next_dy[c];
         fetch(row + step);
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {                // dy is 0 where a row has ended
+                const float g = vdy[c].at(i), h = (vx[c].at(i) - mean) * rstd, d = g * gamma[c][i];
+                dgamma[c][i] = __builtin_fmaf(g, h, dgamma[c][i]);
+                dbeta[c][i] += g;
+                along += d;
+                both = __builtin_fmaf(d, h, both);
+            }
         if (!b.dx.p) continue;                                           // uniform
         across.sum2(along, both);
         along *= share, both *= share;
@@ -218,8 +222,12 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) void mv_layernorm_grad_kernel(Ba
         for (int c = 0; c < C; ++c) {
             const int64_t col = (int64_t)(c * LANES + t) * V;
             float dx[V];
+            vx[c].forget(), vdy[c].forget();             // as they came: h and d would take four times the registers
 #pragma unroll
-            for (int i = 0; i < V; ++i) dx[i] = rstd * __builtin_fmaf(-h[c][i], both, d[c][i] - along);
+            for (int i = 0; i < V; ++i) {
+                const float h = (vx[c].at(i) - mean) * rstd, d = vdy[c].at(i) * gamma[c][i];
+                dx[i] = rstd * __builtin_fmaf(-h, both, d - along);
+            }
             b.dx.store(row * b.ld_dx + col, b.n - col, dx);
         }
     }
@@ -355,18 +363,19 @@ __global__ __launch_bounds__(256) void mv_layernorm_join_kernel(const float* __r
     }
 }
 
-// How a row is held: LANES threads with C chunks each, or 0: not at all.  Four chunks of bf16 are 32 columns: with their weights
-// (gradients: two chunks, with their sums) more than the 128 registers that a thread of 1024 has.
+// How a row is held: LANES threads with up to `values` of its values each, or 0: not at all.  Forward, sixteen values a thread are
+// as fast as eight, or faster (bf16 16,384 x 8192 102 us, by twice the threads 144).  With the sums for the weights eight
+// are (16,384 x 4096 83, with sixteen 90), and rows beyond 8192 do not fit: 1024 threads with sixteen values each leave
+// registers (8192 x 16,384 bf16 369 us, fp32 861; read twice from memory 276 and 499).
 struct Held {
-    int lanes, chunks;
+    int lanes, values;
 };
-static Held held_of(int64_t n, int32_t dtype, bool grad)
+static Held held_of(int64_t n, bool grad)
 {
-    const int64_t wide = dtype == MV_BF16 ? 8 : 4, chunks = (n + wide - 1) / wide;
-    const int most[3] = {2, grad ? 2 : 4, (grad ? 2 : 4) / (dtype == MV_BF16 ? 2 : 1)};
-    for (int i = 0; i < 3; ++i)
-        for (int c = 1; c <= most[i]; c *= 2)
-            if (chunks <= ((int64_t)64 << (2 * i)) * c) return {64 << (2 * i), c};
+    if (n <= 64 * 16) return {64, n <= 64 * 8 ? 8 : 16};
+    for (int lanes : {256, 512, 1024})
+        for (int values : {8, 16})
+            if (n <= lanes * values && (values == 8 || !grad)) return {lanes, values};
     return {0, 0};
 }
 
@@ -374,45 +383,64 @@ template <typename T, int LANES, int C>
 static void forward_of(const Forward& f, hipStream_t st)
 {
     constexpr int kRows = kThreadsOf<LANES> / LANES;
-    const int64_t groups = (f.rows + kRows - 1) / kRows, most = LANES == 1024 ? 512 : 2048;
+    const int64_t groups = (f.rows + kRows - 1) / kRows, most = 2048 * 256 / kThreadsOf<LANES>;
     hipLaunchKernelGGL((mv_layernorm_kernel<T, LANES, C>), dim3((uint32_t)(groups < most ? groups : most)), dim3(kThreadsOf<LANES>), 0, st, f);
 }
 template <typename T>
 static void forward(const Forward& f, const Held& h, hipStream_t st)
 {
-    if (h.lanes == 64) h.chunks == 1 ? forward_of<T, 64, 1>(f, st) : forward_of<T, 64, 2>(f, st);
-    else if (h.lanes == 256)
-        h.chunks == 1 ? forward_of<T, 256, 1>(f, st) : h.chunks == 2 ? forward_of<T, 256, 2>(f, st) : forward_of<T, 256, 4>(f, st);
-    else if (h.lanes == 1024)
-        h.chunks == 1 ? forward_of<T, 1024, 1>(f, st) : h.chunks == 2 ? forward_of<T, 1024, 2>(f, st) : forward_of<float, 1024, 4>(f, st);
-    else
-        hipLaunchKernelGGL(mv_layernorm_long_kernel<T>, dim3((uint32_t)(f.rows < 512 ? f.rows : 512)), dim3(kLongThreads), 0, st, f);
+    constexpr int C = 8 / kChunk<T>;
+    switch (h.lanes + h.values) {
+    case 64 + 8: return forward_of<T, 64, C>(f, st);
+    case 64 + 16: return forward_of<T, 64, 2 * C>(f, st);
+    case 256 + 8: return forward_of<T, 256, C>(f, st);
+    case 256 + 16: return forward_of<T, 256, 2 * C>(f, st);
+    case 512 + 8: return forward_of<T, 512, C>(f, st);
+    case 512 + 16: return forward_of<T, 512, 2 * C>(f, st);
+    case 1024 + 8: return forward_of<T, 1024, C>(f, st);
+    case 1024 + 16: return forward_of<T, 1024, 2 * C>(f, st);
+    }
+    hipLaunchKernelGGL(mv_layernorm_long_kernel<T>, dim3((uint32_t)(f.rows < 512 ? f.rows : 512)), dim3(kLongThreads), 0, st, f);
 }
 
-constexpr int64_t kMostParts = 512;
+// Workgroups of the gradients' kernel, each with a part of the weights' sums to be joined: what runs at once, and at least two rows
+// each where that leaves 256.  us with 256, 512, 768: bf16 32,768 x 2048 184, 104, 82; 16,384 x 4096 103, 83, 96; 16,384 x 8192
+// 164, 169, 176; 300 x 8192 15, 19, 19; fp32 32,768 x 2048 208, 145, 152; 16,384 x 768 42, 38, 45; 2000 x 512 10.8, 12.0, 11.9.
+constexpr int64_t kMostParts = 768, kLeastParts = 256;
 inline int64_t pitch_of(int64_t n) { return (n + 3) / 4 * 4; }
-// Workgroups of the gradients' kernel, at most: a part each.
-inline int64_t parts_of(int64_t rows) { return rows < kMostParts ? rows : kMostParts; }
-inline size_t  parts_bytes(int64_t rows, int64_t n) { return (size_t)parts_of(rows) * 2 * (size_t)pitch_of(n) * 4; }
+static int64_t parts_of(int64_t rows, const Held& h, bool bf16)
+{
+    const int64_t groups = h.lanes == 64 ? (rows + 3) / 4 : rows, most = h.lanes == 1024 ? 256 : h.lanes == 256 && bf16 ? kMostParts : 512;
+    int64_t parts = groups / 2 < kLeastParts ? kLeastParts : groups / 2;
+    if (parts > most) parts = most;
+    return parts < groups ? parts : groups;
+}
+inline size_t parts_bytes(int64_t rows, int64_t n)
+{
+    return (size_t)(rows < kMostParts ? rows : kMostParts) * 2 * (size_t)pitch_of(n) * 4;
+}
 
 template <typename T, int LANES, int C>
-static uint32_t backward_of(const Backward& b, hipStream_t st)
+static uint32_t backward_of(const Backward& b, const Held& h, hipStream_t st)
 {
-    constexpr int kRows = kThreadsOf<LANES> / LANES;
-    const int64_t groups = (b.rows + kRows - 1) / kRows;
-    const uint32_t grid = (uint32_t)(groups < kMostParts ? groups : kMostParts);
+    const uint32_t grid = (uint32_t)parts_of(b.rows, h, sizeof(T) == 2);
     hipLaunchKernelGGL((mv_layernorm_grad_kernel<T, LANES, C>), dim3(grid), dim3(kThreadsOf<LANES>), 0, st, b);
     return grid;
 }
 template <typename T>
 static uint32_t backward(const Backward& b, const Held& h, hipStream_t st)               // returns how many parts there are
 {
-    if (h.lanes == 64) return h.chunks == 1 ? backward_of<T, 64, 1>(b, st) : backward_of<T, 64, 2>(b, st);
-    if (h.lanes == 256) return h.chunks == 1 ? backward_of<T, 256, 1>(b, st) : backward_of<T, 256, 2>(b, st);
-    if (h.lanes == 1024) return h.chunks == 1 ? backward_of<T, 1024, 1>(b, st) : backward_of<float, 1024, 2>(b, st);
+    constexpr int C = 8 / kChunk<T>;
+    switch (h.lanes + h.values) {
+    case 64 + 8: return backward_of<T, 64, C>(b, h, st);
+    case 64 + 16: return backward_of<T, 64, 2 * C>(b, h, st);
+    case 256 + 8: return backward_of<T, 256, C>(b, h, st);
+    case 512 + 8: return backward_of<T, 512, C>(b, h, st);
+    case 1024 + 8: return backward_of<T, 1024, C>(b, h, st);
+    }
     if (b.dx.p)
         hipLaunchKernelGGL(mv_layernorm_grad_sums_kernel<T>, dim3((uint32_t)(b.rows < 512 ? b.rows : 512)), dim3(kLongThreads), 0, st, b);
-    const int64_t tiles = (b.n + kColumnThreads * kChunk<T> - 1) / (kColumnThreads * kChunk<T>), most = tiles < 64 ? kMostParts / 8 : 8;
+    const int64_t tiles = (b.n + kColumnThreads * kChunk<T> - 1) / (kColumnThreads * kChunk<T>), most = tiles < 64 ? 64 : 8;
     const uint32_t deep = (uint32_t)(b.rows < most ? b.rows : most);
     hipLaunchKernelGGL(mv_layernorm_grad_columns_kernel<T>, dim3((uint32_t)tiles, deep), dim3(kColumnThreads), 0, st, b);
     return deep;
@@ -436,7 +464,7 @@ mv_status mv_layernorm_forward(const void* x, int32_t x_dtype, int64_t ld_x, int
         return MV_ERR_INVALID_ARG;
     const uint32_t bf16 = weight_dtype == MV_BF16;
     const Forward f = {x, ld_x, rows, n, {gamma, bf16}, {beta, bf16}, eps, {y, y_dtype == MV_BF16}, ld_y, mean, rstd};
-    const Held h = held_of(n, x_dtype, false);
+    const Held h = held_of(n, false);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (x_dtype == MV_BF16) forward<uint16_t>(f, h, st);
     else forward<float>(f, h, st);
@@ -464,7 +492,7 @@ mv_status mv_layernorm_backward(const void* x, int64_t ld_x, const void* dy, int
     float* parts = dgamma || dbeta ? reinterpret_cast<float*>(static_cast<char*>(scratch) + sums) : nullptr;
     const Backward b = {x, dy, ld_x, ld_dy, rows, n, {gamma, weight_dtype == MV_BF16}, mean, rstd, {dx, dx_dtype == MV_BF16}, ld_dx,
                         parts, pitch_of(n), static_cast<float*>(scratch)};
-    const Held h = held_of(n, dtype, true);
+    const Held h = held_of(n, true);
     hipStream_t st = static_cast<hipStream_t>(stream);
     const uint32_t count = dtype == MV_BF16 ? backward<uint16_t>(b, h, st) : backward<float>(b, h, st);
     if (parts) {
