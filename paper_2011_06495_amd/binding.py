@@ -406,12 +406,14 @@ def mv_quant_decode(streams, n: int, q: int, means, out, stream=None) -> None:
 # ---- gradient norm over many tensors, and clipping ---------------------------------
 
 _dtypes = None      # torch.float32 and torch.bfloat16 to mv_dtype, once torch is there
+_int32 = None       # torch.int32, set with them
 
 
 def _types():
-    global _dtypes
+    global _dtypes, _int32
     if _dtypes is None:
         import torch
+        _int32 = torch.int32
         _dtypes = {torch.float32: MV_F32, torch.bfloat16: MV_BF16}
     return _dtypes
 
@@ -428,7 +430,7 @@ def _float32(t, what: str, numel: int, device: int) -> int:
     """Address of a contiguous float32 device tensor of at least numel values; 0 for None."""
     if t is None:
         return 0
-    if _value_type(t, what) != MV_F32 or not t.is_contiguous() or t.numel() < numel or t.get_device() != device:
+    if (_dtypes or _types()).get(t.dtype) != MV_F32 or not t.is_contiguous() or t.numel() < numel or t.get_device() != device:
         raise ValueError("%s has to be contiguous float32 of %d values or more on the same GPU" % (what, numel))
     return t.data_ptr()
 
@@ -832,16 +834,15 @@ def mv_f8_linear_grad(x, dy, wt_codes, wt_scales, dx, dw, scratch, stream=None) 
 
 def _weights(a, b, n: int, device: int):
     """(address of gamma, address of beta, mv_dtype) of float32 or bfloat16 vectors of one type, either may be None."""
-    d, at = None, []
-    for t, what in ((a, "gamma"), (b, "beta")):
-        if t is None:
-            at.append(0)
-            continue
-        kind = _value_type(t, what)
-        if t.numel() != n or not t.is_contiguous() or t.get_device() != device or (d is not None and kind != d):
-            raise ValueError("%s has to be %d contiguous values on the same GPU, of the other weights' type" % (what, n))
-        d = kind
-        at.append(t.data_ptr())
+    kinds, d, at = _dtypes or _types(), None, [0, 0]
+    for i, t in enumerate((a, b)):
+        if t is not None:
+            kind = kinds.get(t.dtype)
+            if kind is None or t.numel() != n or not t.is_contiguous() or t.get_device() != device or (d is not None and kind != d):
+                raise ValueError("%s has to be %d contiguous float32 or bfloat16 values on the same GPU, of the other weights' type"
+                                 % (("gamma", "beta")[i], n))
+            d = kind
+            at[i] = t.data_ptr()
     return at[0], at[1], MV_F32 if d is None else d
 
 
@@ -852,9 +853,9 @@ def mv_layernorm_forward(x, gamma, beta, eps: float, out, mean=None, rstd=None, 
     device = x.get_device()
     a, xd, ld_x = _matrix(x, "x", rows, n, device)
     o, od, ld_o = _matrix(out, "out", rows, n, device)
-    st = (_lib or load()).mv_layernorm_forward(a, xd, ld_x, rows, n, *_weights(gamma, beta, n, device), eps, o, od, ld_o,
-                                               _float32(mean, "mean", rows, device), _float32(rstd, "rstd", rows, device),
-                                               _stream_handle(stream, x))
+    g, b, wd = _weights(gamma, beta, n, device)
+    st = (_lib or load()).mv_layernorm_forward(a, xd, ld_x, rows, n, g, b, wd, eps, o, od, ld_o, _float32(mean, "mean", rows, device),
+                                               _float32(rstd, "rstd", rows, device), _stream_handle(stream, x))
     if st != MV_OK:
         raise MvError(st, "mv_layernorm_forward")
 
@@ -885,27 +886,23 @@ def mv_layernorm_backward(x, dy, gamma, mean, rstd, dx, dgamma, dbeta, scratch, 
 # ---- distillation from a teacher's top logits ---------------------------------
 
 
-def _int32(t, what: str, shape, device: int) -> int:
-    """Address of an int32 tensor of this shape on the GPU whose last dimension lies in one piece; 0 for None."""
-    if t is None:
-        return 0
-    if t.dtype.itemsize != 4 or t.dtype.is_floating_point or tuple(t.shape) != shape or t.get_device() != device or (
-            shape[-1] > 1 and t.stride(-1) != 1):
-        raise ValueError("%s has to be int32 of shape %s on the same GPU, its rows in one piece" % (what, shape))
-    return t.data_ptr()
-
-
-def _listed(logits, idx, top, labels):
-    """The arguments that both calls begin with, up to the labels, and the GPU."""
-    rows, n = logits.shape
-    device = logits.get_device()
-    z, zd, ld_z = _matrix(logits, "logits", rows, n, device)
-    i, ld_i, t, td, ld_t, k = 0, 0, 0, 0, 0, 0
-    if idx is not None and idx.shape[1] > 0:
-        k = idx.shape[1]
-        i, ld_i = _int32(idx, "idx", (rows, k), device), idx.stride(0) if rows > 1 else max(idx.stride(0), k)
-        t, td, ld_t = _matrix(top, "top", rows, k, device)
-    return (z, zd, ld_z, rows, n, i, ld_i, t, td, ld_t, k, _int32(labels, "labels", (rows,), device)), device
+def _list(idx, top, labels, rows: int, device: int):
+    """(address and row stride of the coordinates; address, mv_dtype and row stride of the teacher's logits; entries of a row;
+    address of the labels)."""
+    i, ld_i, t, td, ld_t, k, at = 0, 0, 0, 0, 0, 0, 0
+    if idx is not None:
+        r, k = idx.shape
+        ld_i, step = idx.stride()
+        if r != rows or idx.dtype != _int32 or (k > 1 and step != 1) or idx.get_device() != device:
+            raise ValueError("idx has to be %d rows of int32 on the same GPU, each in one piece" % rows)
+        if k:
+            i, ld_i = idx.data_ptr(), ld_i if rows > 1 else max(ld_i, k)
+            t, td, ld_t = _matrix(top, "top", rows, k, device)
+    if labels is not None:
+        if labels.dtype != _int32 or labels.numel() != rows or not labels.is_contiguous() or labels.get_device() != device:
+            raise ValueError("labels have to be %d contiguous int32 on the same GPU" % rows)
+        at = labels.data_ptr()
+    return i, ld_i, t, td, ld_t, k, at
 
 
 def mv_distill_scratch_bytes(rows: int, n: int) -> int:
@@ -918,22 +915,26 @@ def mv_distill_loss(logits, idx, top, labels, temperature: float, soft: float, h
     coordinates (rows x k int32, any other than 0 .. n-1 is no entry) and logits (rows x k float32 or bfloat16), or both None;
     labels: rows int32 or None; stats: rows x 3 float32 (out) or None, for mv_distill_grad; dz: rows x n (out; may be logits)
     or None, with grad, rows float32, the gradients that arrive at the losses, None for 1."""
-    at, device = _listed(logits, idx, top, labels)
-    rows, n = at[3], at[4]
+    rows, n = logits.shape
+    device = logits.get_device()
+    z, zd, ld_z = _matrix(logits, "logits", rows, n, device)
     o, od, ld_o = _matrix(dz, "dz", rows, n, device) if dz is not None else (0, 0, 0)
-    st = (_lib or load()).mv_distill_loss(*at, temperature, soft, hard, _float32(loss, "loss", rows, device),
-                                          _float32(stats, "stats", 3 * rows, device), _float32(grad, "grad", rows, device), o, od, ld_o,
-                                          *_scratch_of(scratch, device), _stream_handle(stream, logits))
+    c, size = _scratch_of(scratch, device)
+    st = (_lib or load()).mv_distill_loss(z, zd, ld_z, rows, n, *_list(idx, top, labels, rows, device), temperature, soft, hard,
+                                          _float32(loss, "loss", rows, device), _float32(stats, "stats", 3 * rows, device),
+                                          _float32(grad, "grad", rows, device), o, od, ld_o, c, size, _stream_handle(stream, logits))
     if st != MV_OK:
         raise MvError(st, "mv_distill_loss")
 
 
 def mv_distill_grad(logits, idx, top, labels, temperature: float, soft: float, hard: float, stats, dz, grad=None, stream=None) -> None:
     """dz of mv_distill_loss from the stats of a call with the same arguments."""
-    at, device = _listed(logits, idx, top, labels)
-    rows, n = at[3], at[4]
+    rows, n = logits.shape
+    device = logits.get_device()
+    z, zd, ld_z = _matrix(logits, "logits", rows, n, device)
     o, od, ld_o = _matrix(dz, "dz", rows, n, device)
-    st = (_lib or load()).mv_distill_grad(*at, temperature, soft, hard, _float32(stats, "stats", 3 * rows, device),
-                                          _float32(grad, "grad", rows, device), o, od, ld_o, _stream_handle(stream, logits))
+    st = (_lib or load()).mv_distill_grad(z, zd, ld_z, rows, n, *_list(idx, top, labels, rows, device), temperature, soft, hard,
+                                          _float32(stats, "stats", 3 * rows, device), _float32(grad, "grad", rows, device), o, od, ld_o,
+                                          _stream_handle(stream, logits))
     if st != MV_OK:
         raise MvError(st, "mv_distill_grad")

@@ -21,7 +21,9 @@ def test_sizes(lib):
     for f in (B.mv_layernorm_scratch_bytes, B.mv_distill_scratch_bytes):
         assert f(0, 1) == 0 and f(1, 1 << 31) == 0 and f(-1, 5) == 0
     assert B.mv_layernorm_scratch_bytes(1, 1) > 0
-    assert B.mv_distill_scratch_bytes(1000, 65_536) == 0 and B.mv_distill_scratch_bytes(1000, 65_537) > 0
+    # neither cut into ranges nor too long to be held
+    assert B.mv_distill_scratch_bytes(5000, 65_536) == 0 and B.mv_distill_scratch_bytes(1, 16_384) == 0
+    assert B.mv_distill_scratch_bytes(1, 16_385) > 0 and B.mv_distill_scratch_bytes(5000, 70_000) > 0
 
 
 # every call with good arguments by name, in the order of the C declaration
