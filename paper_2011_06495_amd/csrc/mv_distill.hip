@@ -276,6 +276,9 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
     const List list = list_at(lds + mine * list_bytes(d.top), d.top);
     const int n = (int)d.n, full = n / (LANES * V), rest = n - full * (LANES * V) - (int)t * V;
     Chunk<T> held[C], tail;
+    // The first chunks of the next row are fetched into LDS while this one's are summed up; each wavefront reads its own again.
+    constexpr int kAhead = kWaves > 1 ? C / 2 : 0;
+    __shared__ __attribute__((aligned(16))) uint8_t ahead[kAhead ? kAhead * LANES * 16 : 16];
     // in one scalar comparison each time, not in sixteen masks that are kept
     auto there = [&](int c) {
         int f = full;
@@ -303,11 +306,19 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
             if (there(c)) most.look(held[c]);
         float largest = wave_max(most.value());
         if (wave == 0) entry.look(row_at(row));
+        const bool more = row + step < d.rows;                           // behind the last row there is nothing
+        const RowOf next(row_at(more ? row + step : row), more ? full * (LANES * 16) : 0);
         if constexpr (kWaves > 1) {
             if ((t & 63u) == 0) tops[wave] = largest;
             __syncthreads();
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) largest = larger(tops[w], largest);
+        }
+        // between the two barriers, which wait for them
+        if constexpr (kAhead > 0) {
+            __builtin_amdgcn_s_waitcnt(kNoLds);                          // what was read of the last ones is here
+#pragma unroll
+            for (int c = 0; c < kAhead; ++c) next.load_lds(ahead + (c * kWaves + wave) * 1024, t * 16, c * (LANES * 16));
         }
         float a = 0.0f, b = 0.0f;
         add_up<T, TERMS>(tail, largest, d.scale, a, b);
@@ -338,9 +349,7 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
             }
         }
         const Weights weights = weights_of<TERMS>(d, w.soft, w.label, d.grad ? d.grad[row] : 1.0f, largest, a, b);
-        // each chunk's registers take the next row's as soon as its own is written; behind the last row there is nothing
-        const bool more = row + step < d.rows;
-        const RowOf next(row_at(more ? row + step : row), more ? full * (LANES * 16) : 0);
+        // each chunk's registers take the next row's as soon as its own is written
         const RowOf dz(static_cast<char*>(d.dz.p) + row * d.ld_dz * (d.dz.bf16 ? 2 : 4), d.dz.p ? full * (LANES * V) * (d.dz.bf16 ? 2 : 4) : 0);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -350,7 +359,8 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
                 plain_grad<T, TERMS>(held[c], weights, d.scale, y);
                 dz.store<LANES>(y, t, c, d.dz.bf16);
             }
-            held[c].take(next.load(t * 16, c * (LANES * 16)));
+            if (c < kAhead) held[c].take(*reinterpret_cast<const u32x4*>(ahead + (c * kWaves + wave) * 1024 + (t & 63u) * 16));
+            else held[c].take(next.load(t * 16, c * (LANES * 16)));
         }
         if (d.dz.p) {
             float y[V];

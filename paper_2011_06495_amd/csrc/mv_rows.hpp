@@ -11,6 +11,7 @@ using mvx::u32x4;
 using mvx::values_valid;
 
 constexpr float kInf = __builtin_inff();
+constexpr int   kNoLds = 0xC07F;        // s_waitcnt: no LDS access in flight
 constexpr int   kNoLoads = 0x0F70;      // s_waitcnt: none of the vector loads in flight, the other counters as they are
 
 // A row is LANES threads' (64, 256 or 1024); thread t has chunks t, t + LANES, ... of 16 bytes.
@@ -142,9 +143,16 @@ struct RowOf {
     {
         return __builtin_amdgcn_raw_buffer_load_b128(buf, mine, all, 0);
     }
+    // 1024 bytes of a wavefront straight into LDS.
+    __device__ __forceinline__ void load_lds(uint8_t* to, uint32_t mine, uint32_t all) const
+    {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void*)to, 16, mine, all, 0, 0);
+    }
+    // Past the caches.  The whole offset is the lane's: of a store with a shared one in a scalar register the compiler (hipcc 7.2)
+    // takes the data as read at once, and the next instruction may write over it; addresses have turned up in place of values.
     __device__ __forceinline__ void store(const u32x4& w, uint32_t mine, uint32_t all) const
     {
-        __builtin_amdgcn_raw_buffer_store_b128(w, buf, mine, all, 2);    // past the caches
+        __builtin_amdgcn_raw_buffer_store_b128(w, buf, mine + all, 0, 2);
     }
     // V values at chunk `c` of LANES threads, fp32 or bf16.
     template <int LANES, int V>
@@ -161,7 +169,7 @@ struct RowOf {
             for (int i = 0; i < V / 2; ++i) w[i] = mvx::narrow(y[2 * i]) | mvx::narrow(y[2 * i + 1]) << 16;
             typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
             if constexpr (V == 8) store(u32x4{w[0], w[1], w[2], w[3]}, t * 16, c * (LANES * 16));
-            else __builtin_amdgcn_raw_buffer_store_b64(u32x2{w[0], w[1]}, buf, t * 8, c * (LANES * 8), 2);
+            else __builtin_amdgcn_raw_buffer_store_b64(u32x2{w[0], w[1]}, buf, t * 8 + c * (LANES * 8), 0, 2);
         }
     }
 };
