@@ -113,21 +113,34 @@ __device__ __forceinline__ void add_up(const Chunk<T>& c, float largest, float s
 
 // ---- the list ------------------------------------------------------------------------------------------------------
 
-// A row's list in LDS: coordinates, p, and the logits there; entry `room` is the label.
+// A row's list in LDS: coordinates, p (its sign set where another entry may name the same coordinate), and the logits there;
+// and a slot for each entry, where entries of one coordinate meet.
 struct List {
-    int32_t* idx;
-    float *  p, *z;
+    int32_t*  idx;
+    float *   p, *z;
+    uint16_t* slots;
+    uint32_t  many;                     // slots
 };
 __host__ __device__ constexpr uint32_t room_of(uint32_t top) { return (top + 3) / 4 * 4; }
-__host__ __device__ constexpr size_t   list_bytes(uint32_t top) { return (size_t)(room_of(top) + 4) * 12; }
+__host__ __device__ constexpr uint32_t slots_of(uint32_t top) { return room_of(top) * 16 < 8192 ? room_of(top) * 16 : 8192; }
+__host__ __device__ constexpr size_t   list_bytes(uint32_t top) { return (size_t)room_of(top) * 12 + slots_of(top) * 2; }
 __device__ __forceinline__ List list_at(void* lds, uint32_t top)
 {
-    const uint32_t each = room_of(top) + 4;
+    const uint32_t each = room_of(top);
     int32_t* idx = static_cast<int32_t*>(lds);
-    return {idx, reinterpret_cast<float*>(idx + each), reinterpret_cast<float*>(idx + 2 * each)};
+    return {idx, reinterpret_cast<float*>(idx + each), reinterpret_cast<float*>(idx + 2 * each), reinterpret_cast<uint16_t*>(idx + 3 * each),
+            slots_of(top)};
 }
+__device__ __forceinline__ uint32_t slot_of(const List& l, int32_t at) { return __umulhi((uint32_t)at * 0x9E3779B1u, l.many); }
+// The slot may hold what another lane has put there: LDS is in order within a wavefront, and the compiler does not know the place.
+__device__ __forceinline__ uint16_t& slot_again(const List& l, int32_t at) { return l.slots[fresh(slot_of(l, at))]; }
 
-// An entry of the list on its way.
+template <typename T>
+__device__ __forceinline__ float logit(const T* row, int32_t at)
+{
+    return sizeof(T) == 2 ? mvx::widen(reinterpret_cast<const uint16_t*>(row)[at]) : reinterpret_cast<const float*>(row)[at];
+}
+// An entry of the list on its way, or the label.
 struct Entry {
     int32_t at;                         // -1: none
     float   t, z;
@@ -137,17 +150,25 @@ struct Entry {
         if (j < d.top) {
             at = d.idx[row * d.ld_idx + j];
             t = d.t.at(row * d.ld_t + j);
-        } else if (j == room_of(d.top) && d.labels) {
-            at = d.labels[row];
         }
         if (at < 0 || at >= d.n) at = -1, t = -kInf;
     }
-    template <typename T>
-    __device__ __forceinline__ void look(const T* row)
+    __device__ __forceinline__ void name_label(const Distill& d, int64_t row)
     {
-        if (at >= 0) z = sizeof(T) == 2 ? mvx::widen(reinterpret_cast<const uint16_t*>(row)[at]) : reinterpret_cast<const float*>(row)[at];
+        at = __builtin_amdgcn_readfirstlane(d.labels ? d.labels[row] : -1), t = -kInf, z = 0.0f;    // a wavefront's row is one
+        if (at < 0 || at >= d.n) at = -1;
     }
-    __device__ __forceinline__ void keep(const List& l, uint32_t j) const { l.idx[j] = at, l.p[j] = t, l.z[j] = z; }
+    // With a range of coordinates only, logits elsewhere are not looked at.
+    template <typename T>
+    __device__ __forceinline__ void look(const T* row, int64_t from, int64_t to)
+    {
+        if (at >= from && at < to) z = logit(row, at);
+    }
+    __device__ __forceinline__ void keep(const List& l, uint32_t j) const
+    {
+        l.idx[j] = at, l.p[j] = t, l.z[j] = z;
+        if (at >= 0) l.slots[slot_of(l, at)] = (uint16_t)j;
+    }
 };
 
 // What a row's terms come to, but for the sums over its logits.
@@ -157,46 +178,55 @@ struct Terms {
     float   share;                      // sum p, as rounding has it
     float   label_z;
     int32_t label;                      // -1: none
+    bool    listed;                     // is the label's coordinate in the list, too
 };
 
-// A wavefront makes p of the list: `first` is its lanes' first entries, the others are fetched here.  With the rows of
-// coordinates [from, to) only, logits elsewhere are not looked at.
+// A wavefront makes p of the list: `first` is its lanes' first entries, the others are fetched here.  An entry that finds
+// another one in its slot marks it, and all entries of a marked slot are told apart where dz is written.
 template <typename T>
-__device__ __forceinline__ Terms take_list(const Distill& d, const List& l, int64_t row, const T* z, Entry first, float largest, int64_t from,
-                                           int64_t to)
+__device__ __forceinline__ Terms take_list(const Distill& d, const List& l, int64_t row, const T* z, Entry first, Entry label, float largest,
+                                           int64_t from, int64_t to)
 {
-    const uint32_t lane = fresh(threadIdx.x & 63u), all = room_of(d.top) + 1;
+    constexpr uint16_t kMarked = 0xFFFF;
+    const uint32_t lane = fresh(threadIdx.x & 63u);
     float most = first.t;
-    if (lane < all) first.keep(l, lane);
-    for (uint32_t j = lane + 64; j < all; j += 64) {
+    bool  listed = first.at == label.at;
+    if (lane < d.top) first.keep(l, lane);
+    for (uint32_t j = lane + 64; j < d.top; j += 64) {
         Entry e;
         e.name(d, row, j);
-        if (e.at >= from && e.at < to) e.look(z);
+        e.look(z, from, to);
         e.keep(l, j);
         most = fmaxf(most, e.t);
+        listed |= e.at == label.at;
     }
     most = wave_max(most);
     float sum = 0.0f;
     for (uint32_t j = lane; j < d.top; j += 64) {
-        const float v = l.p[j];
+        const float   v = l.p[j];
+        const int32_t at = l.idx[j];
         if (v != -kInf) sum += expf((v - most) * d.inv_t);               // NaN among them, or +infinity: NaN
+        if (at >= 0) {
+            uint16_t& slot = slot_again(l, at);
+            if (slot != j) slot = kMarked;
+        }
     }
     sum = wave_sum(sum);
     const float log_sum = logf(sum);
-    Terms w = {sum == 0.0f ? 0.0f : sum * 0.0f + 1.0f, 0.0f, 0.0f, 0.0f, -1};
-    for (uint32_t j = lane; j < all - 1; j += 64) {
-        const float v = l.p[j];
+    Terms w = {sum == 0.0f ? 0.0f : sum * 0.0f + 1.0f, 0.0f, 0.0f, label.z, label.at, __ballot(listed) != 0 && label.at >= 0};
+    for (uint32_t j = lane; j < d.top; j += 64) {
+        const float   v = l.p[j];
+        const int32_t at = l.idx[j];
         float p = 0.0f;
         if (v != -kInf) {
             const float log_p = (v - most) * d.inv_t - log_sum;
             p = expf(log_p);
             if (p != 0.0f) w.cross += p * (log_p - (l.z[j] - largest) * d.inv_t), w.share += p;
         }
-        l.p[j] = p;
+        const bool met = at >= 0 && slot_again(l, at) != j;
+        l.p[j] = __uint_as_float((__float_as_uint(p) & 0x7FFFFFFFu) | (met ? 0x80000000u : 0u));
     }
     w.cross = wave_sum(w.cross), w.share = wave_sum(w.share);
-    __builtin_amdgcn_wave_barrier();
-    w.label = l.idx[all - 1], w.label_z = l.z[all - 1];                  // another lane's: LDS is in order within a wavefront
     return w;
 }
 __device__ __forceinline__ float loss_of(const Distill& d, const Terms& w, float largest, float a, float b)
@@ -233,38 +263,52 @@ __device__ __forceinline__ void plain_grad(const Chunk<T>& c, const Weights& w, 
 // dz at what the list and the label name among the coordinates from `from` to `to` that this wavefront wrote before: chunks go
 // round THREADS threads.
 template <typename T, int THREADS, int TERMS>
-__device__ __forceinline__ void patch(const Distill& d, const List& l, const Weights& w, int64_t row, int32_t label, int64_t from, int64_t to)
+__device__ __forceinline__ void patch(const Distill& d, const List& l, const Weights& w, int64_t row, const Terms& terms, int64_t from,
+                                      int64_t to)
 {
-    typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-    const uint32_t lane = fresh(threadIdx.x & 63u), room = room_of(d.top);
+    const uint32_t lane = fresh(threadIdx.x & 63u);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x % THREADS / 64);
     if (!w.any) return;
-    for (uint32_t j = lane; j < room + 1; j += 64) {
-        const int32_t at = l.idx[j];
-        if (at < from || at >= to) continue;                             // none is -1
-        if ((uint32_t)(at - (int32_t)from) / (64 * kChunk<T>) % (THREADS / 64) != wave) continue;
-        float p = 0.0f;
-        bool  named = false;                                             // by an entry before
-        for (uint32_t i = 0; i < room; i += 4) {
-            const i32x4 other = *reinterpret_cast<const i32x4*>(l.idx + i);
-#pragma unroll
-            for (uint32_t e = 0; e < 4; ++e)
-                if (other[e] == at) {
-                    named |= i + e < j;
-                    p += l.p[i + e];
-                }
+    auto ours = [&](int32_t at) {                                        // none is -1
+        return at >= from && at < to && (uint32_t)(at - (int32_t)from) / (64 * kChunk<T>) % (THREADS / 64) == wave;
+    };
+    auto put = [&](int32_t at, float z, float p) {
+        const float off = d.soft_grad * p + (at == terms.label ? d.hard : 0.0f);
+        d.dz.put(row * d.ld_dz + at, w.of(Pair<TERMS>(z - w.largest, d.scale)) - w.g * off);
+    };
+    __builtin_amdgcn_s_waitcnt(kNoLoads);                                // the stores before, too: these are behind them
+    for (uint32_t j = lane; j - lane < d.top; j += 64) {
+        const int32_t at = j < d.top ? l.idx[j] : -1;
+        bool  write = ours(at);
+        float p = write ? l.p[j] : 0.0f;
+        // entries that share their slot, one by one: the first of a coordinate has the sum in the list's order
+        for (uint64_t met = __ballot(write && __float_as_uint(p) >> 31); met; met &= met - 1) {
+            const int     whose = __builtin_ctzll(met);
+            const int32_t name = __builtin_amdgcn_readlane(at, whose);
+            uint32_t first = d.top;
+            float    sum = 0.0f;
+            for (uint32_t i = 0; i < d.top; i += 64) {
+                const bool same = i + lane < d.top && l.idx[i + lane] == name;
+                const float q = same ? l.p[i + lane] : 0.0f;
+                uint64_t hits = __ballot(same);
+                if (hits && first == d.top) first = i + __builtin_ctzll(hits);
+                for (; hits; hits &= hits - 1) sum += fabsf(lane_of(q, __builtin_ctzll(hits)));
+            }
+            if (lane == (uint32_t)whose) p = sum, write = first == j;
         }
-        if (named) continue;
-        const float off = d.soft_grad * p + (at == label ? d.hard : 0.0f);
-        d.dz.put(row * d.ld_dz + at, w.of(Pair<TERMS>(l.z[j] - w.largest, d.scale)) - w.g * off);
+        if (write) put(at, l.z[j], fabsf(p));
     }
+    if (!terms.listed && lane == 0 && ours(terms.label)) put(terms.label, terms.label_z, 0.0f);
 }
 
 // ---- a row in registers ------------------------------------------------------------------------------------------------
 
+// How many chunks of the next row a thread has in LDS beforehand.
+__host__ __device__ constexpr int ahead_of(int lanes, int chunks) { return lanes > 64 ? chunks / 2 : 0; }
+
 // LANES threads with up to C whole chunks each, and one that the row may end in.  With no more than a hundred registers
 // beside them: whole chunks come and go through buffers, and chunks that a row does not have are 0 and left out.
-template <typename T, int LANES, int C, int TERMS>
+template <typename T, int LANES, int C, int TERMS, bool AHEAD>
 __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distill d)
 {
     constexpr int V = kChunk<T>, kRows = kThreadsOf<LANES> / LANES, kWaves = LANES / 64;
@@ -277,7 +321,7 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
     const int n = (int)d.n, full = n / (LANES * V), rest = n - full * (LANES * V) - (int)t * V;
     Chunk<T> held[C], tail;
     // The first chunks of the next row are fetched into LDS while this one's are summed up; each wavefront reads its own again.
-    constexpr int kAhead = kWaves > 1 ? C / 2 : 0;
+    constexpr int kAhead = AHEAD ? ahead_of(LANES, C) : 0;
     __shared__ __attribute__((aligned(16))) uint8_t ahead[kAhead ? kAhead * LANES * 16 : 16];
     // in one scalar comparison each time, not in sixteen masks that are kept
     auto there = [&](int c) {
@@ -297,15 +341,15 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
         fetch_tail(row_at(row));
     }
     for (; row < d.rows; row += step) {
-        Entry entry;
-        if (wave == 0) entry.name(d, row, t);
+        Entry entry, label;
+        if (wave == 0) entry.name(d, row, t), label.name_label(d, row);
         Largest<T> most;
         most.look(tail);
 #pragma unroll
         for (int c = 0; c < C; ++c)
             if (there(c)) most.look(held[c]);
         float largest = wave_max(most.value());
-        if (wave == 0) entry.look(row_at(row));
+        if (wave == 0) entry.look(row_at(row), 0, d.n), label.look(row_at(row), 0, d.n);
         const bool more = row + step < d.rows;                           // behind the last row there is nothing
         const RowOf next(row_at(more ? row + step : row), more ? full * (LANES * 16) : 0);
         if constexpr (kWaves > 1) {
@@ -328,7 +372,7 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
         a = wave_sum(a);
         if (TERMS != kOne) b = wave_sum(b);
         Terms w;
-        if (wave == 0) w = take_list(d, list, row, row_at(row), entry, largest, 0, d.n);
+        if (wave == 0) w = take_list(d, list, row, row_at(row), entry, label, largest, 0, d.n);
         __builtin_amdgcn_s_waitcnt(kNoLoads);                            // dz may be z: all that is read of the row is here
         if constexpr (kWaves > 1) {
             if ((t & 63u) == 0) sums[0][wave] = a, sums[1][wave] = b;
@@ -366,7 +410,7 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
             float y[V];
             plain_grad<T, TERMS>(tail, weights, d.scale, y);
             d.dz.store(row * d.ld_dz + full * (LANES * V) + t * V, rest, y);
-            patch<T, LANES, TERMS>(d, list, weights, row, w.label, 0, d.n);
+            patch<T, LANES, TERMS>(d, list, weights, row, w, 0, d.n);
         }
         if (more) fetch_tail(row_at(row + step));
     }
@@ -436,10 +480,10 @@ __global__ __launch_bounds__(kStreamThreads) void mv_distill_loss_kernel(Distill
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     for (int64_t row = blockIdx.x; row < d.rows; row += gridDim.x) {
         const T* z = static_cast<const T*>(d.z) + row * d.ld_z;
-        Entry entry;
+        Entry entry, label;
         if (wave == 0 && d.loss) {
-            entry.name(d, row, threadIdx.x);
-            entry.look(z);
+            entry.name(d, row, threadIdx.x), label.name_label(d, row);
+            entry.look(z, 0, d.n), label.look(z, 0, d.n);
         }
         float largest, a, b;
         stream<T, TERMS>(z, 0, d.n, d.scale, largest, a, b);
@@ -448,7 +492,7 @@ __global__ __launch_bounds__(kStreamThreads) void mv_distill_loss_kernel(Distill
         if (largest == -kInf) a = b = __builtin_nanf("");
         if (wave == 0) {
             if (d.loss) {
-                const Terms w = take_list(d, list, row, z, entry, largest, 0, d.n);
+                const Terms w = take_list(d, list, row, z, entry, label, largest, 0, d.n);
                 if (threadIdx.x == 0) d.loss[row] = loss_of(d, w, largest, a, b);
             }
             if (threadIdx.x == 0 && d.stats) {
@@ -487,10 +531,10 @@ __global__ __launch_bounds__(64) void mv_distill_join_kernel(Distill d)
     const List list = list_at(lds, d.top);
     for (int64_t row = blockIdx.x; row < d.rows; row += gridDim.x) {
         const T* z = static_cast<const T*>(d.z) + row * d.ld_z;
-        Entry entry;
+        Entry entry, label;
         if (d.loss) {
-            entry.name(d, row, threadIdx.x);
-            entry.look(z);
+            entry.name(d, row, threadIdx.x), label.name_label(d, row);
+            entry.look(z, 0, d.n), label.look(z, 0, d.n);
         }
         const float* part = d.parts + 4 * row * d.ranges;
         float largest = -kInf, a = 0.0f, b = 0.0f;
@@ -503,7 +547,7 @@ __global__ __launch_bounds__(64) void mv_distill_join_kernel(Distill d)
         }
         a = wave_sum(a), b = wave_sum(b);
         if (d.loss) {
-            const Terms w = take_list(d, list, row, z, entry, largest, 0, d.n);
+            const Terms w = take_list(d, list, row, z, entry, label, largest, 0, d.n);
             if (threadIdx.x == 0) d.loss[row] = loss_of(d, w, largest, a, b);
         }
         if (threadIdx.x == 0 && d.stats) {
@@ -531,16 +575,16 @@ __global__ __launch_bounds__(kStreamThreads) void mv_distill_grad_kernel(Distill
         const float* had = d.had + 3 * row;
         const float largest = had[0];
         if (wave == 0) {
-            Entry entry;
-            entry.name(d, row, threadIdx.x);
-            if (entry.at >= first && entry.at < last) entry.look(z);     // logits elsewhere may have been written over
-            const Terms w = take_list(d, list, row, z, entry, largest, first, last);
+            Entry entry, label;                                          // logits elsewhere may have been written over
+            entry.name(d, row, threadIdx.x), label.name_label(d, row);
+            entry.look(z, first, last), label.look(z, first, last);
+            const Terms w = take_list(d, list, row, z, entry, label, largest, first, last);
             if (threadIdx.x == 0) shared = w;
             __builtin_amdgcn_s_waitcnt(kNoLoads);                        // dz may be z: the list's logits are here
         }
         __syncthreads();
-        const Weights w = weights_of<TERMS>(d, shared.soft, shared.label, d.grad ? d.grad[row] : 1.0f, largest, had[1], had[2]);
-        const int32_t label = shared.label;
+        const Terms   terms = shared;
+        const Weights w = weights_of<TERMS>(d, terms.soft, terms.label, d.grad ? d.grad[row] : 1.0f, largest, had[1], had[2]);
         for (int64_t col = first; col < last; col += kTurn) {
             Chunk<T> c[G];
             int live[G];
@@ -557,7 +601,7 @@ __global__ __launch_bounds__(kStreamThreads) void mv_distill_grad_kernel(Distill
                 d.dz.store(row * d.ld_dz + col + threadIdx.x * V + g * (kStreamThreads * V), live[g], y);
             }
         }
-        patch<T, kStreamThreads, TERMS>(d, list, w, row, label, first, last);
+        patch<T, kStreamThreads, TERMS>(d, list, w, row, terms, first, last);
         __syncthreads();                                                 // the list and the terms are read before the next ones
     }
 }
@@ -566,8 +610,11 @@ __global__ __launch_bounds__(kStreamThreads) void mv_distill_grad_kernel(Distill
 struct Lanes {
     int lanes, chunks;
 };
-static Lanes lanes_of(int64_t n, int32_t dtype, int64_t top)
+static Lanes lanes_of(int64_t rows, int64_t n, int32_t dtype, int64_t top)
 {
+    // A few long rows are cut into ranges, for a workgroup each in three launches: 1 x 131,072 bf16 23 -> 15 us, 48 rows 25 -> 18, of
+    // 72,000 1 16 -> 15 and 48 17 -> 16; but 128 rows 29 -> 28 and 18 -> 22, of 33,000 1 12.5 -> 14.
+    if (rows <= 48 && n > 65536) return {0, 0};
     const int64_t wide = dtype == MV_BF16 ? 8 : 4, chunks = n / wide;
     if (chunks < 64 * 4 && top <= 1024) return {64, 4};                  // four rows' lists in one workgroup's LDS: 48 KB
     for (int lanes : {256, 512, 1024})
@@ -595,8 +642,16 @@ static void held(const Distill& d, hipStream_t st)
 {
     constexpr int kRows = kThreadsOf<LANES> / LANES;
     // as many as run at once, sixteen wavefronts to a unit
-    hipLaunchKernelGGL((mv_distill_kernel<T, LANES, C, TERMS>), dim3(grid_of((d.rows + kRows - 1) / kRows, 256 * 1024 / kThreadsOf<LANES>)),
-                       dim3(kThreadsOf<LANES>), kRows * list_bytes(d.top), st, d);
+    const dim3   grid(grid_of((d.rows + kRows - 1) / kRows, 256 * 1024 / kThreadsOf<LANES>)), group(kThreadsOf<LANES>);
+    const size_t lists = kRows * list_bytes(d.top);
+    // the longest rows' longest lists need the LDS that the next row would have: 160 KB less what the kernel's own variables take
+    if constexpr (ahead_of(LANES, C) * LANES * 16 + list_bytes(kMostTop) > 159 * 1024) {
+        if (ahead_of(LANES, C) * LANES * 16 + lists > 159 * 1024) {
+            hipLaunchKernelGGL((mv_distill_kernel<T, LANES, C, TERMS, false>), grid, group, lists, st, d);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((mv_distill_kernel<T, LANES, C, TERMS, true>), grid, group, lists, st, d);
 }
 template <typename T, int TERMS>
 static void grad(Distill d, hipStream_t st)
@@ -671,7 +726,7 @@ size_t mv_distill_scratch_bytes(int64_t rows, int64_t n)
     using namespace mvr;
     if (!size_valid(rows) || !size_valid(n)) return 0;
     // what is cut into ranges, and what no type's rows of are held
-    return ranges_of(rows, n).count > 1 || !lanes_of(n, MV_F32, 0).lanes ? parts_bytes(rows, n) + stats_bytes(rows) : 0;
+    return ranges_of(rows, n).count > 1 || !lanes_of(rows, n, MV_F32, 0).lanes ? parts_bytes(rows, n) + stats_bytes(rows) : 0;
 }
 
 mv_status mv_distill_loss(const void* logits, int32_t dtype, int64_t ld_z, int64_t rows, int64_t n, const int32_t* idx, int64_t ld_idx,
@@ -687,7 +742,7 @@ mv_status mv_distill_loss(const void* logits, int32_t dtype, int64_t ld_z, int64
     const size_t need = mv_distill_scratch_bytes(rows, n);
     if (need && (!scratch || scratch_bytes < need || (reinterpret_cast<uintptr_t>(scratch) & 15))) return MV_ERR_INVALID_ARG;
     d.loss = loss, d.stats = stats;
-    const Lanes l = lanes_of(n, dtype, d.top);
+    const Lanes l = lanes_of(rows, n, dtype, d.top);
     if (need) {
         d.parts = static_cast<float*>(scratch);
         if (!stats && !l.lanes) d.stats = reinterpret_cast<float*>(static_cast<char*>(scratch) + parts_bytes(rows, n));

@@ -230,12 +230,28 @@ def test_in_place(n, src):
     assert torch.equal(d, dz)
 
 
-@pytest.mark.parametrize("rows,n,top", [(3, 30, 4096), (2, 5000, 4096), (5, 1000, 1025), (2, 140_000, 3000)])
-def test_long_lists(rows, n, top):
-    z, idx, t, label = make(rows, n, top, "f32", top)
+@pytest.mark.parametrize("src", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n,top", [(4200, 70, 5), (1100, 1500, 30), (1030, 2100, 70), (520, 20_001, 9), (300, 36_001, 5), (270, 69_700, 40)])
+def test_more_rows_than_run_at_once(rows, n, top, src):
+    """Rows that take turns in a workgroup, each fetched while the one before is at work; in place."""
+    z, idx, t, label = make(rows, n, top, src, rows + n)
+    ref = reference(z, idx, t, label, 2.0, 0.6, 0.4, None)
+    loss, d, dz = torch.zeros(rows, device="cuda"), place(z, TYPES[src], 1, 3), torch.zeros((rows, n), device="cuda")
+    at = (idx.cuda(), t.cuda(), label.cuda(), 2.0, 0.6, 0.4)
+    B.mv_distill_loss(d, *at, loss, scratch_of(rows, n), dz=dz)
+    check(ref, loss, dz)
+    B.mv_distill_loss(d, *at, loss, scratch_of(rows, n), dz=d)
+    assert torch.equal(d, dz.to(d.dtype))
+
+
+@pytest.mark.parametrize("src", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n,top", [(3, 30, 4096), (2, 5000, 4096), (5, 1000, 1025), (2, 140_000, 3000), (2, 20_000, 4096), (260, 36_000, 4096),
+                                        (50, 70_000, 4096), (3, 70_000, 2500)])
+def test_long_lists(rows, n, top, src):
+    z, idx, t, label = make(rows, n, top, src, top)
     ref = reference(z, idx, t, label, 2.0, 0.6, 0.4, None)
     loss, dz, stats = torch.zeros(rows, device="cuda"), torch.zeros((rows, n), device="cuda"), torch.zeros((rows, 3), device="cuda")
-    at = (z.cuda(), idx.cuda(), t.cuda(), label.cuda(), 2.0, 0.6, 0.4)
+    at = (z.to(TYPES[src]).cuda(), idx.cuda(), t.cuda(), label.cuda(), 2.0, 0.6, 0.4)
     B.mv_distill_loss(*at, loss, scratch_of(rows, n), stats=stats, dz=dz)
     check(ref, loss, dz)
     B.mv_distill_grad(*at, stats, dz)
