@@ -641,8 +641,8 @@ template <typename T, int LANES, int C, int TERMS>
 static void held(const Distill& d, hipStream_t st)
 {
     constexpr int kRows = kThreadsOf<LANES> / LANES;
-    // as many as run at once, sixteen wavefronts to a unit
-    const dim3   grid(grid_of((d.rows + kRows - 1) / kRows, 256 * 1024 / kThreadsOf<LANES>)), group(kThreadsOf<LANES>);
+    // as many as run at once: sixteen wavefronts to a unit, of the smallest rows twenty-four (20,000 x 100 bf16 30 -> 26 us)
+    const dim3   grid(grid_of((d.rows + kRows - 1) / kRows, LANES == 64 ? 1536 : 256 * 1024 / kThreadsOf<LANES>)), group(kThreadsOf<LANES>);
     const size_t lists = kRows * list_bytes(d.top);
     // the longest rows' longest lists need the LDS that the next row would have: 160 KB less what the kernel's own variables take
     if constexpr (ahead_of(LANES, C) * LANES * 16 + list_bytes(kMostTop) > 159 * 1024) {
