@@ -589,9 +589,9 @@ __global__ __launch_bounds__(64 * kFewWaves, MT == 1 ? 4 : 2) void mv_f8_product
 constexpr int64_t  kFewRows = 16, kFewValues = 64;
 constexpr uint32_t kFewLds = 144 * 1024;
 
-// Whether and how the kernel for few rows takes a product: up to 16 rows of codes (with
-// 32 it is faster for some sizes and slower for others: 32 x 4096 by 4096 12.2 us, in tiles 13.8, 8192 by 8192 29.7, in tiles 21.5), and up to 64 of values where quantising them
-// in every workgroup costs less than a launch that does it once, which is where all of them together have few.
+// Whether and how the kernel for few rows takes a product: up to 16 rows of codes (with 32 it is faster for some sizes and slower
+// for others: 32 x 4096 by 4096 12.2 us, in tiles 13.8, 8192 by 8192 29.7, in tiles 21.5), and up to 64 of values where
+// quantising them in every workgroup costs less than a launch that does it once, which is where all of them together have few.
 // bf16 us in one launch, and in two: 2 x 4096 by 4096, 2 million values to all workgroups, 6.7 (9.1); 32 x 2048 by 2048, 8 M, 8.4
 // (11.9); 1 x 8192 by 16,384, 8 M, 26.7 (27.9); 3 x 8192 by 8192, 13 M, 16.3 (16.1); 16 x 4096 by 4096, 17 M, 10.0 (9.1); 5 x
 // 8192 by 16,384, 42 M, 36.2 (32.2); beyond 16 rows 64 x 1024 by 4096, 17 M, 9.3 (11.8).  fp32: 8 x 2048 by 4096, 4 M, 7.6 (9.0);
@@ -691,11 +691,16 @@ static Cut cut_of(int64_t m, int64_t n, int64_t k, int mt, int64_t share = 0)
     c.splits = (uint32_t)((steps + c.steps_each - 1) / c.steps_each);
     return c;
 }
-// Up to four steps and more tiles of 128 x 128 than units: one buffer and three workgroups a unit, of which one loads or
-// stores while another multiplies.
+// Results in bf16: tiles of 256 x 256, one to a unit, where those of 128 x 128 are more than the 512 that run at once, of up to four
+// steps from 192 on.  us without and with: 2048 x 4352 by 4096 67.8, 59.4; 2816 x 3584 by 8192 127, 105; 4096 x 8192 by 8192
+// 310, 238; but 2048 x 4096 by 4096, 128 of them, 50.1, 57.6; 4096 x 4096 by 512 20.9, 18.6, but 2560 x 3700 by 512 14.4, 17.6.
+//
+// Else, with up to four steps and more tiles than units: one buffer and three workgroups a unit, of which one loads or stores
+// while another multiplies.  us with two buffers and with one: 2304 x 2304 by 512 14.4, 12.3, in fp32 16.4, 15.7; 8192 x 8192 by
+// 512 fp32 112, 104; but 4096 x 4096 by 768 fp32 41.0, 43.7.
 constexpr int64_t kFewSteps = 4, kUnits = 256;
 inline bool few_steps(int64_t k) { return blocks_of(k) <= kFewSteps; }
-static bool large(int64_t m, int64_t n) { return ((m + 255) / 256) * ((n + 255) / 256) >= 192; }
+static bool large(int64_t m, int64_t n, int64_t k) { return ((m + 255) / 256) * ((n + 255) / 256) >= (few_steps(k) ? 192 : 129); }
 inline size_t parts_bytes(int64_t m, int64_t n, int64_t k)
 {
     const uint32_t splits = cut_of(m, n, k, 2).splits;
@@ -792,7 +797,7 @@ static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
     for (int i = 0; i < n; ++i) {
         tiled[i] = !few[i].mt && offsets_fit(w[i], 2);
         if (tiled[i]) {
-            const bool larger = w[i].c.bf16 && large(w[i].a.rows, w[i].b.rows) && offsets_fit(w[i], 4);
+            const bool larger = w[i].c.bf16 && large(w[i].a.rows, w[i].b.rows, w[i].k) && offsets_fit(w[i], 4);
             cut[i] = cut_of(w[i].a.rows, w[i].b.rows, w[i].k, larger ? 4 : 2);
             if (cut[i].groups() > kMostGroups / 2) return MV_ERR_INVALID_ARG;
         }
@@ -811,7 +816,7 @@ static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
         all += c.tiles_m * c.tiles_n;
         work += c.tiles_m * c.tiles_n * blocks_of(w[i].k);
     }
-    one_buffer &= all > kUnits && all <= kMostGroups;
+    one_buffer &= all > kUnits && all <= kMostGroups && (cut[0].mt == 2 || (n == 2 && cut[1].mt == 2));
     // with one buffer: the smaller tiles; in one launch: those for both
     if (one_buffer || (n == 2 && (cut[0].mt == 2 || cut[1].mt == 2))) {
         const int64_t share = n == 1 ? 0 : (work + 2 * kUnits - 1) / (2 * kUnits);

@@ -100,19 +100,20 @@ def test_whole_numbers_are_exact(m, n, k):
         assert torch.equal(out.cpu(), want.to(dst))
 
 
-@pytest.mark.parametrize("m,n,k", [(3, 20, 200), (20, 40, 1000), (200, 300, 1100)])
-def test_nan_blocks_reach_their_rows_and_columns_only(m, n, k):
+@pytest.mark.parametrize("dst", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(3, 20, 200), (20, 40, 1000), (200, 300, 1100), (2100, 2200, 200), (2100, 4400, 700)])
+def test_nan_blocks_reach_their_rows_and_columns_only(m, n, k, dst):
     rng = np.random.default_rng(1)
     x, y = normal(rng, m, k), normal(rng, n, k)
     x[1, k - 1] = np.inf
     y[n - 1, 40] = np.nan
     a_codes, a_scales, _ = hold(x)
     b_codes, b_scales, _ = hold(y)
-    out = torch.zeros((m, n), device="cuda")
+    out = torch.zeros((m, n), dtype=TYPES[dst], device="cuda")
     B.mv_f8_product(a_codes, a_scales, b_codes, b_scales, k, out, scratch_of(B.mv_f8_product_scratch_bytes(m, n, k)))
     lost = np.zeros((m, n), bool)
     lost[1], lost[:, n - 1] = True, True
-    assert np.array_equal(np.isnan(out.cpu().numpy()), lost)
+    assert np.array_equal(torch.isnan(out).cpu().numpy(), lost)
 
 
 def test_scales_far_apart():
@@ -291,7 +292,8 @@ def test_rows_far_apart(length, places):
 
 @pytest.mark.parametrize("dst", ["f32", "bf16"])
 @pytest.mark.parametrize("m,n,k", [(2100, 2070, 20), (2049, 2100, 257), (1030, 4500, 768), (2500, 2100, 1000), (2100, 2200, 1056),
-                                   (3600, 3500, 1100), (2100, 2200, 500)])
+                                   (3600, 3500, 1100), (2100, 2200, 500), (3500, 3520, 300),
+                                   (3500, 3520, 130), (4300, 2100, 650)])
 def test_many_tiles(m, n, k, dst):
     """More tiles than units, with few steps along k and with more of them, and the large tiles."""
     rng = np.random.default_rng(m + n + k)

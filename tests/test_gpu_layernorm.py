@@ -73,7 +73,8 @@ def check_forward(x, gamma, beta, eps, y, mean, rstd):
 
 
 SHAPES = [(1, 1), (3, 2), (5, 7), (2, 64), (7, 255), (9, 512), (4, 1000), (33, 1024), (3, 2049), (2, 4097), (5, 8192), (2, 8200),
-          (1, 16384), (2, 16400), (2, 33_000), (1, 70_001), (1030, 65), (9000, 9), (700, 600), (600, 3000)]
+          (1, 16384), (2, 16400), (2, 33_000), (1, 70_001), (1030, 65), (9000, 9), (700, 600), (600, 3000), (2100, 1500), (1100, 6001),
+          (520, 12_000), (520, 20_001)]
 
 
 @pytest.mark.parametrize("src,dst,weights", [("f32", "f32", "f32"), ("bf16", "bf16", "bf16"), ("bf16", "f32", "f32"),
