@@ -576,6 +576,8 @@ mv_status mv_f8_decode(const uint8_t* codes, int64_t ld_bytes, const uint8_t* sc
  * towards zero, and those sums in fp32: off by at most 7 * 2^-13 of the magnitudes' sum, and by less than
  * 2^-16 of it for normal values, before it is rounded to bf16.
  * scratch: device, 16-byte aligned, >= mv_f8_product_scratch_bytes(m, n, k) (0: may be NULL).
+ * Here and below it is a call's alone until the call's work has ended: calls, or graphs that
+ * hold them, that may run at the same time have one each.  No output overlaps another argument.
  */
 size_t    mv_f8_product_scratch_bytes(int64_t m, int64_t n, int64_t k);
 mv_status mv_f8_product(const uint8_t* a_codes, int64_t ld_ab, const uint8_t* a_scales, int64_t ld_as,
@@ -632,7 +634,9 @@ mv_status mv_layernorm_forward(const void* x, int32_t x_dtype, int64_t ld_x, int
  *
  * x and dy have the same type; mean, rstd as the forward pass left them.  dx, dgamma and
  * dbeta may each be NULL, not all three; dx may be dy or x itself, with its type and stride.
- * scratch: device, 16-byte aligned, >= mv_layernorm_scratch_bytes(rows, n).
+ * Apart from that no output overlaps another argument, as in the forward pass.  scratch:
+ * device, 16-byte aligned, >= mv_layernorm_scratch_bytes(rows, n), one for each call, or graph
+ * that holds calls, that may run at the same time as others.
  */
 size_t    mv_layernorm_scratch_bytes(int64_t rows, int64_t n);   /* 0 for sizes outside 1 .. 2^31-1 */
 mv_status mv_layernorm_backward(const void* x, int64_t ld_x, const void* dy, int64_t ld_dy, int32_t dtype, int64_t rows,
@@ -675,8 +679,10 @@ mv_status mv_layernorm_backward(const void* x, int64_t ld_x, const void* dy, int
  * mv_distill_grad forms the gradient alone from the stats of a call with the same logits,
  * lists, labels and weights.  Sums are fp32 in an order that follows from sizes and types.
  * soft and hard are finite, T is 2^-60 .. 2^60.  1 <= rows, n < 2^31.  Runs on the CURRENT
- * device, enqueued on `stream`; allocates nothing.  scratch: device, 16-byte aligned,
- * >= mv_distill_scratch_bytes(rows, n) (0: may be NULL).
+ * device, enqueued on `stream`; allocates nothing.  Apart from dz over logits no output
+ * overlaps another argument.  scratch: device, 16-byte aligned, >= mv_distill_scratch_bytes(rows,
+ * n) (0: may be NULL), one for each call, or graph that holds calls, that may run at the same
+ * time as others.
  * Errors: MV_ERR_INVALID_ARG, MV_ERR_DEVICE.
  */
 size_t    mv_distill_scratch_bytes(int64_t rows, int64_t n);

@@ -8,11 +8,15 @@
 // terms are wanted and T is not 1 (of T = 2 the second one is the first one's square).  Where dz is wanted with the loss and a
 // row fits a workgroup's registers, z is read once: its maximum, its sums, and dz from the registers, which take the next row's
 // logits as they become free.  Otherwise rows, or ranges of rows where there are few, stream by for their maxima and sums,
-// each thread's joined at the end, and once more for dz.
+// each thread's joined at the end, and once more for dz.  Loss and dz of 4096 x 131,072 bf16, 64 listed, both terms: T = 2 450 us,
+// 4.8 TB/s, T = 3 490 (its exponentials), T = 1 415, 5.2; 2000 x 50,001 fp32 167, 4.8, the loss alone 70, 5.7; dz alone 3000 x
+// 32,768 bf16 77, 5.1.  What is missing to a copy's 5.95 is, with the loss, the time between a row's last load and its first
+// store, in which only the half of the next row that has room in LDS is on its way.
 //
 // A row's list is the first wavefront's, while the others have the logits.  dz has the same formula everywhere but at the
-// listed coordinates and the label.  Those are written behind the rest by the wavefront that wrote them before: one lane for
-// each entry, which adds up what the list has for its coordinate, in the list's order, where it is the first to name it.
+// listed coordinates and the label.  Those are written behind the rest by the wavefront that wrote them before, a lane for each
+// entry.  Entries that name one coordinate add up, in the list's order, for the first of them; they find each other by slots
+// that their coordinates have in LDS (all compared with all took 2000 x 60,000 with 256 listed 288 us, now 129).
 #include "mv_rows.hpp"
 
 #include <type_traits>
