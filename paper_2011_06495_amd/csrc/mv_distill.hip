@@ -8,10 +8,8 @@
 // terms are wanted and T is not 1 (of T = 2 the second one is the first one's square).  Where dz is wanted with the loss and a
 // row fits a workgroup's registers, z is read once: its maximum, its sums, and dz from the registers, which take the next row's
 // logits as they become free.  Otherwise rows, or ranges of rows where there are few, stream by for their maxima and sums,
-// each thread's joined at the end, and once more for dz.  Loss and dz of 4096 x 131,072 bf16, 64 listed, both terms: T = 2 450 us,
-// 4.8 TB/s, T = 3 490 (its exponentials), T = 1 415, 5.2; 2000 x 50,001 fp32 167, 4.8, the loss alone 70, 5.7; dz alone 3000 x
-// 32,768 bf16 77, 5.1.  What is missing to a copy's 5.95 is, with the loss, the time between a row's last load and its first
-// store, in which only the half of the next row that has room in LDS is on its way.
+// each thread's joined at the end, and once more for dz.  Loss and dz of 4096 x 131,072 bf16, 64 listed, both terms: T = 2 430 us,
+// 5.0 TB/s, T = 3 450, T = 1 418, 5.1; 2000 x 50,001 fp32 170, 4.7, the loss alone 70, 5.7; dz alone 3000 x 32,768 bf16 77, 5.1.
 //
 // A row's list is the first wavefront's, while the others have the logits.  dz has the same formula everywhere but at the
 // listed coordinates and the label.  Those are written behind the rest by the wavefront that wrote them before, a lane for each
@@ -139,38 +137,45 @@ __device__ __forceinline__ uint32_t slot_of(const List& l, int32_t at) { return 
 // The slot may hold what another lane has put there: LDS is in order within a wavefront, and the compiler does not know the place.
 __device__ __forceinline__ uint16_t& slot_again(const List& l, int32_t at) { return l.slots[fresh(slot_of(l, at))]; }
 
-template <typename T>
-__device__ __forceinline__ float logit(const T* row, int32_t at)
-{
-    return sizeof(T) == 2 ? mvx::widen(reinterpret_cast<const uint16_t*>(row)[at]) : reinterpret_cast<const float*>(row)[at];
-}
-// An entry of the list on its way, or the label.
+// An entry of the list on its way, or the label: asked for, then taken as it has come, then its logit asked for.  What is loaded
+// stays as it is until then, or it would be waited for at once.
 struct Entry {
-    int32_t at;                         // -1: none
-    float   t, z;
+    int32_t  at;                        // -1: none
+    uint32_t raw, raw16;                // the teacher's logit, in one of them
+    float    t;
+    uint32_t z;                         // the row's, as it is
     __device__ __forceinline__ void name(const Distill& d, int64_t row, uint32_t j)
     {
-        at = -1, t = -kInf, z = 0.0f;
+        at = -1, raw = raw16 = 0;
         if (j < d.top) {
             at = d.idx[row * d.ld_idx + j];
-            t = d.t.at(row * d.ld_t + j);
+            if (d.t.bf16) raw16 = static_cast<const uint16_t*>(d.t.p)[row * d.ld_t + j];
+            else raw = static_cast<const uint32_t*>(d.t.p)[row * d.ld_t + j];
         }
+    }
+    __device__ __forceinline__ void name_label(const Distill& d, int64_t row) { at = d.labels ? d.labels[row] : -1; }
+    __device__ __forceinline__ void take(const Distill& d)
+    {
+        t = __uint_as_float(raw | raw16 << 16), z = 0;
         if (at < 0 || at >= d.n) at = -1, t = -kInf;
     }
-    __device__ __forceinline__ void name_label(const Distill& d, int64_t row)
+    __device__ __forceinline__ void take_label(const Distill& d)         // a wavefront's row is one
     {
-        at = __builtin_amdgcn_readfirstlane(d.labels ? d.labels[row] : -1), t = -kInf, z = 0.0f;    // a wavefront's row is one
+        at = __builtin_amdgcn_readfirstlane(at), z = 0;
         if (at < 0 || at >= d.n) at = -1;
     }
     // With a range of coordinates only, logits elsewhere are not looked at.
     template <typename T>
     __device__ __forceinline__ void look(const T* row, int64_t from, int64_t to)
     {
-        if (at >= from && at < to) z = logit(row, at);
+        if (at >= from && at < to) z = sizeof(T) == 2 ? (uint32_t)reinterpret_cast<const uint16_t*>(row)[at] : reinterpret_cast<const uint32_t*>(row)[at];
     }
+    template <typename T>
+    __device__ __forceinline__ float logit() const { return __uint_as_float(sizeof(T) == 2 ? z << 16 : z); }
+    template <typename T>
     __device__ __forceinline__ void keep(const List& l, uint32_t j) const
     {
-        l.idx[j] = at, l.p[j] = t, l.z[j] = z;
+        l.idx[j] = at, l.p[j] = t, l.z[j] = logit<T>();
         if (at >= 0) l.slots[slot_of(l, at)] = (uint16_t)j;
     }
 };
@@ -195,12 +200,13 @@ __device__ __forceinline__ Terms take_list(const Distill& d, const List& l, int6
     const uint32_t lane = fresh(threadIdx.x & 63u);
     float most = first.t;
     bool  listed = first.at == label.at;
-    if (lane < d.top) first.keep(l, lane);
+    if (lane < d.top) first.keep<T>(l, lane);
     for (uint32_t j = lane + 64; j < d.top; j += 64) {
         Entry e;
         e.name(d, row, j);
+        e.take(d);
         e.look(z, from, to);
-        e.keep(l, j);
+        e.keep<T>(l, j);
         most = fmaxf(most, e.t);
         listed |= e.at == label.at;
     }
@@ -217,7 +223,7 @@ __device__ __forceinline__ Terms take_list(const Distill& d, const List& l, int6
     }
     sum = wave_sum(sum);
     const float log_sum = logf(sum);
-    Terms w = {sum == 0.0f ? 0.0f : sum * 0.0f + 1.0f, 0.0f, 0.0f, label.z, label.at, __ballot(listed) != 0 && label.at >= 0};
+    Terms w = {sum == 0.0f ? 0.0f : sum * 0.0f + 1.0f, 0.0f, 0.0f, label.logit<T>(), label.at, __ballot(listed) != 0 && label.at >= 0};
     for (uint32_t j = lane; j < d.top; j += 64) {
         const float   v = l.p[j];
         const int32_t at = l.idx[j];
@@ -280,7 +286,7 @@ __device__ __forceinline__ void patch(const Distill& d, const List& l, const Wei
         const float off = d.soft_grad * p + (at == terms.label ? d.hard : 0.0f);
         d.dz.put(row * d.ld_dz + at, w.of(Pair<TERMS>(z - w.largest, d.scale)) - w.g * off);
     };
-    __builtin_amdgcn_s_waitcnt(kNoLoads);                                // the stores before, too: these are behind them
+    // these stores are behind the ones before without a wait: a wavefront's are in order
     for (uint32_t j = lane; j - lane < d.top; j += 64) {
         const int32_t at = j < d.top ? l.idx[j] : -1;
         bool  write = ours(at);
@@ -309,15 +315,23 @@ __device__ __forceinline__ void patch(const Distill& d, const List& l, const Wei
 
 // How many chunks of the next row a thread has in LDS beforehand.
 __host__ __device__ constexpr int ahead_of(int lanes, int chunks) { return lanes > 64 ? chunks / 2 : 0; }
+constexpr int kSixteenOps = 0x4F70;     // s_waitcnt: no more than sixteen vector loads and stores in flight
 
 // LANES threads with up to C whole chunks each, and one that the row may end in.  With no more than a hundred registers
 // beside them: whole chunks come and go through buffers, and chunks that a row does not have are 0 and left out.
-template <typename T, int LANES, int C, int TERMS, bool AHEAD>
-__global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distill d)
+//
+// 1024 threads have a unit to themselves (OUT: 1 + whether dz is bf16, else 0: known at run time).  So that memory has as much to do
+// while a row is summed up as while it is written, chunks whose successors come from memory are written first, and the stores
+// of the others need not have ended when the next row's maximum is looked for: waits count what was issued since, which takes a
+// store for each chunk, beyond the row's end as well, where the buffer drops it (4096 x 131,072 bf16 T = 2
+// 451 -> 432 us, T = 3 487 -> 449).
+template <typename T, int LANES, int C, int TERMS, bool AHEAD, int OUT>
+__global__ __launch_bounds__(kThreadsOf<LANES>, LANES == 64 ? 6 : 4) void mv_distill_kernel(Distill d)
 {
     constexpr int V = kChunk<T>, kRows = kThreadsOf<LANES> / LANES, kWaves = LANES / 64;
     __shared__ float tops[kWaves], sums[2][kWaves];
     __shared__ Terms shared;
+    __shared__ float shared_g;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const uint32_t t = threadIdx.x % LANES, mine = __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(t / 64);
@@ -327,6 +341,7 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
     // The first chunks of the next row are fetched into LDS while this one's are summed up; each wavefront reads its own again.
     constexpr int kAhead = AHEAD ? ahead_of(LANES, C) : 0;
     __shared__ __attribute__((aligned(16))) uint8_t ahead[kAhead ? kAhead * LANES * 16 : 16];
+    const bool out16 = OUT ? OUT == 2 : d.dz.bf16;
     // in one scalar comparison each time, not in sixteen masks that are kept
     auto there = [&](int c) {
         int f = full;
@@ -334,7 +349,10 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
         return c < f;
     };
     auto row_at = [&](int64_t row) { return static_cast<const T*>(d.z) + row * d.ld_z; };
-    auto fetch_tail = [&](const T* z) { tail.load_low(z + full * (LANES * V) + t * V, rest); };
+    auto fetch_tail = [&](const T* z) {
+        if (rest > 0) tail.load_low(z + full * (LANES * V) + t * V, rest);
+        else tail.none();
+    };
     int64_t row = (int64_t)blockIdx.x * kRows + mine;
     const int64_t step = (int64_t)gridDim.x * kRows;
     if (row >= d.rows) return;                                           // a wavefront's own row, or the whole workgroup's
@@ -344,16 +362,25 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
         for (int c = 0; c < C; ++c) held[c].take(z.load(t * 16, c * (LANES * 16)));
         fetch_tail(row_at(row));
     }
+    Entry entry, label;
+    float g = 1.0f;
+    auto name = [&](int64_t of) {
+        entry.name(d, of, t), label.name_label(d, of);
+        if (d.grad) g = d.grad[of];
+    };
+    if (wave == 0) name(row);
+    if (OUT) __builtin_amdgcn_s_waitcnt(kNoLoads);                       // or the loop would wait for all of its own each time
     for (; row < d.rows; row += step) {
-        Entry entry, label;
-        if (wave == 0) entry.name(d, row, t), label.name_label(d, row);
         Largest<T> most;
         most.look(tail);
 #pragma unroll
         for (int c = 0; c < C; ++c)
             if (there(c)) most.look(held[c]);
         float largest = wave_max(most.value());
-        if (wave == 0) entry.look(row_at(row), 0, d.n), label.look(row_at(row), 0, d.n);
+        if (wave == 0) {
+            entry.take(d), label.take_label(d);
+            entry.look(row_at(row), 0, d.n), label.look(row_at(row), 0, d.n);
+        }
         const bool more = row + step < d.rows;                           // behind the last row there is nothing
         const RowOf next(row_at(more ? row + step : row), more ? full * (LANES * 16) : 0);
         if constexpr (kWaves > 1) {
@@ -362,7 +389,6 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) largest = larger(tops[w], largest);
         }
-        // between the two barriers, which wait for them
         if constexpr (kAhead > 0) {
             __builtin_amdgcn_s_waitcnt(kNoLds);                          // what was read of the last ones is here
 #pragma unroll
@@ -375,17 +401,20 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
             if (there(c)) add_up<T, TERMS>(held[c], largest, d.scale, a, b);
         a = wave_sum(a);
         if (TERMS != kOne) b = wave_sum(b);
+        float row_g = g;
         Terms w;
         if (wave == 0) w = take_list(d, list, row, row_at(row), entry, label, largest, 0, d.n);
-        __builtin_amdgcn_s_waitcnt(kNoLoads);                            // dz may be z: all that is read of the row is here
+        // Dz may be z: what is read of the row is in registers or LDS by now.
         if constexpr (kWaves > 1) {
             if ((t & 63u) == 0) sums[0][wave] = a, sums[1][wave] = b;
-            if (t == 0) shared = w;
-            __syncthreads();
+            if (t == 0) shared = w, shared_g = g;
+            // the next row's chunks need not be here
+            if constexpr (OUT) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            else __syncthreads();
             a = b = 0.0f;
 #pragma unroll
             for (int i = 0; i < kWaves; ++i) a += sums[0][i], b += sums[1][i];
-            w = shared;
+            w = shared, row_g = shared_g;
         }
         if (TERMS == kOne) b = a;
         if (t == 0) {
@@ -396,27 +425,31 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, 4) void mv_distill_kernel(Distil
                 d.stats[3 * row + 2] = d.labels ? b : 0.0f;
             }
         }
-        const Weights weights = weights_of<TERMS>(d, w.soft, w.label, d.grad ? d.grad[row] : 1.0f, largest, a, b);
+        const Weights weights = weights_of<TERMS>(d, w.soft, w.label, row_g, largest, a, b);
         // each chunk's registers take the next row's as soon as its own is written
-        const RowOf dz(static_cast<char*>(d.dz.p) + row * d.ld_dz * (d.dz.bf16 ? 2 : 4), d.dz.p ? full * (LANES * V) * (d.dz.bf16 ? 2 : 4) : 0);
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            if (there(c)) {
-                float y[V];
-                held[c].forget();                                        // what was made of it for the sums is not kept
-                plain_grad<T, TERMS>(held[c], weights, d.scale, y);
-                dz.store<LANES>(y, t, c, d.dz.bf16);
-            }
-            if (c < kAhead) held[c].take(*reinterpret_cast<const u32x4*>(ahead + (c * kWaves + wave) * 1024 + (t & 63u) * 16));
-            else held[c].take(next.load(t * 16, c * (LANES * 16)));
-        }
+        const RowOf dz(static_cast<char*>(d.dz.p) + row * d.ld_dz * (out16 ? 2 : 4), d.dz.p ? full * (LANES * V) * (out16 ? 2 : 4) : 0);
         if (d.dz.p) {
             float y[V];
             plain_grad<T, TERMS>(tail, weights, d.scale, y);
             d.dz.store(row * d.ld_dz + full * (LANES * V) + t * V, rest, y);
-            patch<T, LANES, TERMS>(d, list, weights, row, w, 0, d.n);
         }
         if (more) fetch_tail(row_at(row + step));
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int c = OUT ? (i + kAhead) % C : i;
+            if (i == C / 2 && wave == 0 && more) name(row + step);
+            if (OUT && i == C - kAhead) __builtin_amdgcn_s_waitcnt(kSixteenOps);     // a store and a load a chunk: the ones into LDS are here
+            float y[V] = {};
+            if (there(c)) {
+                held[c].forget();                                        // what was made of it for the sums is not kept
+                plain_grad<T, TERMS>(held[c], weights, d.scale, y);
+                if (!OUT) dz.store<LANES>(y, t, c, out16);
+            }
+            if (OUT) dz.store<LANES>(y, t, c, out16);
+            if (c < kAhead) held[c].take(*reinterpret_cast<const u32x4*>(ahead + (c * kWaves + wave) * 1024 + (t & 63u) * 16));
+            else held[c].take(next.load(t * 16, c * (LANES * 16)));
+        }
+        if (d.dz.p) patch<T, LANES, TERMS>(d, list, weights, row, w, 0, d.n);
     }
 }
 
@@ -487,6 +520,7 @@ __global__ __launch_bounds__(kStreamThreads) void mv_distill_loss_kernel(Distill
         Entry entry, label;
         if (wave == 0 && d.loss) {
             entry.name(d, row, threadIdx.x), label.name_label(d, row);
+            entry.take(d), label.take_label(d);
             entry.look(z, 0, d.n), label.look(z, 0, d.n);
         }
         float largest, a, b;
@@ -538,6 +572,7 @@ __global__ __launch_bounds__(64) void mv_distill_join_kernel(Distill d)
         Entry entry, label;
         if (d.loss) {
             entry.name(d, row, threadIdx.x), label.name_label(d, row);
+            entry.take(d), label.take_label(d);
             entry.look(z, 0, d.n), label.look(z, 0, d.n);
         }
         const float* part = d.parts + 4 * row * d.ranges;
@@ -581,6 +616,7 @@ __global__ __launch_bounds__(kStreamThreads) void mv_distill_grad_kernel(Distill
         if (wave == 0) {
             Entry entry, label;                                          // logits elsewhere may have been written over
             entry.name(d, row, threadIdx.x), label.name_label(d, row);
+            entry.take(d), label.take_label(d);
             entry.look(z, first, last), label.look(z, first, last);
             const Terms w = take_list(d, list, row, z, entry, label, largest, first, last);
             if (threadIdx.x == 0) shared = w;
@@ -648,14 +684,18 @@ static void held(const Distill& d, hipStream_t st)
     // as many as run at once: sixteen wavefronts to a unit, of the smallest rows twenty-four (20,000 x 100 bf16 30 -> 26 us)
     const dim3   grid(grid_of((d.rows + kRows - 1) / kRows, LANES == 64 ? 1536 : 256 * 1024 / kThreadsOf<LANES>)), group(kThreadsOf<LANES>);
     const size_t lists = kRows * list_bytes(d.top);
-    // the longest rows' longest lists need the LDS that the next row would have: 160 KB less what the kernel's own variables take
-    if constexpr (ahead_of(LANES, C) * LANES * 16 + list_bytes(kMostTop) > 159 * 1024) {
-        if (ahead_of(LANES, C) * LANES * 16 + lists > 159 * 1024) {
-            hipLaunchKernelGGL((mv_distill_kernel<T, LANES, C, TERMS, false>), grid, group, lists, st, d);
-            return;
-        }
+    auto launch = [&](auto ahead, auto out) {
+        hipLaunchKernelGGL((mv_distill_kernel<T, LANES, C, TERMS, decltype(ahead)::value, decltype(out)::value>), grid, group, lists, st, d);
+    };
+    const std::integral_constant<int, 0> any{};
+    if constexpr (LANES < 1024) {
+        launch(std::true_type{}, any);
+    } else {
+        // the longest lists need the LDS that the next row would have: 160 KB less what the kernel's own variables take
+        if (ahead_of(LANES, C) * LANES * 16 + lists > 159 * 1024) launch(std::false_type{}, any);
+        else if (d.dz.bf16) launch(std::true_type{}, std::integral_constant<int, 2>{});
+        else launch(std::true_type{}, std::integral_constant<int, 1>{});
     }
-    hipLaunchKernelGGL((mv_distill_kernel<T, LANES, C, TERMS, true>), grid, group, lists, st, d);
 }
 template <typename T, int TERMS>
 static void grad(Distill d, hipStream_t st)

@@ -35,6 +35,7 @@ struct Chunk<float> {
     }
     // To the compiler: other values from here on.
     __device__ __forceinline__ void forget() { asm("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3])); }
+    __device__ __forceinline__ void none() { x[0] = x[1] = x[2] = x[3] = -kInf; }
     __device__ __forceinline__ void load_low(const float* p, int live)
     {
         if (live >= 4) mvx::load4(p, 4, x);
@@ -54,6 +55,7 @@ struct Chunk<uint16_t> {
         for (int i = 0; i < 4; ++i) x[i] = w[i];
     }
     __device__ __forceinline__ void forget() { asm("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3])); }
+    __device__ __forceinline__ void none() { x[0] = x[1] = x[2] = x[3] = 0xFF80FF80u; }
     __device__ __forceinline__ void load_low(const uint16_t* p, int live)
     {
         if (live >= 8) mvx::load8(p, 8, x);
