@@ -74,8 +74,19 @@ __device__ __forceinline__ void join_splits(const float* __restrict__ parts, uin
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
     if (i < m) {
         const float* p = parts + i * (quads * 4) + j;
-#pragma unroll 4
-        for (uint32_t s = lane; s < splits; s += lanes) sum += *reinterpret_cast<const f32x4*>(p + s * split_c);
+        uint32_t s = lane;
+        for (; s + 3 * lanes < splits; s += 4 * lanes)
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u) sum += *reinterpret_cast<const f32x4*>(p + (s + u * lanes) * split_c);
+        // the last ones at once, too, not one after the other
+        if (s < splits) {
+            f32x4 v[3];
+#pragma unroll
+            for (uint32_t u = 0; u < 3; ++u) v[u] = *reinterpret_cast<const f32x4*>(p + min(s + u * lanes, splits - 1) * split_c);
+#pragma unroll
+            for (uint32_t u = 0; u < 3; ++u)
+                if (s + u * lanes < splits) sum += v[u];
+        }
     }
     if (lanes > 1) {                                                     // uniform
         sums[threadIdx.x] = sum;
