@@ -692,6 +692,8 @@ static Cut cut_of(int64_t m, int64_t n, int64_t k, int mt, int64_t share = 0)
     const int64_t steps = blocks_of(k);
     if (mt == 2) c.splits = (uint32_t)splits_of(c.tiles_m * c.tiles_n, steps, m * n, share);
     c.steps_each = (uint32_t)((steps + c.splits - 1) / c.splits);
+    // runs begin at even steps, as pairs of scales do: a pair that begins with a row's last byte would leave the last row's buffer
+    if (c.splits > 1) c.steps_each += c.steps_each % 2;
     c.splits = (uint32_t)((steps + c.steps_each - 1) / c.steps_each);
     return c;
 }

@@ -76,7 +76,8 @@ def test_product(m, n, k, dst):
 
 
 @pytest.mark.parametrize("m,n,k", [(1, 40, 300), (7, 33, 4096), (16, 130, 5000), (40, 50, 900), (130, 260, 2000), (300, 300, 3000),
-                                   (20, 18, 200_000), (2100, 2200, 300), (3600, 3500, 200)])
+                                   (20, 18, 200_000), (2100, 2200, 300), (3600, 3500, 200), (1024, 2048, 5632), (260, 390, 1536),
+                                   (150, 700, 2560)])
 def test_whole_numbers_are_exact(m, n, k):
     """Whole numbers up to 15, which any block with a largest magnitude up to 15 holds; a result's products come to less than
     2^24: half of a long row are zeros, and the others mostly small."""
