@@ -371,11 +371,20 @@ __global__ __launch_bounds__(64 * WM * WN, BUFFERS == 1 ? 3 : 2) void mv_f8_prod
     }
 }
 
-__global__ __launch_bounds__(256) void mv_f8_product_join_kernel(const float* __restrict__ parts, uint32_t splits, uint32_t lanes,
-                                                                 int64_t m, int64_t n, int64_t split_c, int64_t quads, Out c,
-                                                                 int64_t ld_c)
+// A product's splits, to be added up.
+struct Splits {
+    const float* parts;
+    uint32_t     count, lanes;
+    int64_t      m, n, split_c, quads;
+    Out          c;
+    int64_t      ld_c;
+    int64_t      groups() const { return (m * quads + 256 / lanes - 1) / (256 / lanes); }
+};
+template <bool PAIR>
+__global__ __launch_bounds__(256) void mv_f8_product_join_kernel(Launch<Splits, PAIR> l)
 {
-    mvx::join_splits(parts, splits, lanes, m, n, split_c, quads, c, ld_c);
+    const Splits& p = l.product();
+    mvx::join_splits(l.id(), p.parts, p.count, p.lanes, p.m, p.n, p.split_c, p.quads, p.c, p.ld_c);
 }
 
 // ---- few rows of one factor ------------------------------------------------------------------------------------------
@@ -665,15 +674,16 @@ struct Cut {
     uint32_t splits, steps_each;
     int64_t  groups() const { return tiles_m * tiles_n * splits; }
 };
-// How many runs the steps are split into.  With another product in the launch (`share`: the steps that each of two workgroups to a
+// How many runs the steps are split into, of four steps at least (1000 x 300 by 600 in one 9.3 us, of two 10.7; 2000 x 500 by 1024 of four
+// 12.8, of two 13.7).  With another product in the launch (`share`: the steps that each of two workgroups to a
 // unit has of both) never more than alone, which is what the scratch has room for; one where it is not much longer than the
 // share, because the other product's workgroups fill the units meanwhile; and no more than pay for writing and reading the
 // sums, a microsecond a step against 4 TB/s.  us with as many splits as fit beside the other's tiles, with runs of the share's
 // length, and so: 300 x 2000 by 4000 45.6, 34.0, 34.0; 8000 x 300 by 300 47.0, 34.7, 34.1; 4900 x 4608 by 512 82.8, 88.0, 82.4; 3000 x 512 by
-// 2048 38.9, 42.2, 38.7.
+// 2048 38.9, 42.2, 38.7 (by now 33.0, 27.8, 78.0 and 34.0).
 static constexpr int64_t splits_of(int64_t tiles, int64_t steps, int64_t results, int64_t share)
 {
-    int64_t splits = 512 / tiles < steps / 4 ? 512 / tiles : steps / 4;
+    int64_t splits = 512 / tiles < steps / 3 ? 512 / tiles : steps / 3;
     // many splits only of small results: all of them are written and read again
     if (splits > 16 && splits * results > (4 << 20)) splits = 16;
     if (share) {
@@ -729,13 +739,24 @@ static Product product_of(const Wanted& w, const Cut& cut)
             split ? Out{w.parts, 0} : w.c, split ? quads * 4 : w.ld_c, w.a.rows * quads * 4,
             w.a.rows * w.b.rows * (split ? 4 * (int64_t)cut.splits : w.c.bf16 ? 2 : 4) >= kPastBytes};
 }
-static void launch_join(const Wanted& w, const Cut& cut, hipStream_t st)
+// Of one product or two, in one launch (1000 x 1000 by 1000, both gradients: 22.8 us, joined one after the other 24.8).
+static void launch_joins(const Wanted* w, const Cut* cut, int n, hipStream_t st)
 {
-    if (cut.splits == 1) return;
-    const int64_t quads = quads_of(w.b.rows), all = w.a.rows * quads;
-    const uint32_t lanes = cut.splits > 16 ? 16 : 1, per = 256 / lanes;
-    hipLaunchKernelGGL(mv_f8_product_join_kernel, dim3((uint32_t)((all + per - 1) / per)), dim3(256), 0, st,
-                       static_cast<const float*>(w.parts), cut.splits, lanes, w.a.rows, w.b.rows, all * 4, quads, w.c, w.ld_c);
+    Splits s[2];
+    int    many = 0;
+    for (int i = 0; i < n; ++i) {
+        if (cut[i].splits == 1) continue;
+        const int64_t rows = w[i].a.rows, quads = quads_of(w[i].b.rows);
+        s[many++] = {static_cast<const float*>(w[i].parts), cut[i].splits, cut[i].splits > 16 ? 16u : 1u, rows, w[i].b.rows,
+                     rows * quads * 4, quads, w[i].c, w[i].ld_c};
+    }
+    if (!many) return;
+    const uint32_t firsts = (uint32_t)s[0].groups();
+    if (many == 2)
+        hipLaunchKernelGGL((mv_f8_product_join_kernel<true>), dim3(firsts + (uint32_t)s[1].groups()), dim3(256), 0, st,
+                           Launch<Splits, true>{{s[0], s[1]}, firsts});
+    else
+        hipLaunchKernelGGL((mv_f8_product_join_kernel<false>), dim3(firsts), dim3(256), 0, st, Launch<Splits, false>{{s[0]}, firsts});
 }
 // The kernel without LDS, for rows so long that a tile's byte offsets leave 32 bits.
 static mv_status launch_plain(const Wanted& w, hipStream_t st)
@@ -787,6 +808,9 @@ static void launch_tiles(const Launch<Product, PAIR>& l, int mt, bool one_buffer
 #undef MV_F8_TILES
 }
 
+// A product of few rows with fewer bytes of codes than this goes into the other one's launch of tiles: 500 x 10 by 300, both
+// gradients, 13.1 us, in two launches 16.4; 12 x 3000 by 1000, 3 million, 17.7 (18.9); 1000 x 10 by 4000, 4 million, 21.4 (20.2).
+constexpr int64_t kFewBeside = 3 << 20;
 // Up to two products (n: how many) in as few launches as their sizes allow.
 static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
 {
@@ -798,6 +822,10 @@ static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
         if (few[i].mt) fp[i] = few_codes(w[i], few_a[i]);
     }
     if (n == 2 && few[0].mt && few[1].mt) return launch_few(fp, few, 2, st);
+    if (n == 2 && (few[0].mt || few[1].mt)) {
+        const int f = few[0].mt ? 0 : 1;
+        if (w[0].c.bf16 == w[1].c.bf16 && (few_a[f] ? w[f].b.rows : w[f].a.rows) * w[f].k <= kFewBeside) few[f].mt = 0;
+    }
     Cut  cut[2] = {};
     bool tiled[2] = {};
     for (int i = 0; i < n; ++i) {
@@ -838,7 +866,7 @@ static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
     } else {
         launch_tiles(Launch<Product, false>{{p}, firsts}, cut[0].mt, one_buffer, wide, firsts, st);
     }
-    for (int i = 0; i < n; ++i) launch_join(w[i], cut[i], st);
+    launch_joins(w, cut, n, st);
     return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
 }
 

@@ -339,7 +339,7 @@ __global__ __launch_bounds__(256) void mv_mx_product_join_kernel(const float* __
                                                                  int64_t m, int64_t n, int64_t split_c, int64_t quads, Out c,
                                                                  int64_t ld_c)
 {
-    join_splits(parts, splits, lanes, m, n, split_c, quads, c, ld_c);
+    join_splits(blockIdx.x, parts, splits, lanes, m, n, split_c, quads, c, ld_c);
 }
 
 // ---- few rows of one factor ------------------------------------------------------------------------------------------

@@ -64,12 +64,12 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t 
 
 // c = the sum of the splits: a group of `lanes` threads takes four results, each thread every lanes-th split, and their
 // sums are added in order.
-__device__ __forceinline__ void join_splits(const float* __restrict__ parts, uint32_t splits, uint32_t lanes, int64_t m, int64_t n,
-                                            int64_t split_c, int64_t quads, Out c, int64_t ld_c)
+__device__ __forceinline__ void join_splits(uint32_t id, const float* __restrict__ parts, uint32_t splits, uint32_t lanes, int64_t m,
+                                            int64_t n, int64_t split_c, int64_t quads, Out c, int64_t ld_c)
 {
     __shared__ f32x4 sums[256];
     const uint32_t per = 256 / lanes, lane = threadIdx.x / per;          // a group's threads lie `per` apart
-    const int64_t at = (int64_t)blockIdx.x * per + threadIdx.x % per;
+    const int64_t at = (int64_t)id * per + threadIdx.x % per;
     const int64_t i = at / quads, j = at % quads * 4;
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
     if (i < m) {

@@ -179,7 +179,7 @@ def test_gradients_follow_their_formula(m, n, k, src):
     # each alone
     dx2, dw2 = torch.zeros_like(dx), torch.zeros((n, k), dtype=torch.bfloat16, device="cuda")
     B.mv_f8_linear_grad(None, dy, wt_codes, wt_scales, dx2, None, scratch)
-    assert torch.equal(dx, dx2)
+    check(dx2, R.held(dy32), wt, TYPES[src])             # alone, its sums may be another kernel's, in another order
     B.mv_f8_linear_grad(x, dy, None, None, None, dw2, scratch)
     check(dw2, held_dy, held_x, torch.bfloat16)
 
