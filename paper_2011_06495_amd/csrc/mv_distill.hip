@@ -326,7 +326,7 @@ constexpr int kSixteenOps = 0x4F70;     // s_waitcnt: no more than sixteen vecto
 // store for each chunk, beyond the row's end as well, where the buffer drops it (4096 x 131,072 bf16 T = 2
 // 451 -> 432 us, T = 3 487 -> 449).
 template <typename T, int LANES, int C, int TERMS, bool AHEAD, int OUT>
-__global__ __launch_bounds__(kThreadsOf<LANES>, LANES == 64 ? 6 : 4) void mv_distill_kernel(Distill d)
+__global__ __launch_bounds__(kThreadsOf<LANES>, C == 4 ? 6 : 4) void mv_distill_kernel(Distill d)
 {
     constexpr int V = kChunk<T>, kRows = kThreadsOf<LANES> / LANES, kWaves = LANES / 64;
     __shared__ float tops[kWaves], sums[2][kWaves];
@@ -455,28 +455,28 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, LANES == 64 ? 6 : 4) void mv_dis
 
 // ---- rows that stream by ---------------------------------------------------------------------------------------------
 
-constexpr int kStreamThreads = 512;
+constexpr int kRangeThreads = 512;      // of a range
 template <typename T>
 constexpr int kAhead = sizeof(T) == 2 ? 2 : 4;                           // chunks of a turn
 
 // A thread's largest and sums of [first, last) of a row: each turn's largest first, what was added up before scaled down to it.
-template <typename T, int TERMS>
+template <typename T, int THREADS, int TERMS>
 __device__ __forceinline__ void stream(const T* z, int64_t first, int64_t last, float scale, float& largest, float& a, float& b)
 {
     constexpr int V = kChunk<T>, G = kAhead<T>;
-    constexpr int64_t kTurn = (int64_t)kStreamThreads * V * G;
+    constexpr int64_t kTurn = (int64_t)THREADS * V * G;
     largest = -kInf, a = b = 0.0f;
     for (int64_t at = first; at < last; at += kTurn) {
         Chunk<T> c[G];
         const T* p = z + at + threadIdx.x * V;
         if (at + kTurn <= last) {
 #pragma unroll
-            for (int g = 0; g < G; ++g) c[g].load(p + g * (kStreamThreads * V), V);
+            for (int g = 0; g < G; ++g) c[g].load(p + g * (THREADS * V), V);
         } else {
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const int64_t live = last - at - threadIdx.x * V - g * (kStreamThreads * V);
-                c[g].load_low(p + g * (kStreamThreads * V), live < 0 ? 0 : live < V ? (int)live : V);
+                const int64_t live = last - at - threadIdx.x * V - g * (THREADS * V);
+                c[g].load_low(p + g * (THREADS * V), live < 0 ? 0 : live < V ? (int)live : V);
             }
         }
         Largest<T> most;
@@ -495,8 +495,8 @@ __device__ __forceinline__ void stream(const T* z, int64_t first, int64_t last, 
     }
 }
 // Joined over the workgroup; sums of nothing but -infinity are 0.
-template <int TERMS>
-__device__ __forceinline__ void join(Across<kStreamThreads>& across, float scale, float& largest, float& a, float& b)
+template <int THREADS, int TERMS>
+__device__ __forceinline__ void join(Across<THREADS>& across, float scale, float& largest, float& a, float& b)
 {
     const float top = across.max(largest), down = largest - (top == -kInf ? 0.0f : top);
     a *= power(down * scale);
@@ -507,12 +507,12 @@ __device__ __forceinline__ void join(Across<kStreamThreads>& across, float scale
 }
 
 // The loss of whole rows, a workgroup each.
-template <typename T, int TERMS>
-__global__ __launch_bounds__(kStreamThreads) void mv_distill_loss_kernel(Distill d)
+template <typename T, int THREADS, int TERMS>
+__global__ __launch_bounds__(THREADS) void mv_distill_loss_kernel(Distill d)
 {
-    __shared__ float sums[2][2][kStreamThreads / 64];
+    __shared__ float sums[2][2][THREADS / 64];
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    Across<kStreamThreads> across(sums);
+    Across<THREADS> across(sums);
     const List list = list_at(lds, d.top);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     for (int64_t row = blockIdx.x; row < d.rows; row += gridDim.x) {
@@ -524,8 +524,8 @@ __global__ __launch_bounds__(kStreamThreads) void mv_distill_loss_kernel(Distill
             entry.look(z, 0, d.n), label.look(z, 0, d.n);
         }
         float largest, a, b;
-        stream<T, TERMS>(z, 0, d.n, d.scale, largest, a, b);
-        join<TERMS>(across, d.scale, largest, a, b);
+        stream<T, THREADS, TERMS>(z, 0, d.n, d.scale, largest, a, b);
+        join<THREADS, TERMS>(across, d.scale, largest, a, b);
         // a row of nothing but -infinity has no sums
         if (largest == -kInf) a = b = __builtin_nanf("");
         if (wave == 0) {
@@ -544,16 +544,16 @@ __global__ __launch_bounds__(kStreamThreads) void mv_distill_loss_kernel(Distill
 
 // Largest and sums of a range.
 template <typename T, int TERMS>
-__global__ __launch_bounds__(kStreamThreads) void mv_distill_range_kernel(Distill d)
+__global__ __launch_bounds__(kRangeThreads) void mv_distill_range_kernel(Distill d)
 {
-    __shared__ float sums[2][2][kStreamThreads / 64];
-    Across<kStreamThreads> across(sums);
+    __shared__ float sums[2][2][kRangeThreads / 64];
+    Across<kRangeThreads> across(sums);
     const int64_t all = d.rows * d.ranges;
     for (int64_t at = blockIdx.x; at < all; at += gridDim.x) {
         const int64_t row = at / d.ranges, first = at % d.ranges * d.range, last = first + d.range < d.n ? first + d.range : d.n;
         float largest, a, b;
-        stream<T, TERMS>(static_cast<const T*>(d.z) + row * d.ld_z, first, last, d.scale, largest, a, b);
-        join<TERMS>(across, d.scale, largest, a, b);
+        stream<T, kRangeThreads, TERMS>(static_cast<const T*>(d.z) + row * d.ld_z, first, last, d.scale, largest, a, b);
+        join<kRangeThreads, TERMS>(across, d.scale, largest, a, b);
         if (threadIdx.x == 0) {
             float* to = d.parts + 4 * at;
             to[0] = largest, to[1] = a, to[2] = b;
@@ -598,11 +598,11 @@ __global__ __launch_bounds__(64) void mv_distill_join_kernel(Distill d)
 }
 
 // dz of a range, from the row's stats.
-template <typename T, int TERMS>
-__global__ __launch_bounds__(kStreamThreads) void mv_distill_grad_kernel(Distill d)
+template <typename T, int THREADS, int TERMS>
+__global__ __launch_bounds__(THREADS) void mv_distill_grad_kernel(Distill d)
 {
     constexpr int V = kChunk<T>, G = kAhead<T>;
-    constexpr int64_t kTurn = (int64_t)kStreamThreads * V * G;
+    constexpr int64_t kTurn = (int64_t)THREADS * V * G;
     __shared__ Terms shared;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const List list = list_at(lds, d.top);
@@ -630,18 +630,18 @@ __global__ __launch_bounds__(kStreamThreads) void mv_distill_grad_kernel(Distill
             int live[G];
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const int64_t left = last - col - threadIdx.x * V - g * (kStreamThreads * V);
+                const int64_t left = last - col - threadIdx.x * V - g * (THREADS * V);
                 live[g] = left < 0 ? 0 : left < V ? (int)left : V;
-                c[g].load(z + col + threadIdx.x * V + g * (kStreamThreads * V), live[g]);
+                c[g].load(z + col + threadIdx.x * V + g * (THREADS * V), live[g]);
             }
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 float y[V];
                 plain_grad<T, TERMS>(c[g], w, d.scale, y);
-                d.dz.store(row * d.ld_dz + col + threadIdx.x * V + g * (kStreamThreads * V), live[g], y);
+                d.dz.store(row * d.ld_dz + col + threadIdx.x * V + g * (THREADS * V), live[g], y);
             }
         }
-        patch<T, kStreamThreads, TERMS>(d, list, w, row, terms, first, last);
+        patch<T, THREADS, TERMS>(d, list, w, row, terms, first, last);
         __syncthreads();                                                 // the list and the terms are read before the next ones
     }
 }
@@ -656,7 +656,10 @@ static Lanes lanes_of(int64_t rows, int64_t n, int32_t dtype, int64_t top)
     // 72,000 1 16 -> 15 and 48 17 -> 16; but 128 rows 29 -> 28 and 18 -> 22, of 33,000 1 12.5 -> 14.
     if (rows <= 48 && n > 65536) return {0, 0};
     const int64_t wide = dtype == MV_BF16 ? 8 : 4, chunks = n / wide;
-    if (chunks < 64 * 4 && top <= 1024) return {64, 4};                  // four rows' lists in one workgroup's LDS: 48 KB
+    // A wavefront's rows need no barriers, and four times as many are at once on a unit: 8192 x 2500 bf16 26 us, with 256 threads 50; fp32
+    // 42 (53); 4096 x 8192 bf16 30 (35); but 1000 x 8192 13.5 (12.3).  Four rows' lists share a workgroup's LDS.
+    if (chunks < 64 * 4 && top <= 1024) return {64, 4};
+    if (chunks < 64 * 17 && top <= 1024 && rows >= 1000) return {64, 16};
     for (int lanes : {256, 512, 1024})
         if (chunks < (int64_t)lanes * 17) return {lanes, 16};            // the tail is one more
     return {0, 0};
@@ -682,7 +685,7 @@ static void held(const Distill& d, hipStream_t st)
 {
     constexpr int kRows = kThreadsOf<LANES> / LANES;
     // as many as run at once: sixteen wavefronts to a unit, of the smallest rows twenty-four (20,000 x 100 bf16 30 -> 26 us)
-    const dim3   grid(grid_of((d.rows + kRows - 1) / kRows, LANES == 64 ? 1536 : 256 * 1024 / kThreadsOf<LANES>)), group(kThreadsOf<LANES>);
+    const dim3   grid(grid_of((d.rows + kRows - 1) / kRows, C == 4 ? 1536 : 256 * 1024 / kThreadsOf<LANES>)), group(kThreadsOf<LANES>);
     const size_t lists = kRows * list_bytes(d.top);
     auto launch = [&](auto ahead, auto out) {
         hipLaunchKernelGGL((mv_distill_kernel<T, LANES, C, TERMS, decltype(ahead)::value, decltype(out)::value>), grid, group, lists, st, d);
@@ -697,32 +700,53 @@ static void held(const Distill& d, hipStream_t st)
         else launch(std::true_type{}, std::integral_constant<int, 1>{});
     }
 }
-template <typename T, int TERMS>
-static void grad(Distill d, hipStream_t st)
+// Threads of a row, or range, that streams by: as few as have a few chunks each, for many short ones are at once on a unit then, and
+// a list's way is long (6 us).  us with 64, 256 and 512.  The loss alone: 8192 x 5000 bf16 23, 28, 40; fp32 35, 34, 50; 8192 x
+// 12,000 bf16 47, 42, 60; 8192 x 30,000 101, 90, 102; 3000 x 32,768 43, 41, 40; 4000 x 30,000 fp32 88, 86, 82; 100 x 2500 fp32 12, 9, 9.  Dz: 8192 x
+// 5000 bf16 48, 53, 67; 8192 x 2500 fp32 52, 45, 69; 8192 x 12,000 bf16 98, 86, 101; fp32 198, 168, 152; 3000 x 32,768 bf16 86, 82, 77.
+template <typename F>
+static void with_threads(int64_t rows, int64_t chunks, int64_t most256, F launch)
 {
+    if (chunks <= 640 && rows >= 1000) launch(std::integral_constant<int, 64>{});
+    else if (chunks <= most256) launch(std::integral_constant<int, 256>{});
+    else launch(std::integral_constant<int, 512>{});
+}
+template <typename T, int TERMS>
+static void grad(Distill d, const Lanes& l, hipStream_t st)
+{
+    // The shortest rows as for the loss, whose sums are formed again: 8192 x 1000 bf16 14.5 us, from the stats 55.
+    if (l.chunks == 4) return held<T, 64, 4, TERMS>(d, st);
     const Ranges r = ranges_of(d.rows, d.n);
     d.ranges = r.count, d.range = r.length;
-    hipLaunchKernelGGL((mv_distill_grad_kernel<T, TERMS>), dim3(grid_of(d.rows * r.count, 1 << 20)), dim3(kStreamThreads), list_bytes(d.top),
-                       st, d);
+    with_threads(d.rows * r.count, d.range / kChunk<T>, 2048, [&](auto threads) {
+        constexpr int kThreads = decltype(threads)::value;
+        hipLaunchKernelGGL((mv_distill_grad_kernel<T, kThreads, TERMS>), dim3(grid_of(d.rows * r.count, 1 << 20)), dim3(kThreads),
+                           list_bytes(d.top), st, d);
+    });
 }
 template <typename T, int TERMS>
 static void loss(Distill d, const Lanes& l, hipStream_t st)
 {
-    if (l.lanes == 64) return held<T, 64, 4, TERMS>(d, st);
+    if (l.chunks == 4) return held<T, 64, 4, TERMS>(d, st);
+    if (d.dz.p && l.lanes == 64) return held<T, 64, 16, TERMS>(d, st);
     if (d.dz.p && l.lanes == 256) return held<T, 256, 16, TERMS>(d, st);
     if (d.dz.p && l.lanes == 512) return held<T, 512, 16, TERMS>(d, st);
     if (d.dz.p && l.lanes == 1024) return held<T, 1024, 16, TERMS>(d, st);
     const Ranges r = ranges_of(d.rows, d.n);
     d.ranges = r.count, d.range = r.length;
     if (r.count == 1 || !d.parts) {
-        hipLaunchKernelGGL((mv_distill_loss_kernel<T, TERMS>), dim3(grid_of(d.rows, 1 << 20)), dim3(kStreamThreads), list_bytes(d.top), st, d);
+        with_threads(d.rows, d.n / kChunk<T>, 4000, [&](auto threads) {
+            constexpr int kThreads = decltype(threads)::value;
+            hipLaunchKernelGGL((mv_distill_loss_kernel<T, kThreads, TERMS>), dim3(grid_of(d.rows, 1 << 20)), dim3(kThreads), list_bytes(d.top), st,
+                               d);
+        });
     } else {
-        hipLaunchKernelGGL((mv_distill_range_kernel<T, TERMS>), dim3(grid_of(d.rows * r.count, 1 << 20)), dim3(kStreamThreads), 0, st, d);
+        hipLaunchKernelGGL((mv_distill_range_kernel<T, TERMS>), dim3(grid_of(d.rows * r.count, 1 << 20)), dim3(kRangeThreads), 0, st, d);
         hipLaunchKernelGGL((mv_distill_join_kernel<T, TERMS>), dim3(grid_of(d.rows, 1 << 20)), dim3(64), list_bytes(d.top), st, d);
     }
     if (d.dz.p) {
         d.had = d.stats;
-        grad<T, TERMS>(d, st);
+        grad<T, TERMS>(d, l, st);
     }
 }
 
@@ -808,10 +832,11 @@ mv_status mv_distill_grad(const void* logits, int32_t dtype, int64_t ld_z, int64
         !fill(d, logits, dtype, ld_z, rows, n, idx, ld_idx, t, t_dtype, ld_t, top, labels, temperature, soft, hard, grad, dz, dz_dtype, ld_dz))
         return MV_ERR_INVALID_ARG;
     d.had = stats;
+    const Lanes l = lanes_of(rows, n, dtype, d.top);
     hipStream_t st = static_cast<hipStream_t>(stream);
     return with_terms(d, temperature, [&](auto terms) {
-        if (dtype == MV_BF16) mvr::grad<uint16_t, decltype(terms)::value>(d, st);
-        else mvr::grad<float, decltype(terms)::value>(d, st);
+        if (dtype == MV_BF16) mvr::grad<uint16_t, decltype(terms)::value>(d, l, st);
+        else mvr::grad<float, decltype(terms)::value>(d, l, st);
     });
 }
 

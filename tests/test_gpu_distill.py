@@ -128,7 +128,7 @@ def scratch_of(rows, n):
 
 
 SHAPES = [(1, 1, 1), (3, 2, 2), (96, 10, 4), (5, 100, 7), (6, 100, 200), (4, 1000, 50), (2, 2048, 64), (7, 2049, 3), (3, 5000, 100),
-          (2, 8193, 300), (4, 16_385, 40), (2, 33_000, 20), (2, 65_537, 5), (3, 131_073, 33), (1, 300_001, 64), (1100, 300, 9)]
+          (2, 8193, 300), (4, 16_385, 40), (2, 33_000, 20), (2, 65_537, 5), (3, 131_073, 33), (1, 300_001, 64), (1100, 300, 9), (1010, 2300, 7)]
 
 
 @pytest.mark.parametrize("src,dst", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")])
@@ -231,7 +231,7 @@ def test_in_place(n, src):
 
 
 @pytest.mark.parametrize("src", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,n,top", [(4200, 70, 5), (1100, 1500, 30), (1030, 2100, 70), (520, 20_001, 9), (300, 36_001, 5), (270, 69_700, 40)])
+@pytest.mark.parametrize("rows,n,top", [(4200, 70, 5), (6200, 100, 5), (4200, 1300, 6), (4200, 2200, 6), (1100, 1500, 30), (1030, 2100, 70), (520, 20_001, 9), (300, 36_001, 5), (270, 69_700, 40)])
 def test_more_rows_than_run_at_once(rows, n, top, src):
     """Rows that take turns in a workgroup, each fetched while the one before is at work; in place."""
     z, idx, t, label = make(rows, n, top, src, rows + n)
