@@ -5,7 +5,7 @@
 //
 // Memory bounds both: a row is read once, into registers, and written once.  A workgroup takes row after row, with gamma and
 // beta (for the gradients: gamma, and the sums for dgamma and dbeta) of its threads' columns in registers, and the next row
-// on its way meanwhile.  16,384 x 8192 bf16 forward 101 us, 5.3 TB/s, fp32 198, 5.4; backward 162 and 298, 5.0 and 5.4, the
+// on its way meanwhile.  16,384 x 8192 bf16 forward 98 us, 5.5 TB/s, fp32 198, 5.4; backward 152 and 297, 5.3 and 5.4, the
 // join of the workgroups' sums (4 to 5 us) among them.
 //
 // The mean is formed first and the squares are those of the differences from it; what the mean's own rounding left over,
@@ -41,7 +41,9 @@ __device__ __forceinline__ void load_weights(const Any& from, int64_t n, uint32_
 
 __device__ __forceinline__ float rstd_of(float var, float eps) { return 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps); }
 
-template <typename T, int LANES, int C>
+// AHEAD: the next row by load_ahead.  Of bf16, whose rows may end in a chunk of up to seven values, 32,768 x 2047 77 -> 61 us, whole
+// chunks 32,768 x 4096 107 -> 102; those of 1024 threads, 8192 x 16,384 99 -> 109, and fp32 rows, 32,768 x 1536 78 -> 94, come as others do.
+template <typename T, int LANES, int C, bool AHEAD>
 __global__ __launch_bounds__(kThreadsOf<LANES>) void mv_layernorm_kernel(Forward f)
 {
     constexpr int V = kChunk<T>, kRows = kThreadsOf<LANES> / LANES;
@@ -58,7 +60,8 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) void mv_layernorm_kernel(Forward
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int64_t col = (int64_t)(c * LANES + t) * V;
-            next[c].load(x + row * f.ld_x + col, row < f.rows ? f.n - col : 0);
+            if constexpr (AHEAD) load_ahead(next[c], x + row * f.ld_x, col, row < f.rows ? f.n - col : 0);
+            else next[c].load(x + row * f.ld_x + col, row < f.rows ? f.n - col : 0);
         }
     };
     int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
@@ -70,6 +73,7 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) void mv_layernorm_kernel(Forward
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             v[c] = next[c];
+            if (AHEAD) v[c].settle((int)f.n - (c * LANES + (int)t) * V);
 #pragma unroll
             for (int i = 0; i < V; ++i) sum += v[c].at(i);
         }
@@ -90,6 +94,8 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) void mv_layernorm_kernel(Forward
         more *= share;
         const float rstd = rstd_of(squares * share - more * more, f.eps);
         if (row >= f.rows) continue;
+        // the next row is waited for here, or it would be together with these stores
+        __builtin_amdgcn_s_waitcnt(kNoLoads);
         if (t == 0) {
             if (f.mean) f.mean[row] = mean + more;
             if (f.rstd) f.rstd[row] = rstd;
@@ -173,7 +179,9 @@ struct Backward {
     float*       sums;                  // of long rows: mean(d) and mean(d h)
 };
 
-template <typename T, int LANES, int C>
+// AHEAD: as there.  bf16 32,768 x 2047 203 -> 100 us, x 1100 126 -> 71, 16,384 x 8192 162 -> 150; fp32 32,768 x 1100 112 -> 92, but x 4096
+// 296 -> 309: of fp32 rows up to 2048 only.
+template <typename T, int LANES, int C, bool AHEAD>
 __global__ __launch_bounds__(kThreadsOf<LANES>) void mv_layernorm_grad_kernel(Backward b)
 {
     constexpr int V = kChunk<T>, kRows = kThreadsOf<LANES> / LANES;
@@ -185,24 +193,35 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) void mv_layernorm_grad_kernel(Ba
     float gamma[C][V], dgamma[C][V] = {}, dbeta[C][V] = {};
     load_weights<T, LANES, C>(b.gamma, b.n, t, 1.0f, gamma);
     Chunk<T> next_x[C], next_dy[C];
+    float    next_mean = 0.0f, next_rstd = 0.0f;
     auto fetch = [&](int64_t row) {
+        if constexpr (AHEAD) next_mean = b.mean[row < b.rows ? row : b.rows - 1], next_rstd = b.rstd[row < b.rows ? row : b.rows - 1];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int64_t col = (int64_t)(c * LANES + t) * V, live = row < b.rows ? b.n - col : 0;
-            next_x[c].load(x + row * b.ld_x + col, live);
-            next_dy[c].load(dy + row * b.ld_dy + col, live);
+            if constexpr (AHEAD) {
+                load_ahead(next_x[c], x + row * b.ld_x, col, live);
+                load_ahead(next_dy[c], dy + row * b.ld_dy, col, live);
+            } else {
+                next_x[c].load(x + row * b.ld_x + col, live);
+                next_dy[c].load(dy + row * b.ld_dy + col, live);
+            }
         }
     };
     int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
     const int64_t step = (int64_t)gridDim.x * kRows;
     fetch(row);
     for (int64_t first = (int64_t)blockIdx.x * kRows; first < b.rows; first += step, row += step) {
-        const bool live_row = row < b.rows;
-        const float mean = live_row ? b.mean[row] : 0.0f, rstd = live_row ? b.rstd[row] : 0.0f;
+        const bool  live_row = row < b.rows;
+        const float mean = live_row ? AHEAD ? next_mean : b.mean[row] : 0.0f, rstd = live_row ? AHEAD ? next_rstd : b.rstd[row] : 0.0f;
         Chunk<T> vx[C], vdy[C];
         float along = 0.0f, both = 0.0f;
 #pragma unroll
-        for (int c = 0; c < C; ++c) vx[c] = next_x[c], vdy[c] = next_dy[c];
+        for (int c = 0; c < C; ++c) {
+            vx[c] = next_x[c], vdy[c] = next_dy[c];
+            const int live = live_row ? (int)b.n - (c * LANES + (int)t) * V : 0;
+            if (AHEAD) vx[c].settle(live), vdy[c].settle(live);
+        }
         fetch(row + step);
 #pragma unroll
         for (int c = 0; c < C; ++c)
@@ -396,7 +415,15 @@ static void forward_of(const Forward& f, hipStream_t st)
 {
     constexpr int kRows = kThreadsOf<LANES> / LANES;
     const int64_t groups = (f.rows + kRows - 1) / kRows, most = 2048 * 256 / kThreadsOf<LANES>;
-    hipLaunchKernelGGL((mv_layernorm_kernel<T, LANES, C>), dim3((uint32_t)(groups < most ? groups : most)), dim3(kThreadsOf<LANES>), 0, st, f);
+    const dim3 grid((uint32_t)(groups < most ? groups : most)), threads(kThreadsOf<LANES>);
+    if constexpr (sizeof(T) == 2) {
+        if (LANES == 64 ? f.n >= kChunk<T> : LANES < 1024 || f.n % kChunk<T> != 0) {
+            hipLaunchKernelGGL((mv_layernorm_kernel<T, LANES, C, true>), grid, threads, 0, st, f);
+            return;
+        }
+    }
+    if constexpr (sizeof(T) == 4 || LANES == 64 || LANES == 1024)
+        hipLaunchKernelGGL((mv_layernorm_kernel<T, LANES, C, false>), grid, threads, 0, st, f);
 }
 template <typename T>
 static void forward(const Forward& f, const Held& h, hipStream_t st)
@@ -436,7 +463,15 @@ template <typename T, int LANES, int C>
 static uint32_t backward_of(const Backward& b, const Held& h, hipStream_t st)
 {
     const uint32_t grid = (uint32_t)parts_of(b.rows, h, sizeof(T) == 2);
-    hipLaunchKernelGGL((mv_layernorm_grad_kernel<T, LANES, C>), dim3(grid), dim3(kThreadsOf<LANES>), 0, st, b);
+    constexpr bool kAlways = LANES > 64 && (sizeof(T) == 2 || LANES == 256), kNever = LANES > 256 && sizeof(T) == 4;
+    if constexpr (!kNever) {
+        if (kAlways || b.n >= kChunk<T>) {
+            hipLaunchKernelGGL((mv_layernorm_grad_kernel<T, LANES, C, true>), dim3(grid), dim3(kThreadsOf<LANES>), 0, st, b);
+            return grid;
+        }
+    }
+    if constexpr (!kAlways)
+        hipLaunchKernelGGL((mv_layernorm_grad_kernel<T, LANES, C, false>), dim3(grid), dim3(kThreadsOf<LANES>), 0, st, b);
     return grid;
 }
 template <typename T>

@@ -44,6 +44,19 @@ struct Chunk<float> {
             for (int i = 0; i < 4; ++i) x[i] = i < live ? p[i] : -kInf;
     }
     __device__ __forceinline__ void load(const float* p, int64_t live) { mvx::load4(p, live, x); }
+    // What a chunk that a row ends in has been loaded from ends where the row does: its first `live` values are the last ones.
+    __device__ __forceinline__ void settle(int live)
+    {
+        const int s = live > 0 && live < 4 ? 4 - live : 0;
+        if (s & 1) x[0] = x[1], x[1] = x[2], x[2] = x[3], x[3] = 0.0f;
+        if (s & 2) x[0] = x[2], x[1] = x[3], x[2] = x[3] = 0.0f;
+    }
+    __device__ __forceinline__ void none_at_all() { x[0] = x[1] = x[2] = x[3] = 0.0f; }
+    __device__ __forceinline__ void load_whole(const float* p)
+    {
+        const mvx::f32x4u v = *reinterpret_cast<const mvx::f32x4u*>(p);
+        x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+    }
     __device__ __forceinline__ float at(int i) const { return x[i]; }
 };
 template <>
@@ -65,8 +78,33 @@ struct Chunk<uint16_t> {
                 x[i] = (2 * i < live ? p[2 * i] : 0xFF80u) | (2 * i + 1 < live ? (uint32_t)p[2 * i + 1] : 0xFF80u) << 16;
     }
     __device__ __forceinline__ void load(const uint16_t* p, int64_t live) { mvx::load8(p, live, x); }
+    __device__ __forceinline__ void settle(int live)
+    {
+        const int s = live > 0 && live < 8 ? 8 - live : 0;
+        if (s & 1)
+            x[0] = __builtin_amdgcn_alignbit(x[1], x[0], 16), x[1] = __builtin_amdgcn_alignbit(x[2], x[1], 16),
+            x[2] = __builtin_amdgcn_alignbit(x[3], x[2], 16), x[3] >>= 16;
+        if (s & 2) x[0] = x[1], x[1] = x[2], x[2] = x[3], x[3] = 0;
+        if (s & 4) x[0] = x[2], x[1] = x[3], x[2] = x[3] = 0;
+    }
+    __device__ __forceinline__ void none_at_all() { x[0] = x[1] = x[2] = x[3] = 0; }
+    __device__ __forceinline__ void load_whole(const uint16_t* p)
+    {
+        const mvx::u32x4u v = *reinterpret_cast<const mvx::u32x4u*>(p);
+        x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+    }
     __device__ __forceinline__ float at(int i) const { return i & 1 ? __uint_as_float(x[i / 2] & 0xFFFF0000u) : mvx::widen(x[i / 2]); }
 };
+
+// Loads that are on their way while others are at work leave what they bring as it is: a row's last values one by one, each
+// waited for, would hold everything up.  A chunk that a row ends in is the row's last values, to be settled when they are used; of
+// rows with at least one chunk's.  `live`: values from `col` on.
+template <typename T>
+__device__ __forceinline__ void load_ahead(Chunk<T>& c, const T* row, int64_t col, int64_t live)
+{
+    c.none_at_all();
+    if (live > 0) c.load_whole(row + col + (live < kChunk<T> ? live - kChunk<T> : 0));
+}
 
 // Chunk-sized runs of fp32 or bf16 at any address, in a type that only the call knows.
 struct Any {
