@@ -416,13 +416,14 @@ static void forward_of(const Forward& f, hipStream_t st)
     constexpr int kRows = kThreadsOf<LANES> / LANES;
     const int64_t groups = (f.rows + kRows - 1) / kRows, most = 2048 * 256 / kThreadsOf<LANES>;
     const dim3 grid((uint32_t)(groups < most ? groups : most)), threads(kThreadsOf<LANES>);
+    constexpr bool kShort = LANES == 64 && C * kChunk<T> == 8;           // perhaps no chunk long
     if constexpr (sizeof(T) == 2) {
-        if (LANES == 64 ? f.n >= kChunk<T> : LANES < 1024 || f.n % kChunk<T> != 0) {
+        if (kShort ? f.n >= kChunk<T> : LANES < 1024 || f.n % kChunk<T> != 0) {
             hipLaunchKernelGGL((mv_layernorm_kernel<T, LANES, C, true>), grid, threads, 0, st, f);
             return;
         }
     }
-    if constexpr (sizeof(T) == 4 || LANES == 64 || LANES == 1024)
+    if constexpr (sizeof(T) == 4 || kShort || LANES == 1024)
         hipLaunchKernelGGL((mv_layernorm_kernel<T, LANES, C, false>), grid, threads, 0, st, f);
 }
 template <typename T>
@@ -463,7 +464,7 @@ template <typename T, int LANES, int C>
 static uint32_t backward_of(const Backward& b, const Held& h, hipStream_t st)
 {
     const uint32_t grid = (uint32_t)parts_of(b.rows, h, sizeof(T) == 2);
-    constexpr bool kAlways = LANES > 64 && (sizeof(T) == 2 || LANES == 256), kNever = LANES > 256 && sizeof(T) == 4;
+    constexpr bool kShort = LANES == 64 && C * kChunk<T> == 8, kNever = LANES > 256 && sizeof(T) == 4, kAlways = !kShort && !kNever;
     if constexpr (!kNever) {
         if (kAlways || b.n >= kChunk<T>) {
             hipLaunchKernelGGL((mv_layernorm_grad_kernel<T, LANES, C, true>), dim3(grid), dim3(kThreadsOf<LANES>), 0, st, b);
