@@ -768,23 +768,6 @@ static mv_status launch_plain(const Wanted& w, hipStream_t st)
     return hipGetLastError() == hipSuccess ? MV_OK : MV_ERR_DEVICE;
 }
 
-// The kernel for few rows on codes: which factor's rows are the few ones.
-static FewCut few_codes_cut(const Wanted& w, bool& few_a)
-{
-    few_a = w.a.rows <= w.b.rows;
-    FewCut c = few_a ? few_cut(w.a.rows, w.b.rows, w.k, 0) : few_cut(w.b.rows, w.a.rows, w.k, 0);
-    if (!c.mt) {
-        few_a = !few_a;
-        c = few_a ? few_cut(w.a.rows, w.b.rows, w.k, 0) : few_cut(w.b.rows, w.a.rows, w.k, 0);
-    }
-    return c;
-}
-static FewProduct<uint8_t> few_codes(const Wanted& w, bool few_a)
-{
-    const Factor& few = few_a ? w.a : w.b;
-    return few_product(few_a ? w.b : w.a, Few<uint8_t>{few.codes, few.ld_bytes, few.scales, few.ld_scales, (uint32_t)few.rows}, w.k, w.c,
-                       few_a ? 1 : w.ld_c, few_a ? w.ld_c : 1);
-}
 // Whether a tile's byte offsets fit 32 bits: those of rows that there are stay below 2^31, where the loads of blocks that there
 // are not begin, and those of all rows of a tile below 2^32.
 static bool offsets_fit(const Factor& f, int64_t blocks, int mt)
@@ -795,6 +778,33 @@ static bool offsets_fit(const Factor& f, int64_t blocks, int mt)
 }
 static bool offsets_fit(const Wanted& w, int mt) { return offsets_fit(w.a, blocks_of(w.k), mt) && offsets_fit(w.b, blocks_of(w.k), mt); }
 
+// The kernel for few rows has a workgroup for 16 of the many rows and all of k.  Where those are few and k is long, the tiles, which
+// split it over the units, are faster, if a tile's offsets fit.  us of few rows and of tiles, fp32 results, codes: 16 x 16 by
+// 8192 10.7, 10.1, by 131,072 126, 12; 16 x 1000 by 8192 11.0, 11.2, by 16,384 18.9, 11.8; 1 x 512 by 16,384 12.5, 10.2; 3 x 5 by 16,384
+// 9.3, 9.5, by 2,000,000 773, 50; 16 x 2048 by 32,768 34.8, 22.1; 16 x 4096 37.9, 35.3.  Values, with the launch that quantises them:
+// 16 x 64 by 12,288 fp32 17.6, 12.8; 1 x 1000 by 16,384 13.3, 13.1; 1 x 2048 by 16,384 14.2, 17.3, by 32,768 24.2, 23.2.
+static bool long_sum(int64_t few, int64_t many, int64_t k)
+{
+    return many <= 1024 ? k > (few > 4 ? 8192 : 16384) : many <= 2048 && k > 32768;
+}
+// The kernel for few rows on codes: which factor's rows are the few ones.
+static FewCut few_codes_cut(const Wanted& w, bool& few_a)
+{
+    few_a = w.a.rows <= w.b.rows;
+    FewCut c = few_a ? few_cut(w.a.rows, w.b.rows, w.k, 0) : few_cut(w.b.rows, w.a.rows, w.k, 0);
+    if (!c.mt) {
+        few_a = !few_a;
+        c = few_a ? few_cut(w.a.rows, w.b.rows, w.k, 0) : few_cut(w.b.rows, w.a.rows, w.k, 0);
+    }
+    if (c.mt && long_sum(few_a ? w.a.rows : w.b.rows, few_a ? w.b.rows : w.a.rows, w.k) && offsets_fit(w, 2)) return FewCut{};
+    return c;
+}
+static FewProduct<uint8_t> few_codes(const Wanted& w, bool few_a)
+{
+    const Factor& few = few_a ? w.a : w.b;
+    return few_product(few_a ? w.b : w.a, Few<uint8_t>{few.codes, few.ld_bytes, few.scales, few.ld_scales, (uint32_t)few.rows}, w.k, w.c,
+                       few_a ? 1 : w.ld_c, few_a ? w.ld_c : 1);
+}
 template <bool PAIR>
 static void launch_tiles(const Launch<Product, PAIR>& l, int mt, bool one_buffer, bool wide, uint32_t groups, hipStream_t st)
 {
@@ -932,13 +942,13 @@ mv_status mv_f8_linear(const void* x, int32_t x_dtype, int64_t ld_x, const uint8
     const Factor w = {w_codes, w_scales, ld_bytes, ld_scales, n};
     const Out out = {y, y_dtype == MV_BF16};
     const FewCut cut = few_cut(m, n, k, x_dtype == MV_BF16 ? kQuantisedBf16 : kQuantisedF32);
-    if (cut.mt)
-        return x_dtype == MV_BF16 ? launch_few_values<uint16_t>(cut, x, ld_x, m, w, k, out, ld_y, st)
-                                  : launch_few_values<float>(cut, x, ld_x, m, w, k, out, ld_y, st);
     char* at = static_cast<char*>(scratch);
     const Held q = carve(at, m, k);
-    if (const mv_status rc = launch_encode({x, ld_x, m, k}, x_dtype, q, st)) return rc;
     const Wanted p = {factor_of(q), w, k, out, ld_y, at};
+    if (cut.mt && !(long_sum(m, n, k) && offsets_fit(p, 2)))
+        return x_dtype == MV_BF16 ? launch_few_values<uint16_t>(cut, x, ld_x, m, w, k, out, ld_y, st)
+                                  : launch_few_values<float>(cut, x, ld_x, m, w, k, out, ld_y, st);
+    if (const mv_status rc = launch_encode({x, ld_x, m, k}, x_dtype, q, st)) return rc;
     return launch_products(&p, 1, st);
 }
 
