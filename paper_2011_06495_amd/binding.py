@@ -896,8 +896,12 @@ def _list(idx, top, labels, rows: int, device: int):
         if r != rows or idx.dtype != _int32 or (k > 1 and step != 1) or idx.get_device() != device:
             raise ValueError("idx has to be %d rows of int32 on the same GPU, each in one piece" % rows)
         if k:
+            if top is None:
+                raise ValueError("idx names coordinates that top has no logits of")
             i, ld_i = idx.data_ptr(), ld_i if rows > 1 else max(ld_i, k)
             t, td, ld_t = _matrix(top, "top", rows, k, device)
+    elif top is not None:
+        raise ValueError("top has logits of coordinates that no idx names")
     if labels is not None:
         if labels.dtype != _int32 or labels.numel() != rows or not labels.is_contiguous() or labels.get_device() != device:
             raise ValueError("labels have to be %d contiguous int32 on the same GPU" % rows)
