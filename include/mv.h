@@ -615,8 +615,9 @@ mv_status mv_f8_linear_grad(const void* x, int64_t ld_x, const void* dy, int64_t
  * out, what the backward pass takes; either may be NULL.  y may be x itself, with its type
  * and stride.  Sums are fp32; the squares are those of differences from the mean, so rows far from
  * zero keep their digits.  A row that holds an infinity or a NaN, or whose sums leave fp32, has no
- * finite results, and no other row is touched by it.  eps >= 0 and finite; with eps 0 a row of
- * equal values has an infinite rstd, or one as large as its mean's rounding makes it.
+ * finite y and rstd, and no other row's are touched by it.  eps >= 0 and finite; with eps 0 a row of
+ * equal values has an infinite rstd, or one as large as its mean's rounding makes it, and so has a row
+ * whose squared differences are too small for fp32.
  *
  * These calls run on the CURRENT device, are enqueued on `stream` and allocate nothing.
  * 1 <= rows, n < 2^31.  The order of all sums follows from sizes and types: equal calls

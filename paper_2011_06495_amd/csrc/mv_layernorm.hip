@@ -39,7 +39,12 @@ __device__ __forceinline__ void load_weights(const Any& from, int64_t n, uint32_
     }
 }
 
-__device__ __forceinline__ float rstd_of(float var, float eps) { return 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps); }
+// Squares that have left fp32 would make a reciprocal of 0 and so results of beta, which look as if they were some.
+__device__ __forceinline__ float rstd_of(float var, float eps)
+{
+    const float v = (var < 0.0f ? 0.0f : var) + eps;
+    return v < kInf ? 1.0f / sqrtf(v) : __builtin_nanf("");
+}
 
 // AHEAD: the next row by load_ahead.  Of bf16, whose rows may end in a chunk of up to seven values, 32,768 x 2047 77 -> 61 us, whole
 // chunks 32,768 x 4096 107 -> 102; those of 1024 threads, 8192 x 16,384 99 -> 109, and fp32 rows, 32,768 x 1536 78 -> 94, come as others do.
