@@ -678,11 +678,12 @@ mv_status mv_layernorm_backward(const void* x, int64_t ld_x, const void* dy, int
  *
  * mv_distill_loss forms loss and, where dz is wanted, the gradient in the same call;
  * mv_distill_grad forms the gradient alone from the stats of a call with the same logits,
- * lists, labels and weights.  Sums are fp32 in an order that follows from sizes and types.
- * soft and hard are finite, T is 2^-60 .. 2^60.  1 <= rows, n < 2^31.  Runs on the CURRENT
- * device, enqueued on `stream`; allocates nothing.  Apart from dz over logits no output
- * overlaps another argument.  scratch: device, 16-byte aligned, >= mv_distill_scratch_bytes(rows,
- * n) (0: may be NULL), one for each call, or graph that holds calls, that may run at the same
+ * lists, labels and weights: q = exp((z - stats[0]) / T) / stats[1], s = exp(z - stats[0]) /
+ * stats[2].  Sums are fp32 in an order that follows from sizes and types.  soft and hard are
+ * finite, T is 2^-60 .. 2^60.  1 <= rows, n < 2^31.  Runs on the CURRENT device, enqueued on
+ * `stream`; allocates nothing.  Apart from dz over logits no output overlaps another argument.
+ * scratch: device, 16-byte aligned, >= mv_distill_scratch_bytes(rows, n) (0: may be NULL), one
+ * for each call, or graph that holds calls, that may run at the same
  * time as others.
  * Errors: MV_ERR_INVALID_ARG, MV_ERR_DEVICE.
  */

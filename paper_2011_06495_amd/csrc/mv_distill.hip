@@ -325,7 +325,10 @@ constexpr int kSixteenOps = 0x4F70;     // s_waitcnt: no more than sixteen vecto
 // of the others need not have ended when the next row's maximum is looked for: waits count what was issued since, which takes a
 // store for each chunk, beyond the row's end as well, where the buffer drops it (4096 x 131,072 bf16 T = 2
 // 451 -> 432 us, T = 3 487 -> 449).
-template <typename T, int LANES, int C, int TERMS, bool AHEAD, int OUT>
+//
+// GIVEN: the gradient alone, from the stats of a call before (a variant of its own: asked at run time, loss and dz of 20,000 x 100 bf16
+// took 26.2 us instead of 24.1).
+template <typename T, int LANES, int C, int TERMS, bool AHEAD, int OUT, bool GIVEN>
 __global__ __launch_bounds__(kThreadsOf<LANES>, C == 4 ? 6 : 4) void mv_distill_kernel(Distill d)
 {
     constexpr int V = kChunk<T>, kRows = kThreadsOf<LANES> / LANES, kWaves = LANES / 64;
@@ -363,20 +366,26 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, C == 4 ? 6 : 4) void mv_distill_
         fetch_tail(row_at(row));
     }
     Entry entry, label;
-    float g = 1.0f;
+    float g = 1.0f, had[3];
     auto name = [&](int64_t of) {
         entry.name(d, of, t), label.name_label(d, of);
         if (d.grad) g = d.grad[of];
+        if constexpr (GIVEN) had[0] = d.had[3 * of], had[1] = d.had[3 * of + 1], had[2] = d.had[3 * of + 2];
     };
     if (wave == 0) name(row);
     if (OUT) __builtin_amdgcn_s_waitcnt(kNoLoads);                       // or the loop would wait for all of its own each time
     for (; row < d.rows; row += step) {
-        Largest<T> most;
-        most.look(tail);
+        float largest;
+        if constexpr (GIVEN) {
+            largest = had[0];
+        } else {
+            Largest<T> most;
+            most.look(tail);
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-            if (there(c)) most.look(held[c]);
-        float largest = wave_max(most.value());
+            for (int c = 0; c < C; ++c)
+                if (there(c)) most.look(held[c]);
+            largest = wave_max(most.value());
+        }
         if (wave == 0) {
             entry.take(d), label.take_label(d);
             entry.look(row_at(row), 0, d.n), label.look(row_at(row), 0, d.n);
@@ -395,12 +404,17 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, C == 4 ? 6 : 4) void mv_distill_
             for (int c = 0; c < kAhead; ++c) next.load_lds(ahead + (c * kWaves + wave) * 1024, t * 16, c * (LANES * 16));
         }
         float a = 0.0f, b = 0.0f;
-        add_up<T, TERMS>(tail, largest, d.scale, a, b);
+        if constexpr (GIVEN) {
+            static_assert(kWaves == 1, "sums of a wavefront's own");
+            a = had[1], b = had[2];
+        } else {
+            add_up<T, TERMS>(tail, largest, d.scale, a, b);
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-            if (there(c)) add_up<T, TERMS>(held[c], largest, d.scale, a, b);
-        a = wave_sum(a);
-        if (TERMS != kOne) b = wave_sum(b);
+            for (int c = 0; c < C; ++c)
+                if (there(c)) add_up<T, TERMS>(held[c], largest, d.scale, a, b);
+            a = wave_sum(a);
+            if (TERMS != kOne) b = wave_sum(b);
+        }
         float row_g = g;
         Terms w;
         if (wave == 0) w = take_list(d, list, row, row_at(row), entry, label, largest, 0, d.n);
@@ -416,8 +430,8 @@ __global__ __launch_bounds__(kThreadsOf<LANES>, C == 4 ? 6 : 4) void mv_distill_
             for (int i = 0; i < kWaves; ++i) a += sums[0][i], b += sums[1][i];
             w = shared, row_g = shared_g;
         }
-        if (TERMS == kOne) b = a;
-        if (t == 0) {
+        if (TERMS == kOne && !GIVEN) b = a;
+        if (t == 0 && !GIVEN) {
             if (d.loss) d.loss[row] = loss_of(d, w, largest, a, b);
             if (d.stats) {
                 d.stats[3 * row] = largest;
@@ -680,7 +694,7 @@ static Ranges ranges_of(int64_t rows, int64_t n)
 }
 inline uint32_t grid_of(int64_t groups, int64_t most) { return (uint32_t)(groups < most ? groups : most); }
 
-template <typename T, int LANES, int C, int TERMS>
+template <typename T, int LANES, int C, int TERMS, bool GIVEN = false>
 static void held(const Distill& d, hipStream_t st)
 {
     constexpr int kRows = kThreadsOf<LANES> / LANES;
@@ -688,7 +702,8 @@ static void held(const Distill& d, hipStream_t st)
     const dim3   grid(grid_of((d.rows + kRows - 1) / kRows, C == 4 ? 1536 : 256 * 1024 / kThreadsOf<LANES>)), group(kThreadsOf<LANES>);
     const size_t lists = kRows * list_bytes(d.top);
     auto launch = [&](auto ahead, auto out) {
-        hipLaunchKernelGGL((mv_distill_kernel<T, LANES, C, TERMS, decltype(ahead)::value, decltype(out)::value>), grid, group, lists, st, d);
+        hipLaunchKernelGGL((mv_distill_kernel<T, LANES, C, TERMS, decltype(ahead)::value, decltype(out)::value, GIVEN>), grid, group, lists,
+                           st, d);
     };
     const std::integral_constant<int, 0> any{};
     if constexpr (LANES < 1024) {
@@ -714,8 +729,8 @@ static void with_threads(int64_t rows, int64_t chunks, int64_t most256, F launch
 template <typename T, int TERMS>
 static void grad(Distill d, const Lanes& l, hipStream_t st)
 {
-    // The shortest rows as for the loss, whose sums are formed again: 8192 x 1000 bf16 14.5 us, from the stats 55.
-    if (l.chunks == 4) return held<T, 64, 4, TERMS>(d, st);
+    // The shortest rows in registers, as for the loss: 8192 x 1000 bf16 13.8 us, streaming by 55.
+    if (l.chunks == 4) return held<T, 64, 4, TERMS, true>(d, st);
     const Ranges r = ranges_of(d.rows, d.n);
     d.ranges = r.count, d.range = r.length;
     with_threads(d.rows * r.count, d.range / kChunk<T>, 2048, [&](auto threads) {
