@@ -287,24 +287,27 @@ __device__ __forceinline__ void patch(const Distill& d, const List& l, const Wei
         d.dz.put(row * d.ld_dz + at, w.of(Pair<TERMS>(z - w.largest, d.scale)) - w.g * off);
     };
     // these stores are behind the ones before without a wait: a wavefront's are in order
-    for (uint32_t j = lane; j - lane < d.top; j += 64) {
-        const int32_t at = j < d.top ? l.idx[j] : -1;
+    for (uint32_t base = 0; base < d.top; base += 64) {
+        const uint32_t j = base + lane;
+        const int32_t  at = j < d.top ? l.idx[j] : -1;
         bool  write = ours(at);
         float p = write ? l.p[j] : 0.0f;
-        // entries that share their slot, one by one: the first of a coordinate has the sum in the list's order
-        for (uint64_t met = __ballot(write && __float_as_uint(p) >> 31); met; met &= met - 1) {
+        // Entries that share their slot, one by one: the first of a coordinate has the sum in the list's order, and takes the others
+        // out of the list, so that a coordinate is looked for once, however often it is named (64 rows of 5000 with 4096 entries
+        // for one coordinate 0.2 ms; each of them looking for all 538).
+        for (uint64_t met = __ballot(write && __float_as_uint(p) >> 31); met;) {
             const int     whose = __builtin_ctzll(met);
             const int32_t name = __builtin_amdgcn_readlane(at, whose);
-            uint32_t first = d.top;
-            float    sum = 0.0f;
-            for (uint32_t i = 0; i < d.top; i += 64) {
+            float sum = 0.0f;
+            for (uint32_t i = base; i < d.top; i += 64) {
                 const bool same = i + lane < d.top && l.idx[i + lane] == name;
                 const float q = same ? l.p[i + lane] : 0.0f;
                 uint64_t hits = __ballot(same);
-                if (hits && first == d.top) first = i + __builtin_ctzll(hits);
+                if (i == base) met &= ~hits, write &= !same;
+                else if (same) l.idx[i + lane] = -1;
                 for (; hits; hits &= hits - 1) sum += fabsf(lane_of(q, __builtin_ctzll(hits)));
             }
-            if (lane == (uint32_t)whose) p = sum, write = first == j;
+            if (lane == (uint32_t)whose) p = sum, write = true;
         }
         if (write) put(at, l.z[j], fabsf(p));
     }
