@@ -460,9 +460,19 @@ static int64_t parts_of(int64_t rows, const Held& h, bool bf16)
     if (parts > most) parts = most;
     return parts < groups ? parts : groups;
 }
+// Of rows beyond the registers: tiles of columns, and workgroups that share the rows of each.
+static int64_t tiles_of(int64_t n, int chunk) { return (n + kColumnThreads * chunk - 1) / (kColumnThreads * chunk); }
+static int64_t deep_of(int64_t rows, int64_t n, int chunk)
+{
+    const int64_t most = tiles_of(n, chunk) < 64 ? 64 : 8;
+    return rows < most ? rows : most;
+}
+// Room for the parts of either type's rows: bf16's are never fewer.
 inline size_t parts_bytes(int64_t rows, int64_t n)
 {
-    return (size_t)(rows < kMostParts ? rows : kMostParts) * 2 * (size_t)pitch_of(n) * 4;
+    const Held h = held_of(n, true);
+    const int64_t parts = h.lanes ? parts_of(rows, h, true) : deep_of(rows, n, kChunk<uint16_t>);
+    return (size_t)parts * 2 * (size_t)pitch_of(n) * 4;
 }
 
 template <typename T, int LANES, int C>
@@ -493,9 +503,8 @@ static uint32_t backward(const Backward& b, const Held& h, hipStream_t st)      
     }
     if (b.dx.p)
         hipLaunchKernelGGL(mv_layernorm_grad_sums_kernel<T>, dim3((uint32_t)(b.rows < 512 ? b.rows : 512)), dim3(kLongThreads), 0, st, b);
-    const int64_t tiles = (b.n + kColumnThreads * kChunk<T> - 1) / (kColumnThreads * kChunk<T>), most = tiles < 64 ? 64 : 8;
-    const uint32_t deep = (uint32_t)(b.rows < most ? b.rows : most);
-    hipLaunchKernelGGL(mv_layernorm_grad_columns_kernel<T>, dim3((uint32_t)tiles, deep), dim3(kColumnThreads), 0, st, b);
+    const uint32_t deep = (uint32_t)deep_of(b.rows, b.n, kChunk<T>);
+    hipLaunchKernelGGL(mv_layernorm_grad_columns_kernel<T>, dim3((uint32_t)tiles_of(b.n, kChunk<T>), deep), dim3(kColumnThreads), 0, st, b);
     return deep;
 }
 
