@@ -571,7 +571,9 @@ mv_status mv_f8_decode(const uint8_t* codes, int64_t ld_bytes, const uint8_t* sc
 /*
  * c[i][j] = sum over k of a[i][k] * b[j][k], as mv_mx_product, in 8 bits along k; the order
  * of the sums follows from the arguments, as there.  An fp32 c is a sum in fp32 (a factor's
- * value counts to the nearest multiple of 2^-133).  A bf16 c may come from matrix instructions that
+ * value counts to the nearest multiple of 2^-133, and from 2^128 on, which scale bytes from 247 on
+ * reach and a quantised value from 248 * 2^120 on, as infinite: c is right or not finite then, in
+ * bf16, too).  A bf16 c may come from matrix instructions that
  * add eight neighbouring products at a time on a grid of 2^-13 of the largest one, cut
  * towards zero, and those sums in fp32: off by at most 7 * 2^-13 of the magnitudes' sum, and by less than
  * 2^-16 of it for normal values, before it is rounded to bf16.
