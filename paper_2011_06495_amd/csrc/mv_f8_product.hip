@@ -7,10 +7,14 @@
 // a row have one scale, so which of them its lanes hold does not matter as long as both factors agree, and the power of
 // two costs no instruction of its own.  But it adds each eight neighbouring products, before they join the fp32 sum, on a
 // grid 2^-13 below the largest of them, cut towards zero (measured with single products; normal values come out within
-// 2^-16.8 of the sum of the magnitudes, at worst 7 * 2^-13 of it).  That is far below the rounding of a bf16 result, and results
-// in bf16 are formed so.  For fp32 results codes become bf16 values, which holds each and its power of two exactly (down to
-// multiples of 2^-133), and v_mfma_f32_32x32x16_bf16 adds those to within 2^-23: half the rate, and two values an
-// instruction to convert.  Few rows, whose products are not what they wait for, always take that way.
+// 2^-16.8 of the sum of the magnitudes, rms 2^-21.9 of it in sums of 8192, at worst 7 * 2^-13 of it).  That is far below the rounding
+// of a typical bf16 result, and results in bf16 are formed so: of 4096 x 8192 by 8192 with random signs, whose magnitudes' sum is some
+// 70 times a typical result, 1.2 to 1.6 % are the other neighbour of the exact value, and the error against 64 bits is 0.0016576
+// where rounding alone makes 0.0016575; with products of one sign 0.06 %.  Results that nearly vanish keep that share of the
+// magnitudes, not of themselves; who needs those asks for fp32.  For fp32 results codes become bf16 values, which holds each and its
+// power of two exactly (down to multiples of 2^-133), and v_mfma_f32_32x32x16_bf16 adds those to within 2^-23: half the rate, and
+// two values an instruction to convert.  Few rows, whose products are not what they wait for, always take that way, but for small ones
+// beside another product.
 #include "mv_f8.hpp"
 #include "mv_product.hpp"
 
@@ -785,10 +789,10 @@ static bool offsets_fit(const Wanted& w, int mt) { return offsets_fit(w.a, block
 // 16 x 64 by 12,288 fp32 17.6, 12.8; 1 x 1000 by 16,384 13.3, 13.1; 1 x 2048 by 16,384 14.2, 17.3, by 32,768 24.2, 23.2.
 static bool long_sum(int64_t few, int64_t many, int64_t k)
 {
-    return many <= 1024 ? k > (few > 4 ? 8192 : 16384) : many <= 2048 && k > 32768;
+    return few <= kFewRows && (many <= 1024 ? k > (few > 4 ? 8192 : 16384) : many <= 2048 && k > 32768);
 }
-// The kernel for few rows on codes: which factor's rows are the few ones.
-static FewCut few_codes_cut(const Wanted& w, bool& few_a)
+// The kernel for few rows on codes: which factor's rows are the few ones; `split`: not taken because the tiles' splits are faster.
+static FewCut few_codes_cut(const Wanted& w, bool& few_a, bool& split)
 {
     few_a = w.a.rows <= w.b.rows;
     FewCut c = few_a ? few_cut(w.a.rows, w.b.rows, w.k, 0) : few_cut(w.b.rows, w.a.rows, w.k, 0);
@@ -796,8 +800,8 @@ static FewCut few_codes_cut(const Wanted& w, bool& few_a)
         few_a = !few_a;
         c = few_a ? few_cut(w.a.rows, w.b.rows, w.k, 0) : few_cut(w.b.rows, w.a.rows, w.k, 0);
     }
-    if (c.mt && long_sum(few_a ? w.a.rows : w.b.rows, few_a ? w.b.rows : w.a.rows, w.k) && offsets_fit(w, 2)) return FewCut{};
-    return c;
+    split = c.mt && long_sum(few_a ? w.a.rows : w.b.rows, few_a ? w.b.rows : w.a.rows, w.k) && offsets_fit(w, 2);
+    return split ? FewCut{} : c;
 }
 static FewProduct<uint8_t> few_codes(const Wanted& w, bool few_a)
 {
@@ -825,11 +829,16 @@ constexpr int64_t kFewBeside = 3 << 20;
 static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
 {
     FewCut few[2] = {};
-    bool few_a[2] = {};
+    bool few_a[2] = {}, split[2] = {};
     FewProduct<uint8_t> fp[2];
     for (int i = 0; i < n; ++i) {
-        few[i] = few_codes_cut(w[i], few_a[i]);
+        few[i] = few_codes_cut(w[i], few_a[i], split[i]);
         if (few[i].mt) fp[i] = few_codes(w[i], few_a[i]);
+        // by bf16 products like few rows' others, so not in a launch that forms bf16 results from 8-bit ones, unless it is small
+        if (n == 2 && split[i] && w[i].c.bf16 && (few_a[i] ? w[i].b.rows : w[i].a.rows) * w[i].k > kFewBeside) {
+            if (const mv_status rc = launch_products(w, 1, st)) return rc;
+            return launch_products(w + 1, 1, st);
+        }
     }
     if (n == 2 && few[0].mt && few[1].mt) return launch_few(fp, few, 2, st);
     if (n == 2 && (few[0].mt || few[1].mt)) {
@@ -869,7 +878,7 @@ static mv_status launch_products(const Wanted* w, int n, hipStream_t st)
     }
     const Product  p = product_of(w[0], cut[0]);
     const uint32_t firsts = (uint32_t)cut[0].groups();
-    const bool     wide = !w[0].c.bf16;
+    const bool     wide = !w[0].c.bf16 || (n == 1 && split[0]);
     if (n == 2) {
         const Launch<Product, true> l = {{p, product_of(w[1], cut[1])}, firsts};
         launch_tiles(l, cut[0].mt, one_buffer, wide, firsts + (uint32_t)cut[1].groups(), st);
