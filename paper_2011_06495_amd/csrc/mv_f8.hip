@@ -3,7 +3,7 @@
 // As with 4 bits each value is read and written once and a few instructions are spent on it: HBM bounds these kernels,
 // launches where they are short.  A block is sixteen lanes', eight values each, and its largest magnitude four DPP moves away.
 // 16,384 x 8192 rows bf16 70 us, 5.8 TB/s, fp32 119, 5.6; columns 95 and 157, 4.2 and 4.3: their codes go out as single lines
-// of 128 bytes, a row apart.
+// of 128 bytes, a row apart.  Read back to bf16 66 us, to fp32 112, both 6.0.
 #include "mv_f8.hpp"
 
 namespace mvf {

@@ -5,8 +5,9 @@
 //
 // Memory bounds both: a row is read once, into registers, and written once.  A workgroup takes row after row, with gamma and
 // beta (for the gradients: gamma, and the sums for dgamma and dbeta) of its threads' columns in registers, and the next row
-// on its way meanwhile.  16,384 x 8192 bf16 forward 98 us, 5.5 TB/s, fp32 198, 5.4; backward 152 and 297, 5.3 and 5.4, the
-// join of the workgroups' sums (4 to 5 us) among them.
+// on its way meanwhile.  16,384 x 8192 bf16 forward 98 us, 5.5 TB/s, fp32 199, 5.4; backward 152 and 298, 5.3 and 5.4, the
+// join of the workgroups' sums (4 to 5 us) among them.  Rows beyond the registers are read again: 4096 x 30,000 bf16 forward 184 us, 2.7 of
+// what one read and one write would be, fp32 335, 2.9; backward (8192 x 16,384) 279 and 498, 2.9 and 3.2.
 //
 // The mean is formed first and the squares are those of the differences from it; what the mean's own rounding left over,
 // the differences' mean, is taken off them and out of the variance, so rows far from zero keep their digits.
@@ -47,7 +48,8 @@ __device__ __forceinline__ float rstd_of(float var, float eps)
 }
 
 // AHEAD: the next row by load_ahead.  Of bf16, whose rows may end in a chunk of up to seven values, 32,768 x 2047 77 -> 61 us, whole
-// chunks 32,768 x 4096 107 -> 102; those of 1024 threads, 8192 x 16,384 99 -> 109, and fp32 rows, 32,768 x 1536 78 -> 94, come as others do.
+// chunks 32,768 x 4096 107 -> 102; those of 1024 threads, 8192 x 16,384 99 -> 109, and fp32 rows, 32,768 x 1536 78 -> 94, come as others do
+// (that is of whole chunks; those that end inside one, x 1023 58 us, x 2047 112, have 4.6 and 4.8 TB/s).
 template <typename T, int LANES, int C, bool AHEAD>
 __global__ __launch_bounds__(kThreadsOf<LANES>) void mv_layernorm_kernel(Forward f)
 {
@@ -400,7 +402,7 @@ __global__ __launch_bounds__(256) void mv_layernorm_join_kernel(const float* __r
 }
 
 // How a row is held: LANES threads with up to `values` of its values each, or 0: not at all.  Forward, sixteen values a thread are
-// as fast as eight, or faster (bf16 16,384 x 8192 102 us, by twice the threads 144).  With the sums for the weights eight
+// as fast as eight, or faster (bf16 16,384 x 8192 98 us, by twice the threads 144).  With the sums for the weights eight
 // are (16,384 x 4096 83, with sixteen 90), and rows beyond 8192 do not fit: 1024 threads with sixteen values each leave
 // registers (8192 x 16,384 bf16 369 us, fp32 861; read twice from memory 276 and 499).
 struct Held {

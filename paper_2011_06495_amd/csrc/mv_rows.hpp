@@ -14,7 +14,7 @@ constexpr float kInf = __builtin_inff();
 constexpr int   kNoLds = 0xC07F;        // s_waitcnt: no LDS access in flight
 constexpr int   kNoLoads = 0x0F70;      // s_waitcnt: none of the vector loads in flight, the other counters as they are
 
-// A row is LANES threads' (64, 256 or 1024); thread t has chunks t, t + LANES, ... of 16 bytes.
+// A row is LANES threads' (64, 256, 512 or 1024); thread t has chunks t, t + LANES, ... of 16 bytes.
 template <typename T>
 constexpr int kChunk = 16 / (int)sizeof(T);
 
@@ -133,10 +133,6 @@ struct Any {
                 }
             }
         }
-    }
-    __device__ __forceinline__ float at(int64_t i) const
-    {
-        return bf16 ? mvx::widen(static_cast<const uint16_t*>(p)[i]) : static_cast<const float*>(p)[i];
     }
 };
 struct AnyOut {
