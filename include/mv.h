@@ -635,7 +635,8 @@ mv_status mv_layernorm_forward(const void* x, int32_t x_dtype, int64_t ld_x, int
  *   dx     = rstd (d - sum(d) / n - h sum(d h) / n)     rounded once to dx's type
  *   dgamma = sum over rows of dy h,  dbeta = sum over rows of dy      (n fp32 each)
  *
- * x and dy have the same type; mean, rstd as the forward pass left them.  dx, dgamma and
+ * x and dy have the same type; mean, rstd as the forward pass left them.  A row whose mean times
+ * rstd is beyond fp32 (equal values, very large) may have no finite dx.  dx, dgamma and
  * dbeta may each be NULL, not all three; dx may be dy or x itself, with its type and stride.
  * Apart from that no output overlaps another argument, as in the forward pass.  scratch:
  * device, 16-byte aligned, >= mv_layernorm_scratch_bytes(rows, n), one for each call, or graph
