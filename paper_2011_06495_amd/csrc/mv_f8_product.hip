@@ -6,15 +6,16 @@
 // There are two ways to multiply.  v_mfma_scale_f32_32x32x64_f8f6f4 takes codes and scales as they are: all bytes that it takes of
 // a row have one scale, so which of them its lanes hold does not matter as long as both factors agree, and the power of
 // two costs no instruction of its own.  But it adds each eight neighbouring products, before they join the fp32 sum, on a
-// grid 2^-13 below the largest of them, cut towards zero (measured with single products; normal values come out within
-// 2^-16.8 of the sum of the magnitudes, rms 2^-21.9 of it in sums of 8192, at worst 7 * 2^-13 of it).  That is far below the rounding
-// of a typical bf16 result, and results in bf16 are formed so: of 4096 x 8192 by 8192 with random signs, whose magnitudes' sum is some
-// 70 times a typical result, 1.2 to 1.6 % are the other neighbour of the exact value, and the error against 64 bits is 0.0016576
-// where rounding alone makes 0.0016575; with products of one sign 0.06 %.  Results that nearly vanish keep that share of the
-// magnitudes, not of themselves; who needs those asks for fp32.  For fp32 results codes become bf16 values, which holds each and its
-// power of two exactly (down to multiples of 2^-133), and v_mfma_f32_32x32x16_bf16 adds those to within 2^-23: half the rate, and
-// two values an instruction to convert.  Few rows, whose products are not what they wait for, always take that way, but for small ones
-// beside another product.
+// grid 2^-13 below the largest of them, cut towards zero (measured with single products): at worst 7 * 2^-13 of the sum of the
+// magnitudes.  Normal values come out within 2^-12.7 of it where k is 8, 2^-15.2 at 128, 2^-17.4 at 768 and 2^-18.5 at 8192, rms
+// 2^-17.1, 2^-18.9, 2^-20.2 and 2^-21.9 (the products' eight bits lie on the grid but for those below 2^-6 of the largest).  That
+// is far below the rounding of a typical bf16 result, and results in bf16 are formed so: of 4096 x 8192 by 8192 with random signs,
+// whose magnitudes' sum is some 70 times a typical result, 1.2 to 1.6 % are the other neighbour of the exact value, and the error
+// against 64 bits is 0.0016576 where rounding alone makes 0.0016575; with products of one sign 0.06 %.  Results that nearly vanish
+// keep that share of the magnitudes, not of themselves; who needs those asks for fp32.  For fp32 results codes become bf16 values,
+// which holds each and its power of two exactly (down to multiples of 2^-133), and v_mfma_f32_32x32x16_bf16 adds those to within
+// 2^-23: half the rate, and two values an instruction to convert.  Few rows, whose products are not what they wait for, always
+// take that way, but for small ones beside another product.
 #include "mv_f8.hpp"
 #include "mv_product.hpp"
 
