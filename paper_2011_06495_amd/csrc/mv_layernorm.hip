@@ -469,12 +469,19 @@ static int64_t deep_of(int64_t rows, int64_t n, int chunk)
     const int64_t most = tiles_of(n, chunk) < 64 ? 64 : 8;
     return rows < most ? rows : most;
 }
-// Room for the parts of either type's rows: bf16's are never fewer.
+// Room for the parts of either type's rows (bf16's are never fewer), and of shorter rows: what is enough for a program's longest ones
+// is enough for all of them, though longer ones may have fewer parts.
 inline size_t parts_bytes(int64_t rows, int64_t n)
 {
-    const Held h = held_of(n, true);
-    const int64_t parts = h.lanes ? parts_of(rows, h, true) : deep_of(rows, n, kChunk<uint16_t>);
-    return (size_t)parts * 2 * (size_t)pitch_of(n) * 4;
+    size_t most = 0;
+    for (int64_t top : {(int64_t)1024, (int64_t)2048, (int64_t)4096, (int64_t)8192, (int64_t)63 * kColumnThreads * kChunk<uint16_t>, n}) {
+        const int64_t at = top < n ? top : n;
+        const Held    h = held_of(at, true);
+        const int64_t parts = h.lanes ? parts_of(rows, h, true) : deep_of(rows, at, kChunk<uint16_t>);
+        const size_t  bytes = (size_t)parts * 2 * (size_t)pitch_of(at) * 4;
+        if (bytes > most) most = bytes;
+    }
+    return most;
 }
 
 template <typename T, int LANES, int C>
