@@ -786,12 +786,14 @@ static bool offsets_fit(const Wanted& w, int mt) { return offsets_fit(w.a, block
 // The kernel for few rows has a workgroup for 16 of the many rows and all of k. Where those are few and k is long, the tiles,
 // which split it over the units, are faster, if a tile's offsets fit. us of few rows and of tiles, fp32 results, codes: 16 x 16 by
 // 10,300 11.9, 10.1, by 131,072 126, 12; 5 x 300 by 10,300 9.7, 10.3, by 12,288 11.4, 10.2; 16 x 1000 by 16,384 18.9, 11.5; 1 x
-// 1000 by 16,500 12.1, 11.5; 3 x 5 by 16,384 9.3, 9.5, by 2,000,000 773, 50; 16 x 2048 by 32,768 34.8, 22.1; 16 x 4096 37.9, 35.3.
-// Values, with the launch that quantises them: 16 x 16 by 10,300 fp32 14.6, 12.9; 5 x 16 bf16 11.4, 12.5, by 12,288 12.0, 12.4, by
-// 14,000 13.2, 12.4; 1 x 1000 by 16,384 fp32 13.3, 13.1; 1 x 2048 by 16,384 14.2, 17.3, by 32,768 24.2, 23.2.
+// 1000 by 16,500 12.1, 11.5; 1 x 1 by 16,384 6.5, 9.6, by 32,768 10.2, 9.6; 3 x 5 by 16,384 9.3, 9.5, by 2,000,000 773, 50; 16 x
+// 2048 by 32,768 34.8, 22.1; 16 x 4096 37.9, 35.3. Values, with the launch that quantises them: 16 x 16 by 10,300 fp32 14.6, 12.9;
+// 5 x 16 bf16 11.4, 12.5, by 12,288 12.0, 12.4, by 14,000 13.2, 12.4; 1 x 1000 by 16,384 fp32 13.3, 13.1; 1 x 2048 by 16,384 14.2,
+// 17.3, by 32,768 24.2, 23.2.
 static bool long_sum(int64_t few, int64_t many, int64_t k)
 {
-    return few <= kFewRows && (many <= 1024 ? k > (few > 4 ? 10240 : 16384) : many <= 2048 && k > 32768);
+    const int64_t from = many > 1024 || few * many < 8 ? 32768 : few > 4 ? 10240 : 16384;
+    return few <= kFewRows && many <= 2048 && k > from;
 }
 // The kernel for few rows on codes: which factor's rows are the few ones; `split`: not taken because the tiles' splits are faster.
 static FewCut few_codes_cut(const Wanted& w, bool& few_a, bool& split)
